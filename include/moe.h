@@ -322,6 +322,147 @@ moe_status moe_mse_loss(const moe_config* cfg, const void* out, const void* targ
 moe_status moe_sgd_update(void* w, const void* dw, float* w_master, int64_t n_groups, int64_t group_elems,
                           const int32_t* group_counts, float lr, moe_dtype dtype, moe_stream_t stream);
 
+/*
+ * Gating rules beyond Alg. 7 (HOST struct). A rule takes the picks and weights of a token from its
+ * router logits z [E]; E, k, P, normalize_topk come from the config:
+ *   s = sigmoid(z), or the softmax of z;
+ *   key = s + balance_bias (sigmoid), or z + balance_bias (softmax): the choice only, not the weights;
+ *   the experts are n_groups groups of E / n_groups consecutive ids; a group's key is the sum of its
+ *   group_top largest keys, the top_groups groups of the largest keys are kept (equal keys: the
+ *   lower group first);
+ *   I = the k largest keys of the kept groups in descending order (equal keys: lower id first);
+ *   w_j = scale * s[I_j] (divided by sum_j s[I_j] if normalize_topk).
+ * An expert whose logit is -inf or NaN is out of the token's reach: s = 0, and it comes after
+ * every other one of the kept groups. There are k picks all the same; one of s = 0 has weight 0
+ * and no gradient, and where all k have, none is divided by their sum.
+ */
+typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score;
+typedef struct {
+    int32_t score;      /* moe_score */
+    int32_t n_groups;   /* 1..32, divides E */
+    int32_t top_groups; /* 1..n_groups; the kept groups hold at least k experts */
+    int32_t group_top;  /* 1 or 2, at most E / n_groups */
+    float scale;        /* finite */
+} moe_gate_rule;
+
+/*
+ * Picks and weights by a rule, on fp32 logits (from moe_route, or the caller's own).
+ *   logits [T,E] f32       balance_bias [P,E] f32 or NULL (added to the keys of party p's tokens)
+ *   scores [T,E] f32 out or NULL: s (as probs for moe_aux_loss)
+ *   topk_idx [T,k] i32, topk_w [T,k] f32, counts [P,E] i32 out, as moe_route's
+ * With the same logits and bias the picks and counts are exact integers.
+ */
+moe_status moe_gate(const moe_config* cfg, const moe_gate_rule* rule, const float* logits,
+                    const float* balance_bias, const int32_t* party_offsets, float* scores,
+                    int32_t* topk_idx, float* topk_w, int32_t* counts, moe_stream_t stream);
+
+/* The logits of moe_route (x, w_router, router_bias as there; logits out), then moe_gate on them.
+ * scores is required here. */
+moe_status moe_route_gate(const moe_config* cfg, const moe_gate_rule* rule, const void* x,
+                          const void* w_router, const float* router_bias, const float* balance_bias,
+                          const int32_t* party_offsets, float* logits, float* scores,
+                          int32_t* topk_idx, float* topk_w, int32_t* counts, moe_stream_t stream);
+
+/*
+ * Backward of moe_gate (picks, groups and balance_bias are constants):
+ *   ds[t,e] = sum_j [topk_idx[t,j] == e] * g_tj + aux_coef[p(t),e]
+ *     with g_tj = scale * dtopk_w[t,j], or (scale * dtopk_w[t,j] - <dtopk_w[t], topk_w[t]>) /
+ *     sum_j s[t, topk_idx[t,j]] when normalize_topk (0 where that sum is 0);
+ *   dlogits = ds * s * (1 - s) (sigmoid), or s * (ds - <ds, s>) (softmax)   [T,E] f32 out
+ * aux_coef [P,E] or NULL. A pick outside [0, E) adds nothing and is recorded as
+ * MOE_ERR_DEVICE_CHECK (moe_device_status).
+ * With dw_router, also the router's gradients from dlogits: dw_router, dbias, dx_router, x,
+ * w_router and workspace as in moe_route_bwd. Without it (NULL) these are all unused.
+ */
+moe_status moe_gate_bwd(const moe_config* cfg, const moe_gate_rule* rule, const float* logits,
+                        const int32_t* topk_idx, const float* dtopk_w, const float* aux_coef,
+                        const int32_t* party_offsets, float* dlogits, const void* x,
+                        const void* w_router, void* dw_router, float* dbias, void* dx_router,
+                        void* workspace, size_t workspace_bytes, moe_stream_t stream);
+
+/*
+ * The balance bias after a batch: bias_out[p,e] = bias_in[p,e] + rate * sign(mean_e' counts[p,e'] -
+ * counts[p,e]), the comparison in whole numbers. counts [P,E] i32, bias_in, bias_out [P,E] f32
+ * (the same buffer for an update in place).
+ */
+moe_status moe_gate_balance(const moe_config* cfg, const int32_t* counts, float rate,
+                            const float* bias_in, float* bias_out, moe_stream_t stream);
+
+/*
+ * Layer norm with the residual sum in front of it, on `rows` rows of d elements:
+ *   h = x + residual (residual NULL: h = x), y = (h - mean) * rstd * gamma + beta,
+ *   mean = sum h / d, rstd = 1 / sqrt(sum (h - mean)^2 / d + eps), all in fp32 on the unrounded sum.
+ *   x, residual [rows,d] dtype; gamma, beta [d] f32 (beta may be NULL); y [rows,d] dtype out
+ *   h [rows,d] dtype out: the sum, rounded (required with a residual, NULL without)
+ *   mean, rstd [rows] f32 out, for the backward (both or neither)
+ *   h_q [rows,d] i8, h_scale [rows, ceil(d/128)] f32 out or NULL: the stored h as moe_ckpt_pack
+ *     holds it
+ * rows in [0, 2^31), d in [1, 16384] (MOE_ERR_UNSUPPORTED above), any alignment of whole elements;
+ * 16-byte aligned buffers with a width of whole 16-byte vectors take the wide path.
+ */
+moe_status moe_layer_norm_fwd(int64_t rows, int32_t d, moe_dtype dtype, const void* x,
+                              const void* residual, const float* gamma, const float* beta, float eps,
+                              void* h, void* y, float* mean, float* rstd, int8_t* h_q,
+                              float* h_scale, moe_stream_t stream);
+
+/* Bytes of workspace for moe_layer_norm_bwd. Host only. */
+moe_status moe_layer_norm_workspace_size(int64_t rows, int32_t d, size_t* bytes /* HOST out */);
+
+/*
+ * Backward of moe_layer_norm_fwd, with xh = (h - mean) * rstd and g = dy * gamma:
+ *   dx = dh + rstd * (g - sum(g)/d - xh * sum(g*xh)/d)     (the gradient of x and of residual)
+ *   dgamma = sum over rows of dy * xh, dbeta = sum over rows of dy      [d] f32 out
+ *   dy [rows,d] dtype; h [rows,d] dtype, or h_q and h_scale (its checkpoint) with h NULL;
+ *   mean, rstd [rows] from the forward; dh [rows,d] dtype or NULL: the gradient that reaches h
+ *   past the norm; dx [rows,d] dtype out; dbeta may be NULL.
+ * Deterministic: partial sums of fixed rows in the workspace, added in a fixed order.
+ */
+moe_status moe_layer_norm_bwd(int64_t rows, int32_t d, moe_dtype dtype, const void* dy,
+                              const void* h, const int8_t* h_q, const float* h_scale,
+                              const float* mean, const float* rstd, const float* gamma,
+                              const void* dh, void* dx, float* dgamma, float* dbeta,
+                              void* workspace, size_t workspace_bytes, moe_stream_t stream);
+
+/*
+ * Activation checkpoints in 8 bits. Every 128 columns of a row (fewer at its end) are a block of int8
+ * with one fp32 scale:
+ *   a = max |x|, scale = a / 127, q = rint(x * (127 / a)), value = q * scale
+ * (off by at most a / 254 and the arithmetic's rounding). A block with a < 2^-100 holds zeros; one
+ * with an infinity or NaN has scale NaN, so that all of its values are NaN.
+ *   x [rows,cols] dtype; q [rows,cols] i8; scale [rows, ceil(cols/128)] f32. Any alignment of
+ *   whole elements; 16-byte aligned x with whole 16-byte vectors per row takes the wide path.
+ */
+moe_status moe_ckpt_pack(int64_t rows, int32_t cols, moe_dtype dtype, const void* x, int8_t* q,
+                         float* scale, moe_stream_t stream);
+/* The values that a checkpoint holds, rounded to dtype. */
+moe_status moe_ckpt_unpack(int64_t rows, int32_t cols, moe_dtype dtype, const int8_t* q,
+                           const float* scale, void* x, moe_stream_t stream);
+
+/*
+ * SwiGLU's activation and backward from the checkpoint of h_gu = [G|U] (rows of 2F columns):
+ *   act = G*s*U, s = sigmoid(G);  dU = dact*G*s;  dG = dact*U*s*(1+G*(1-s))
+ *   q [rows,2F], scale [rows, ceil(2F/128)]; dact [rows,F] dtype; act [rows,F] dtype out;
+ *   dh [rows,2F] dtype out = [dG|dU]. act and dh may not overlap dact.
+ */
+moe_status moe_ckpt_swiglu_bwd(int64_t rows, int32_t d_ff, moe_dtype dtype, const int8_t* q,
+                               const float* scale, const void* dact, void* act, void* dh,
+                               moe_stream_t stream);
+
+/*
+ * moe_expert_ffn_bwd from an 8-bit checkpoint of h_gu: gu_q, gu_scale (moe_ckpt_pack on
+ * [TK,2F]) in the place of h_gu and act. act [TK,F] dtype out (made from the checkpoint) and
+ * dact [TK,F] dtype out (= dy_perm W2, rounded to dtype) are buffers of this pass; all else as
+ * there. The shared experts' activations (h_gu_sh, act_sh) are kept in dtype.
+ */
+moe_status moe_expert_ffn_bwd_ckpt(const moe_config* cfg, const void* x_perm,
+                                   const int32_t* offsets, const void* w1, const void* w2,
+                                   const int8_t* gu_q, const float* gu_scale, const void* dy_perm,
+                                   void* dact, void* act, void* dh, void* dx_perm, void* dw1,
+                                   void* dw2, const void* x, const void* dout, const void* ws1,
+                                   const void* ws2, const void* h_gu_sh, const void* act_sh,
+                                   void* dh_sh, void* dx_sh, void* dws1, void* dws2,
+                                   const int32_t* group_expert, moe_stream_t stream);
+
 /* Synchronises `stream`, returns the first error code any kernel recorded since the
  * last call (MOE_OK if none) in *code and clears it. */
 moe_status moe_device_status(moe_stream_t stream, int32_t* code /* HOST out */);

@@ -20,6 +20,8 @@ MOE_OK, MOE_ERR_INVALID_ARG, MOE_ERR_CUDA, MOE_ERR_DEVICE_CHECK, MOE_ERR_TIMEOUT
     MOE_ERR_UNSUPPORTED = range(6)
 MOE_F32, MOE_BF16 = 0, 1
 MOE_PAIRS_OFF, MOE_PAIRS_ALL, MOE_PAIRS_AUTO = 0, 1, 2
+MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
+CKPT_BLOCK = 128  # columns of a row that share a scale in an 8-bit checkpoint
 
 
 class MoEError(RuntimeError):
@@ -47,6 +49,19 @@ class moe_config(ctypes.Structure):
 assert ctypes.sizeof(moe_config) == 48
 
 
+class moe_gate_rule(ctypes.Structure):
+    _fields_ = [
+        ("score", ctypes.c_int32),
+        ("n_groups", ctypes.c_int32),
+        ("top_groups", ctypes.c_int32),
+        ("group_top", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+assert ctypes.sizeof(moe_gate_rule) == 20
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(
@@ -58,6 +73,8 @@ def _load():
 _lib = _load()
 P = ctypes.c_void_p
 _CFG = ctypes.POINTER(moe_config)
+_RULE = ctypes.POINTER(moe_gate_rule)
+_I64, _I32, _INT, _F32, _SIZE = ctypes.c_int64, ctypes.c_int32, ctypes.c_int, ctypes.c_float, ctypes.c_size_t
 
 # name -> argtypes (after the config pointer where present)
 _SIGS = {
@@ -81,6 +98,17 @@ _SIGS = {
     "moe_expert_ffn_bwd_kernels": [_CFG, ctypes.POINTER(ctypes.c_int32)],
     "moe_sgd_update": [P, P, P, ctypes.c_int64, ctypes.c_int64, P, ctypes.c_float, ctypes.c_int, P],
     "moe_gather_rows": [P, P, ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, ctypes.c_int, P, P],
+    "moe_gate": [_CFG, _RULE] + [P] * 8,
+    "moe_route_gate": [_CFG, _RULE] + [P] * 11,
+    "moe_gate_bwd": [_CFG, _RULE] + [P] * 12 + [_SIZE, P],
+    "moe_gate_balance": [_CFG, P, _F32, P, P, P],
+    "moe_layer_norm_fwd": [_I64, _I32, _INT] + [P] * 4 + [_F32] + [P] * 7,
+    "moe_layer_norm_workspace_size": [_I64, _I32, ctypes.POINTER(_SIZE)],
+    "moe_layer_norm_bwd": [_I64, _I32, _INT] + [P] * 12 + [_SIZE, P],
+    "moe_ckpt_pack": [_I64, _I32, _INT] + [P] * 4,
+    "moe_ckpt_unpack": [_I64, _I32, _INT] + [P] * 4,
+    "moe_ckpt_swiglu_bwd": [_I64, _I32, _INT] + [P] * 6,
+    "moe_expert_ffn_bwd_ckpt": [_CFG] + [P] * 25,
 }
 for _n, _a in _SIGS.items():
     f = getattr(_lib, _n)
@@ -104,10 +132,24 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_current_stream = None
+
+
+def _raw_stream_getter():
+    """The current torch stream's handle. The raw getter where torch has it (0.1 us a call against 3 to 5 through a
+    Stream object, of a launch's 3)."""
+    global _current_stream
+    import torch
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    _current_stream = lambda: raw(device())  # noqa: E731
+    return _current_stream()
+
+
 def _stream(s):
     if s is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream() if _current_stream is not None else _raw_stream_getter()
     if isinstance(s, int):
         return s
     return s.cuda_stream
@@ -251,3 +293,145 @@ def moe_route_bwd(cfg, x, w_router, probs, topk_idx, topk_w, dtopk_w, aux_coef, 
 
 def moe_dispatch_bwd(cfg, dx_perm, slot_of, dx_router, dx_sh, dx, stream=None):
     _call("moe_dispatch_bwd", cfg, dx_perm, slot_of, dx_router, dx_sh, dx, stream=stream)
+
+
+# ------------------------------------------------------------------ operators around the layer
+# These also check what a tensor is before its address is taken: on the GPU, dense, of the right
+# element type and as many elements as the call's sizes say.
+_TORCH_TYPES = {}
+
+
+def _types():
+    import torch
+    _TORCH_TYPES.update({MOE_F32: torch.float32, MOE_BF16: torch.bfloat16, "f32": torch.float32, "i32": torch.int32, "i8": torch.int8})
+    return _TORCH_TYPES
+
+
+def _arr(fn, name, t, kind, n):
+    """Address of a dense GPU tensor of n elements of `kind` (a moe_dtype, "f32", "i32" or "i8")."""
+    if t is None or type(t) is int:
+        return t
+    if t.numel() == n and t.is_cuda and t.is_contiguous() and t.dtype is (_TORCH_TYPES or _types())[kind]:
+        return t.data_ptr()
+    raise MoEError(MOE_ERR_INVALID_ARG, fn, f"{name}: expected a dense GPU tensor of {n} elements of {_types()[kind]}, got "
+                                            f"{tuple(t.shape)} {t.dtype}, strides {t.stride()}, on {t.device}")
+
+
+def _dtype_of(fn, dtype):
+    if dtype != MOE_F32 and dtype != MOE_BF16:
+        raise MoEError(MOE_ERR_INVALID_ARG, fn, f"unknown dtype {dtype}")
+    return int(dtype)
+
+
+def ckpt_blocks(cols: int) -> int:
+    """Scales per row of an 8-bit checkpoint of `cols` columns."""
+    return -(-cols // CKPT_BLOCK)
+
+
+def make_gate_rule(score=MOE_SCORE_SOFTMAX, n_groups=1, top_groups=1, group_top=1, scale=1.0) -> moe_gate_rule:
+    return moe_gate_rule(int(score), int(n_groups), int(top_groups), int(group_top), float(scale))
+
+
+def _gate_arrays(fn, cfg, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts):
+    T, E, k, Pn = cfg.T, cfg.n_experts, cfg.top_k, cfg.n_parties
+    return (_arr(fn, "logits", logits, "f32", T * E), _arr(fn, "balance_bias", balance_bias, "f32", Pn * E),
+            _arr(fn, "party_offsets", party_offsets, "i32", Pn + 1), _arr(fn, "scores", scores, "f32", T * E),
+            _arr(fn, "topk_idx", topk_idx, "i32", T * k), _arr(fn, "topk_w", topk_w, "f32", T * k),
+            _arr(fn, "counts", counts, "i32", Pn * E))
+
+
+def moe_gate(cfg, rule, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts, stream=None):
+    a = _gate_arrays("moe_gate", cfg, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts)
+    _check(_lib.moe_gate(cfg, rule, *a, _stream(stream)), "moe_gate")
+
+
+def moe_route_gate(cfg, rule, x, w_router, router_bias, balance_bias, party_offsets, logits, scores, topk_idx, topk_w, counts,
+                   stream=None):
+    fn = "moe_route_gate"
+    T, E, d, Pn = cfg.T, cfg.n_experts, cfg.d_model, cfg.n_parties
+    logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts = _gate_arrays(
+        fn, cfg, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts)
+    dt = _dtype_of(fn, cfg.dtype)
+    _check(_lib.moe_route_gate(cfg, rule, _arr(fn, "x", x, dt, T * d), _arr(fn, "w_router", w_router, dt, Pn * E * d),
+                               _arr(fn, "router_bias", router_bias, "f32", Pn * E), balance_bias, party_offsets, logits, scores,
+                               topk_idx, topk_w, counts, _stream(stream)), fn)
+
+
+def moe_gate_bwd(cfg, rule, logits, topk_idx, dtopk_w, aux_coef, party_offsets, dlogits, x=None, w_router=None, dw_router=None,
+                 dbias=None, dx_router=None, workspace=None, workspace_bytes=0, stream=None):
+    fn = "moe_gate_bwd"
+    T, E, d, k, Pn = cfg.T, cfg.n_experts, cfg.d_model, cfg.top_k, cfg.n_parties
+    dt = _dtype_of(fn, cfg.dtype)
+    _check(_lib.moe_gate_bwd(cfg, rule, _arr(fn, "logits", logits, "f32", T * E), _arr(fn, "topk_idx", topk_idx, "i32", T * k),
+                             _arr(fn, "dtopk_w", dtopk_w, "f32", T * k), _arr(fn, "aux_coef", aux_coef, "f32", Pn * E),
+                             _arr(fn, "party_offsets", party_offsets, "i32", Pn + 1), _arr(fn, "dlogits", dlogits, "f32", T * E),
+                             _arr(fn, "x", x, dt, T * d), _arr(fn, "w_router", w_router, dt, Pn * E * d),
+                             _arr(fn, "dw_router", dw_router, dt, Pn * E * d), _arr(fn, "dbias", dbias, "f32", Pn * E),
+                             _arr(fn, "dx_router", dx_router, dt, T * d), _ptr(workspace), int(workspace_bytes),
+                             _stream(stream)), fn)
+
+
+def moe_gate_balance(cfg, counts, rate, bias_in, bias_out, stream=None):
+    fn, n = "moe_gate_balance", cfg.n_parties * cfg.n_experts
+    _check(_lib.moe_gate_balance(cfg, _arr(fn, "counts", counts, "i32", n), rate, _arr(fn, "bias_in", bias_in, "f32", n),
+                                 _arr(fn, "bias_out", bias_out, "f32", n), _stream(stream)), fn)
+
+
+def moe_layer_norm_workspace_size(rows, d) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.moe_layer_norm_workspace_size(int(rows), int(d), ctypes.byref(n)), "moe_layer_norm_workspace_size")
+    return n.value
+
+
+def moe_layer_norm_fwd(rows, d, dtype, x, residual, gamma, beta, eps, h, y, mean=None, rstd=None, h_q=None, h_scale=None,
+                       stream=None):
+    fn, n = "moe_layer_norm_fwd", rows * d
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_layer_norm_fwd(rows, d, dt, _arr(fn, "x", x, dt, n), _arr(fn, "residual", residual, dt, n),
+                                   _arr(fn, "gamma", gamma, "f32", d), _arr(fn, "beta", beta, "f32", d), eps,
+                                   _arr(fn, "h", h, dt, n), _arr(fn, "y", y, dt, n), _arr(fn, "mean", mean, "f32", rows),
+                                   _arr(fn, "rstd", rstd, "f32", rows), _arr(fn, "h_q", h_q, "i8", n),
+                                   _arr(fn, "h_scale", h_scale, "f32", rows * ckpt_blocks(d)), _stream(stream)), fn)
+
+
+def moe_layer_norm_bwd(rows, d, dtype, dy, h, h_q, h_scale, mean, rstd, gamma, dh, dx, dgamma, dbeta, workspace,
+                       workspace_bytes, stream=None):
+    fn, n = "moe_layer_norm_bwd", rows * d
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_layer_norm_bwd(rows, d, dt, _arr(fn, "dy", dy, dt, n), _arr(fn, "h", h, dt, n), _arr(fn, "h_q", h_q, "i8", n),
+                                   _arr(fn, "h_scale", h_scale, "f32", rows * ckpt_blocks(d)), _arr(fn, "mean", mean, "f32", rows),
+                                   _arr(fn, "rstd", rstd, "f32", rows), _arr(fn, "gamma", gamma, "f32", d),
+                                   _arr(fn, "dh", dh, dt, n), _arr(fn, "dx", dx, dt, n), _arr(fn, "dgamma", dgamma, "f32", d),
+                                   _arr(fn, "dbeta", dbeta, "f32", d), _ptr(workspace), int(workspace_bytes),
+                                   _stream(stream)), fn)
+
+
+def moe_ckpt_pack(rows, cols, dtype, x, q, scale, stream=None):
+    fn, n = "moe_ckpt_pack", rows * cols
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_ckpt_pack(rows, cols, dt, _arr(fn, "x", x, dt, n), _arr(fn, "q", q, "i8", n),
+                              _arr(fn, "scale", scale, "f32", rows * ckpt_blocks(cols)), _stream(stream)), fn)
+
+
+def moe_ckpt_unpack(rows, cols, dtype, q, scale, x, stream=None):
+    fn, n = "moe_ckpt_unpack", rows * cols
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_ckpt_unpack(rows, cols, dt, _arr(fn, "q", q, "i8", n),
+                                _arr(fn, "scale", scale, "f32", rows * ckpt_blocks(cols)), _arr(fn, "x", x, dt, n),
+                                _stream(stream)), fn)
+
+
+def moe_ckpt_swiglu_bwd(rows, d_ff, dtype, q, scale, dact, act, dh, stream=None):
+    fn, n = "moe_ckpt_swiglu_bwd", rows * d_ff
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_ckpt_swiglu_bwd(rows, d_ff, dt, _arr(fn, "q", q, "i8", 2 * n),
+                                    _arr(fn, "scale", scale, "f32", rows * ckpt_blocks(2 * d_ff)),
+                                    _arr(fn, "dact", dact, dt, n), _arr(fn, "act", act, dt, n), _arr(fn, "dh", dh, dt, 2 * n),
+                                    _stream(stream)), fn)
+
+
+def moe_expert_ffn_bwd_ckpt(cfg, x_perm, offsets, w1, w2, gu_q, gu_scale, dy_perm, dact, act, dh, dx_perm, dw1, dw2, x=None,
+                            dout=None, ws1=None, ws2=None, h_gu_sh=None, act_sh=None, dh_sh=None, dx_sh=None, dws1=None,
+                            dws2=None, group_expert=None, stream=None):
+    _call("moe_expert_ffn_bwd_ckpt", cfg, x_perm, offsets, w1, w2, gu_q, gu_scale, dy_perm, dact, act, dh, dx_perm, dw1, dw2, x,
+          dout, ws1, ws2, h_gu_sh, act_sh, dh_sh, dx_sh, dws1, dws2, group_expert, stream=stream)

@@ -17,8 +17,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe.so")
-SOURCES = ["route.cu", "dispatch.cu", "gemm_f32.cu", "gemm_tc.cu", "train.cu", "moe_abi.cu"]
-HEADERS = ["device_state.h", "moe_common.cuh", "moe_internal.h", "tc_ptx.cuh"]
+SOURCES = ["route.cu", "dispatch.cu", "gemm_f32.cu", "gemm_tc.cu", "train.cu", "norm.cu", "gate.cu",
+           "ckpt.cu", "moe_abi.cu"]
+HEADERS = ["device_state.h", "moe_common.cuh", "moe_internal.h", "span.cuh", "tc_ptx.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
          "--expt-relaxed-constexpr", "-I" + os.path.join(ROOT, "include")]

@@ -166,6 +166,56 @@ BwdGemms bwd_gemms(const moe_config* cfg, const int32_t* offsets, const int32_t*
     return g;
 }
 
+// The shared experts' backward GEMMs: the shapes of the routed ones `g`, one group per expert.
+moe_status shared_bwd(const moe_config* cfg, const BwdGemms& g, const void* x, const void* dout, const void* ws1, const void* ws2,
+                      const void* h_gu_sh, const void* act_sh, void* dh_sh, void* dx_sh, void* dws1, void* dws2,
+                      cudaStream_t s) {
+    const bool bf16 = cfg->dtype == MOE_BF16;
+    const int64_t T = cfg->T;
+    const int d = cfg->d_model, S = cfg->n_shared, Fs = cfg->d_ff_shared;
+    moe_status st;
+    GemmMArgs sa = g.a;
+    sa.group_expert = nullptr;  // shared experts: one group per expert
+    sa.G = S;
+    sa.rows = GroupRows{nullptr, (int)T, 0, 0, T};
+    sa.a = dout;
+    sa.b = ws2;
+    sa.b_group_elems = (int64_t)d * Fs;
+    sa.N = Fs;
+    sa.aux = h_gu_sh;
+    sa.out0 = dh_sh;
+    if ((st = cuda_status(launch_gemm_m(sa, bf16, s), "shared dA gemm"))) return st;
+    GemmMArgs sb = g.x;
+    sb.group_expert = nullptr;  // shared experts: one group per expert
+    sb.G = S;
+    sb.rows = GroupRows{nullptr, (int)T, T, 0, T};
+    sb.a = dh_sh;
+    sb.b = ws1;
+    sb.b_group_elems = (int64_t)2 * Fs * d;
+    sb.K = 2 * Fs;
+    sb.out0 = dx_sh;
+    if ((st = cuda_status(launch_gemm_m(sb, bf16, s), "shared dX gemm"))) return st;
+    GemmKArgs sw2 = g.w2;
+    sw2.group_expert = nullptr;  // shared experts: one group per expert
+    sw2.G = S;
+    sw2.rows = GroupRows{nullptr, (int)T, 0, T, 0};
+    sw2.a = dout;
+    sw2.b = act_sh;
+    sw2.N = Fs;
+    sw2.out = dws2;
+    if ((st = cuda_status(launch_gemm_k(sw2, bf16, s), "shared dW2 gemm"))) return st;
+    GemmKArgs sw1 = g.w1;
+    sw1.group_expert = nullptr;  // shared experts: one group per expert
+    sw1.G = S;
+    sw1.rows = GroupRows{nullptr, (int)T, T, 0, 0};
+    sw1.a = dh_sh;
+    sw1.b = x;
+    sw1.M = 2 * Fs;
+    sw1.out = dws1;
+    if ((st = cuda_status(launch_gemm_k(sw1, bf16, s), "shared dW1 gemm"))) return st;
+    return MOE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -576,47 +626,7 @@ moe_status moe_expert_ffn_bwd(const moe_config* cfg, const void* x_perm, const i
         if ((st = cuda_status(cudaStreamWaitEvent(s, ss->join, 0), "join"))) return st;
         side_lock.unlock();
     }
-    if (S) {
-        GemmMArgs sa = a;
-        sa.group_expert = nullptr;  // shared experts: one group per expert
-        sa.G = S;
-        sa.rows = GroupRows{nullptr, (int)T, 0, 0, T};
-        sa.a = dout;
-        sa.b = ws2;
-        sa.b_group_elems = (int64_t)d * Fs;
-        sa.N = Fs;
-        sa.aux = h_gu_sh;
-        sa.out0 = dh_sh;
-        if ((st = cuda_status(launch_gemm_m(sa, bf16, s), "shared dA gemm"))) return st;
-        GemmMArgs sb = b;
-        sb.group_expert = nullptr;  // shared experts: one group per expert
-        sb.G = S;
-        sb.rows = GroupRows{nullptr, (int)T, T, 0, T};
-        sb.a = dh_sh;
-        sb.b = ws1;
-        sb.b_group_elems = (int64_t)2 * Fs * d;
-        sb.K = 2 * Fs;
-        sb.out0 = dx_sh;
-        if ((st = cuda_status(launch_gemm_m(sb, bf16, s), "shared dX gemm"))) return st;
-        GemmKArgs sw2 = w2g;
-        sw2.group_expert = nullptr;  // shared experts: one group per expert
-        sw2.G = S;
-        sw2.rows = GroupRows{nullptr, (int)T, 0, T, 0};
-        sw2.a = dout;
-        sw2.b = act_sh;
-        sw2.N = Fs;
-        sw2.out = dws2;
-        if ((st = cuda_status(launch_gemm_k(sw2, bf16, s), "shared dW2 gemm"))) return st;
-        GemmKArgs sw1 = w1g;
-        sw1.group_expert = nullptr;  // shared experts: one group per expert
-        sw1.G = S;
-        sw1.rows = GroupRows{nullptr, (int)T, T, 0, 0};
-        sw1.a = dh_sh;
-        sw1.b = x;
-        sw1.M = 2 * Fs;
-        sw1.out = dws1;
-        if ((st = cuda_status(launch_gemm_k(sw1, bf16, s), "shared dW1 gemm"))) return st;
-    }
+    if (S) return shared_bwd(cfg, g, x, dout, ws1, ws2, h_gu_sh, act_sh, dh_sh, dx_sh, dws1, dws2, s);
     return MOE_OK;
 }
 
@@ -750,17 +760,362 @@ moe_status moe_sgd_update(void* w, const void* dw, float* w_master, int64_t n_gr
                        "moe_sgd_update");
 }
 
+// ---------------------------------------------------------------- layer norm
+static moe_status check_rows(int64_t rows, int32_t cols, moe_dtype dtype) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (rows < 0 || rows >= (int64_t)1 << 31) return fail(MOE_ERR_INVALID_ARG, "rows=%lld outside [0, 2^31)", (long long)rows);
+    if (cols < 1) return fail(MOE_ERR_INVALID_ARG, "width %d < 1", cols);
+    return MOE_OK;
+}
+static moe_status check_norm(int64_t rows, int32_t d, moe_dtype dtype) {
+    if (d > kNormMaxWidth)
+        return fail(MOE_ERR_UNSUPPORTED, "d=%d > %d, the widest row this build normalises", d, kNormMaxWidth);
+    return check_rows(rows, d, dtype);
+}
+// pointers to elements of more than one byte
+static bool aligned_elem(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+#define REQUIRE_ELEM(ptr, bytes)                                                                                \
+    do {                                                                                                        \
+        if (!(ptr)) return fail(MOE_ERR_INVALID_ARG, "%s is NULL", #ptr);                                       \
+        if (!aligned_elem(ptr, bytes)) return fail(MOE_ERR_INVALID_ARG, "%s is not aligned to its elements", #ptr); \
+    } while (0)
+#define OPTIONAL_ELEM(ptr, bytes)                                                                               \
+    do {                                                                                                        \
+        if (!aligned_elem(ptr, bytes)) return fail(MOE_ERR_INVALID_ARG, "%s is not aligned to its elements", #ptr); \
+    } while (0)
+
+moe_status moe_layer_norm_workspace_size(int64_t rows, int32_t d, size_t* bytes) {
+    moe_status st = check_norm(rows, d, MOE_F32);
+    if (st) return st;
+    REQUIRE(bytes);
+    *bytes = norm_workspace_bytes(rows, d);
+    return MOE_OK;
+}
+
+moe_status moe_layer_norm_fwd(int64_t rows, int32_t d, moe_dtype dtype, const void* x, const void* residual, const float* gamma,
+                              const float* beta, float eps, void* h, void* y, float* mean, float* rstd, int8_t* h_q,
+                              float* h_scale, moe_stream_t stream) {
+    moe_status st = check_norm(rows, d, dtype);
+    if (st) return st;
+    if (!(eps >= 0.f) || eps - eps != 0.f) return fail(MOE_ERR_INVALID_ARG, "eps is negative or not finite");
+    if (rows == 0) return MOE_OK;
+    const size_t es = dtype == MOE_BF16 ? 2 : 4;
+    REQUIRE_ELEM(x, es);
+    OPTIONAL_ELEM(residual, es);
+    REQUIRE_ELEM(gamma, 4);
+    OPTIONAL_ELEM(beta, 4);
+    if (residual) REQUIRE_ELEM(h, es);
+    if (!residual && h) return fail(MOE_ERR_INVALID_ARG, "h without a residual is x: pass NULL");
+    REQUIRE_ELEM(y, es);
+    if (!mean != !rstd) return fail(MOE_ERR_INVALID_ARG, "mean and rstd come together");
+    OPTIONAL_ELEM(mean, 4);
+    OPTIONAL_ELEM(rstd, 4);
+    if (!h_q != !h_scale) return fail(MOE_ERR_INVALID_ARG, "h_q and h_scale come together");
+    OPTIONAL_ELEM(h_scale, 4);
+    return cuda_status(launch_norm_fwd(rows, d, dtype == MOE_BF16, x, residual, gamma, beta, eps, h, y, mean, rstd, h_q, h_scale,
+                                       (cudaStream_t)stream),
+                       "moe_layer_norm_fwd");
+}
+
+moe_status moe_layer_norm_bwd(int64_t rows, int32_t d, moe_dtype dtype, const void* dy, const void* h, const int8_t* h_q,
+                              const float* h_scale, const float* mean, const float* rstd, const float* gamma, const void* dh,
+                              void* dx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes,
+                              moe_stream_t stream) {
+    moe_status st = check_norm(rows, d, dtype);
+    if (st) return st;
+    const size_t es = dtype == MOE_BF16 ? 2 : 4;
+    REQUIRE_ELEM(dgamma, 4);
+    OPTIONAL_ELEM(dbeta, 4);
+    if (rows > 0) {
+        REQUIRE_ELEM(dy, es);
+        if (!h == !h_q) return fail(MOE_ERR_INVALID_ARG, "one of h and h_q, and not both, holds the states");
+        if (!h_q != !h_scale) return fail(MOE_ERR_INVALID_ARG, "h_q and h_scale come together");
+        OPTIONAL_ELEM(h, es);
+        OPTIONAL_ELEM(h_scale, 4);
+        REQUIRE_ELEM(mean, 4);
+        REQUIRE_ELEM(rstd, 4);
+        REQUIRE_ELEM(gamma, 4);
+        OPTIONAL_ELEM(dh, es);
+        REQUIRE_ELEM(dx, es);
+        REQUIRE_ELEM(workspace, 4);
+        const size_t need = norm_workspace_bytes(rows, d);
+        if (workspace_bytes < need)
+            return fail(MOE_ERR_INVALID_ARG, "workspace of %zu bytes < %zu needed", workspace_bytes, need);
+    }
+    return cuda_status(launch_norm_bwd(rows, d, dtype == MOE_BF16, dy, h, h_q, h_scale, mean, rstd, gamma, dh, dx, dgamma, dbeta,
+                                       workspace, (cudaStream_t)stream),
+                       "moe_layer_norm_bwd");
+}
+
+// ---------------------------------------------------------------- gating rules
+static moe_status check_rule(const moe_config* c, const moe_gate_rule* r) {
+    if (!r) return fail(MOE_ERR_INVALID_ARG, "rule is NULL");
+    if (r->score != MOE_SCORE_SOFTMAX && r->score != MOE_SCORE_SIGMOID)
+        return fail(MOE_ERR_INVALID_ARG, "score %d is not MOE_SCORE_SOFTMAX or MOE_SCORE_SIGMOID", r->score);
+    if (r->n_groups < 1 || r->n_groups > 32 || c->n_experts % r->n_groups)
+        return fail(MOE_ERR_INVALID_ARG, "n_groups=%d: 1 to 32 groups, a divisor of n_experts=%d", r->n_groups, c->n_experts);
+    const int size = c->n_experts / r->n_groups;
+    if (r->top_groups < 1 || r->top_groups > r->n_groups)
+        return fail(MOE_ERR_INVALID_ARG, "top_groups=%d outside [1, n_groups]", r->top_groups);
+    if (r->top_groups * size < c->top_k)
+        return fail(MOE_ERR_INVALID_ARG, "top_groups=%d groups of %d experts hold fewer than top_k=%d", r->top_groups, size, c->top_k);
+    if (r->group_top < 1 || r->group_top > 2 || r->group_top > size)
+        return fail(MOE_ERR_INVALID_ARG, "group_top=%d: 1 or 2, at most the %d experts of a group", r->group_top, size);
+    if (r->scale - r->scale != 0.f) return fail(MOE_ERR_INVALID_ARG, "scale is not finite");
+    return MOE_OK;
+}
+
+static moe_status gate_common(const moe_config* cfg, const moe_gate_rule* rule, const float* logits, const float* balance_bias,
+                              const int32_t* po, float* scores, int32_t* topk_idx, float* topk_w, int32_t* counts, cudaStream_t s) {
+    GateArgs a{};
+    a.logits = logits;
+    a.bias = balance_bias;
+    a.po = cfg->n_parties > 1 ? po : nullptr;
+    a.P = cfg->n_parties;
+    a.T = cfg->T;
+    a.E = cfg->n_experts;
+    a.k = cfg->top_k;
+    a.normalize = cfg->normalize_topk;
+    a.sigmoid = rule->score == MOE_SCORE_SIGMOID;
+    a.groups = rule->n_groups;
+    a.top_groups = rule->top_groups;
+    a.group_top = rule->group_top;
+    a.scale = rule->scale;
+    a.scores = scores;
+    a.topk_idx = topk_idx;
+    a.topk_w = topk_w;
+    a.counts = counts;
+    return cuda_status(launch_gate(a, s), "moe_gate");
+}
+
+moe_status moe_gate(const moe_config* cfg, const moe_gate_rule* rule, const float* logits, const float* balance_bias,
+                    const int32_t* party_offsets, float* scores, int32_t* topk_idx, float* topk_w, int32_t* counts,
+                    moe_stream_t stream) {
+    moe_status st = check_cfg(cfg);
+    if (st) return st;
+    if ((st = check_rule(cfg, rule))) return st;
+    if ((st = check_parties(cfg, party_offsets))) return st;
+    REQUIRE_ELEM(counts, 4);
+    if (cfg->T > 0) {
+        REQUIRE_ELEM(logits, 4);
+        OPTIONAL_ELEM(balance_bias, 4);
+        OPTIONAL_ELEM(scores, 4);
+        REQUIRE_ELEM(topk_idx, 4);
+        REQUIRE_ELEM(topk_w, 4);
+    }
+    return gate_common(cfg, rule, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts, (cudaStream_t)stream);
+}
+
+moe_status moe_route_gate(const moe_config* cfg, const moe_gate_rule* rule, const void* x, const void* w_router,
+                          const float* router_bias, const float* balance_bias, const int32_t* party_offsets, float* logits,
+                          float* scores, int32_t* topk_idx, float* topk_w, int32_t* counts, moe_stream_t stream) {
+    moe_status st = check_cfg(cfg);
+    if (st) return st;
+    if ((st = check_rule(cfg, rule))) return st;
+    // the logits of moe_route; its picks and probabilities are overwritten
+    st = moe_route(cfg, x, w_router, router_bias, party_offsets, logits, scores, topk_idx, topk_w, counts, stream);
+    if (st || cfg->T == 0) return st;
+    OPTIONAL_ELEM(balance_bias, 4);
+    return gate_common(cfg, rule, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts, (cudaStream_t)stream);
+}
+
+moe_status moe_gate_bwd(const moe_config* cfg, const moe_gate_rule* rule, const float* logits, const int32_t* topk_idx,
+                        const float* dtopk_w, const float* aux_coef, const int32_t* party_offsets, float* dlogits,
+                        const void* x, const void* w_router, void* dw_router, float* dbias, void* dx_router, void* workspace,
+                        size_t workspace_bytes, moe_stream_t stream) {
+    moe_status st = check_cfg(cfg);
+    if (st) return st;
+    if ((st = check_rule(cfg, rule))) return st;
+    if ((st = check_parties(cfg, party_offsets))) return st;
+    if (!dw_router && (dbias || dx_router))
+        return fail(MOE_ERR_INVALID_ARG, "dbias and dx_router come with dw_router");
+    if (cfg->T > 0) {
+        REQUIRE_ELEM(logits, 4);
+        REQUIRE_ELEM(topk_idx, 4);
+        REQUIRE_ELEM(dtopk_w, 4);
+        OPTIONAL_ELEM(aux_coef, 4);
+        REQUIRE_ELEM(dlogits, 4);
+    }
+    GateBwdArgs g{};
+    g.logits = logits;
+    g.topk_idx = topk_idx;
+    g.dtopk_w = dtopk_w;
+    g.aux_coef = aux_coef;
+    g.po = cfg->n_parties > 1 ? party_offsets : nullptr;
+    g.P = cfg->n_parties;
+    g.T = cfg->T;
+    g.E = cfg->n_experts;
+    g.k = cfg->top_k;
+    g.normalize = cfg->normalize_topk;
+    g.sigmoid = rule->score == MOE_SCORE_SIGMOID;
+    g.scale = rule->scale;
+    g.dlogits = dlogits;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (!dw_router)
+        return cfg->T == 0 ? MOE_OK : cuda_status(launch_gate_bwd(g, nullptr, 0, nullptr, 0, 0, s), "moe_gate_bwd");
+    REQUIRE_VEC(dw_router);
+    if (cfg->T > 0) REQUIRE_VEC(x);
+    if (dx_router && cfg->T > 0) {
+        REQUIRE_VEC(dx_router);
+        REQUIRE_VEC(w_router);
+    }
+    REQUIRE(workspace);
+    const size_t need = route_bwd_workspace(cfg->T, cfg->n_parties, cfg->n_experts, cfg->d_model);
+    if (workspace_bytes < need)
+        return fail(MOE_ERR_INVALID_ARG, "workspace of %zu bytes < %zu needed", workspace_bytes, need);
+    RouteBwdArgs a{};
+    a.x = x;
+    a.topk_idx = topk_idx;
+    a.dtopk_w = dtopk_w;
+    a.aux_coef = aux_coef;
+    a.po = party_offsets;
+    a.P = cfg->n_parties;
+    a.T = cfg->T;
+    a.d = cfg->d_model;
+    a.E = cfg->n_experts;
+    a.k = cfg->top_k;
+    a.normalize = cfg->normalize_topk;
+    a.dlogits = dlogits;
+    a.dw_router = dw_router;
+    a.dbias = dbias;
+    a.w_router = w_router;
+    a.dx_router = dx_router;
+    a.gate = &g;
+    return cuda_status(launch_route_bwd(a, cfg->dtype == MOE_BF16, workspace, s), "moe_gate_bwd");
+}
+
+moe_status moe_gate_balance(const moe_config* cfg, const int32_t* counts, float rate, const float* bias_in, float* bias_out,
+                            moe_stream_t stream) {
+    moe_status st = check_cfg(cfg);
+    if (st) return st;
+    if (rate - rate != 0.f) return fail(MOE_ERR_INVALID_ARG, "rate is not finite");
+    REQUIRE_ELEM(counts, 4);
+    REQUIRE_ELEM(bias_in, 4);
+    REQUIRE_ELEM(bias_out, 4);
+    return cuda_status(launch_gate_balance(counts, cfg->n_parties, cfg->n_experts, rate, bias_in, bias_out, (cudaStream_t)stream),
+                       "moe_gate_balance");
+}
+
+// ---------------------------------------------------------------- 8-bit activation checkpoints
+moe_status moe_ckpt_pack(int64_t rows, int32_t cols, moe_dtype dtype, const void* x, int8_t* q, float* scale, moe_stream_t stream) {
+    moe_status st = check_rows(rows, cols, dtype);
+    if (st) return st;
+    if (rows == 0) return MOE_OK;
+    REQUIRE_ELEM(x, dtype == MOE_BF16 ? 2 : 4);
+    REQUIRE(q);
+    REQUIRE_ELEM(scale, 4);
+    return cuda_status(launch_ckpt_pack(x, rows, cols, dtype == MOE_BF16, q, scale, (cudaStream_t)stream), "moe_ckpt_pack");
+}
+
+moe_status moe_ckpt_unpack(int64_t rows, int32_t cols, moe_dtype dtype, const int8_t* q, const float* scale, void* x,
+                           moe_stream_t stream) {
+    moe_status st = check_rows(rows, cols, dtype);
+    if (st) return st;
+    if (rows == 0) return MOE_OK;
+    REQUIRE(q);
+    REQUIRE_ELEM(scale, 4);
+    REQUIRE_ELEM(x, dtype == MOE_BF16 ? 2 : 4);
+    return cuda_status(launch_ckpt_unpack(q, scale, rows, cols, dtype == MOE_BF16, x, (cudaStream_t)stream), "moe_ckpt_unpack");
+}
+
+moe_status moe_ckpt_swiglu_bwd(int64_t rows, int32_t d_ff, moe_dtype dtype, const int8_t* q, const float* scale, const void* dact,
+                               void* act, void* dh, moe_stream_t stream) {
+    moe_status st = check_rows(rows, d_ff, dtype);
+    if (st) return st;
+    if (d_ff >= 1 << 30) return fail(MOE_ERR_INVALID_ARG, "d_ff=%d >= 2^30", d_ff);
+    if (rows == 0) return MOE_OK;
+    const size_t es = dtype == MOE_BF16 ? 2 : 4;
+    REQUIRE(q);
+    REQUIRE_ELEM(scale, 4);
+    REQUIRE_ELEM(dact, es);
+    REQUIRE_ELEM(act, es);
+    REQUIRE_ELEM(dh, es);
+    return cuda_status(launch_ckpt_swiglu_bwd(q, scale, dact, rows, d_ff, dtype == MOE_BF16, act, dh, (cudaStream_t)stream),
+                       "moe_ckpt_swiglu_bwd");
+}
+
+moe_status moe_expert_ffn_bwd_ckpt(const moe_config* cfg, const void* x_perm, const int32_t* offsets, const void* w1,
+                                   const void* w2, const int8_t* gu_q, const float* gu_scale, const void* dy_perm, void* dact,
+                                   void* act, void* dh, void* dx_perm, void* dw1, void* dw2, const void* x, const void* dout,
+                                   const void* ws1, const void* ws2, const void* h_gu_sh, const void* act_sh, void* dh_sh,
+                                   void* dx_sh, void* dws1, void* dws2, const int32_t* group_expert, moe_stream_t stream) {
+    moe_status st = check_cfg(cfg);
+    if (st) return st;
+    if (cfg->T == 0)  // no rows: all weight gradients are zero
+        return moe_expert_ffn_bwd(cfg, x_perm, offsets, w1, w2, nullptr, act, dy_perm, dh, dx_perm, dw1, dw2, x, dout, ws1, ws2,
+                                  h_gu_sh, act_sh, dh_sh, dx_sh, dws1, dws2, group_expert, stream);
+    const bool bf16 = cfg->dtype == MOE_BF16;
+    REQUIRE_VEC(x_perm);
+    REQUIRE(offsets);
+    REQUIRE_VEC(w1);
+    REQUIRE_VEC(w2);
+    REQUIRE_VEC(gu_q);
+    REQUIRE_ELEM(gu_scale, 4);
+    REQUIRE_VEC(dy_perm);
+    REQUIRE_VEC(dact);
+    REQUIRE_VEC(act);
+    REQUIRE_VEC(dh);
+    REQUIRE_VEC(dx_perm);
+    REQUIRE_VEC(dw1);
+    REQUIRE_VEC(dw2);
+    if (cfg->n_shared) {
+        REQUIRE_VEC(x);
+        REQUIRE_VEC(dout);
+        REQUIRE_VEC(ws1);
+        REQUIRE_VEC(ws2);
+        REQUIRE_VEC(h_gu_sh);
+        REQUIRE_VEC(act_sh);
+        REQUIRE_VEC(dh_sh);
+        REQUIRE_VEC(dx_sh);
+        REQUIRE_VEC(dws1);
+        REQUIRE_VEC(dws2);
+    }
+    cudaStream_t s = (cudaStream_t)stream;
+    const BwdGemms g = bwd_gemms(cfg, offsets, group_expert);
+    // dA = dY W2, stored in dtype: the SwiGLU backward that reads the checkpoint is a pass of its own,
+    // which also makes A anew, so that nothing of [G|U] or A is kept in 16 or 32 bits
+    GemmMArgs a = g.a, b = g.x;
+    GemmKArgs w2g = g.w2, w1g = g.w1;
+    a.a = dy_perm;
+    a.b = w2;
+    a.epi = EPI_STORE;
+    a.out0 = dact;
+    b.a = dh;
+    b.b = w1;
+    b.out0 = dx_perm;
+    w2g.a = dy_perm;
+    w2g.b = act;
+    w2g.out = dw2;
+    w1g.a = dh;
+    w1g.b = x_perm;
+    w1g.out = dw1;
+    if ((st = cuda_status(launch_gemm_m(a, bf16, s), "expert dA gemm"))) return st;
+    if ((st = cuda_status(launch_ckpt_swiglu_bwd(gu_q, gu_scale, dact, cfg->T * cfg->top_k, cfg->d_ff, bf16, act, dh, s),
+                          "expert SwiGLU backward")))
+        return st;
+    if ((st = cuda_status(launch_gemm_k(w2g, bf16, s), "expert dW2 gemm"))) return st;
+    if (g.with_x) {
+        if ((st = cuda_status(launch_gemm_mk(b, w1g, s), "expert dX+dW1 gemm"))) return st;
+    } else {
+        if ((st = cuda_status(launch_gemm_m(b, bf16, s), "expert dX gemm"))) return st;
+        if ((st = cuda_status(launch_gemm_k(w1g, bf16, s), "expert dW1 gemm"))) return st;
+    }
+    if (cfg->n_shared) return shared_bwd(cfg, g, x, dout, ws1, ws2, h_gu_sh, act_sh, dh_sh, dx_sh, dws1, dws2, s);
+    return MOE_OK;
+}
+
 moe_status moe_device_status(moe_stream_t stream, int32_t* code) {
     REQUIRE(code);
     cudaStream_t s = (cudaStream_t)stream;
-    int c[4] = {0, 0, 0, 0};
+    int c[5] = {0, 0, 0, 0, 0};
     cudaError_t e;
     if ((e = route_status(s, &c[0])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = dispatch_status(s, &c[1])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = gemm_status(s, &c[2])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = f32_status(s, &c[3])) != cudaSuccess) return cuda_status(e, "status");
+    if ((e = gate_status(s, &c[4])) != cudaSuccess) return cuda_status(e, "status");
     *code = 0;
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 5; ++i)
         if (c[i] && !*code) *code = c[i];
     return MOE_OK;
 }

@@ -1,6 +1,7 @@
 // Launchers shared between the kernel translation units and the C ABI (host side).
 #pragma once
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -39,7 +40,56 @@ struct RouteBwdArgs {
     float* dbias;
     const void* w_router;  // [P,E,d]
     void* dx_router;       // [T,d] or null
+    const struct GateBwdArgs* gate = nullptr;  // dlogits by this rule instead of from probs
 };
+
+// gating rules (gate.cu)
+struct GateArgs {
+    const float* logits;  // [T,E]
+    const float* bias;    // [P,E] or null
+    const int32_t* po;
+    int P;
+    int64_t T;
+    int E, k, normalize, sigmoid, groups, top_groups, group_top;
+    float scale;
+    float* scores;  // [T,E] or null
+    int32_t* topk_idx;
+    float* topk_w;
+    int32_t* counts;  // [P,E]
+    bool vec;         // set by the launcher: 16-byte loads
+};
+struct GateBwdArgs {
+    const float* logits;
+    const int32_t* topk_idx;
+    const float* dtopk_w;
+    const float* aux_coef;  // [P,E] or null
+    const int32_t* po;
+    int P;
+    int64_t T;
+    int E, k, normalize, sigmoid;
+    float scale;
+    float* dlogits;
+};
+cudaError_t launch_gate(const GateArgs& a, cudaStream_t s);
+// dz16, chunk_off: as the router backward's own dlogits pass writes them (null: not wanted)
+cudaError_t launch_gate_bwd(const GateBwdArgs& a, __nv_bfloat16* dz16, int EP, int32_t* chunk_off, int CH, int nchunk, cudaStream_t s);
+cudaError_t launch_gate_balance(const int32_t* counts, int P, int E, float rate, const float* in, float* out, cudaStream_t s);
+cudaError_t gate_status(cudaStream_t s, int* code);
+
+// layer norm (norm.cu)
+constexpr int kNormMaxWidth = 16384;  // a row is held in the registers of one CTA
+size_t norm_workspace_bytes(int64_t rows, int d);
+cudaError_t launch_norm_fwd(int64_t rows, int d, bool bf16, const void* x, const void* res, const float* gamma, const float* beta,
+                            float eps, void* h, void* y, float* mean, float* rstd, int8_t* q, float* q_scale, cudaStream_t s);
+cudaError_t launch_norm_bwd(int64_t rows, int d, bool bf16, const void* dy, const void* h, const int8_t* q, const float* q_scale,
+                            const float* mean, const float* rstd, const float* gamma, const void* dh, void* dx, float* dgamma,
+                            float* dbeta, void* ws, cudaStream_t s);
+
+// 8-bit activation checkpoints (ckpt.cu)
+cudaError_t launch_ckpt_pack(const void* x, int64_t rows, int cols, bool bf16, int8_t* q, float* scale, cudaStream_t s);
+cudaError_t launch_ckpt_unpack(const int8_t* q, const float* scale, int64_t rows, int cols, bool bf16, void* x, cudaStream_t s);
+cudaError_t launch_ckpt_swiglu_bwd(const int8_t* q, const float* scale, const void* dact, int64_t rows, int F, bool bf16, void* act,
+                                   void* dh, cudaStream_t s);
 
 cudaError_t launch_route(const RouteArgs& a, bool bf16, bool from_logits, cudaStream_t s);
 // bf16 router logits on the tensor cores with the gating epilogue (E > 64, or E % 4 == 0)

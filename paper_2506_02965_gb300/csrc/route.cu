@@ -986,6 +986,7 @@ size_t route_bwd_workspace(int64_t T, int P, int E, int d) {
 
 static cudaError_t launch_dlogits(const RouteBwdArgs& a, __nv_bfloat16* dz16, int EP, int32_t* chunk_off,
                                   int CH, int nchunk, cudaStream_t s) {
+    if (a.gate) return launch_gate_bwd(*a.gate, dz16, EP, chunk_off, CH, nchunk, s);
     const unsigned blocks = (unsigned)((a.T + 7) / 8);
 #define MOE_DL(NV)                                                                                 \
     (void)launch_pdl(dlogits_kernel<NV>, dim3(blocks), dim3(256), 0, s, a.probs, a.topk_idx, a.topk_w, \

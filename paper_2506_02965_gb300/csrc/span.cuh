@@ -58,6 +58,20 @@ template <typename T, int N> struct Span {
             }
         }
     }
+    // Largest magnitude of the elements as the bits of a float: unsigned order is that of the magnitudes, an
+    // infinity above every number and a NaN above that.
+    __device__ __forceinline__ uint32_t largest_bits() const {
+        uint32_t m = 0;
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) m = max(m, w[i] & 0x7fffffffu);
+            return m;
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) m = __vmaxu2(m, w[i] & 0x7fff7fffu);
+            return max(m << 16, m & 0xffff0000u);
+        }
+    }
     __device__ __forceinline__ void store(T* p) const {
         if constexpr (BYTES == 16) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
         else if constexpr (BYTES == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
@@ -74,15 +88,7 @@ template <typename T, int N> struct Span {
 // or a NaN gets scale NaN, so that all its values come back as NaN and none as a wrong number.
 constexpr int CKPT_BLOCK = 128;
 
-// Largest magnitude of N values as the bits of a float: unsigned order is that of the magnitudes,
-// an infinity above every number and a NaN above that.
-template <int N> __device__ __forceinline__ uint32_t largest_bits(const float (&f)[N]) {
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) m = max(m, __float_as_uint(f[i]) & 0x7fffffffu);
-    return m;
-}
-// the same over LANES (a power of two) consecutive, aligned lanes
+// The largest of LANES (a power of two) consecutive, aligned lanes
 template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t m) {
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -93,6 +99,23 @@ __device__ __forceinline__ void block_scale(uint32_t bits, float& scale, float& 
     const bool zero = bits < 0x0d800000u /* 2^-100 */, bad = bits >= 0x7f800000u;
     scale = zero ? 0.f : bad ? __uint_as_float(0x7fffffffu) : __fdiv_rn(a, 127.f);
     inv = zero || bad ? 0.f : __fdiv_rn(127.f, a);
+}
+// Scales of U blocks of LANES lanes each: bits(u) is the lane's largest magnitude of block u. Lane u gets block u's
+// scale, every lane all 127 / a: each lane does the divisions of one block (U of them in a lane cost more than the
+// rest of its quantisation).
+template <int LANES, int U, typename F> __device__ __forceinline__ void block_scales(F bits, float& scale, float (&inv)[U]) {
+    static_assert(U <= LANES && LANES <= 32);
+    const int lane = threadIdx.x % LANES;
+    uint32_t mine = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint32_t m = lanes_max<LANES>(bits(u));
+        mine = lane % U == u ? m : mine;
+    }
+    float v;
+    block_scale(mine, scale, v);
+#pragma unroll
+    for (int u = 0; u < U; ++u) inv[u] = __shfl_sync(0xffffffffu, v, (threadIdx.x & 31) - lane + u);
 }
 // Four values as int8 in a word. Adding 1.5 * 2^23 rounds the product to an integer (nearest, even)
 // and leaves it in the low byte in two's complement; the product is rounded first, as x * inv is.

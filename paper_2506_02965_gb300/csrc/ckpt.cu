@@ -1,6 +1,7 @@
 // Activation checkpoints in 8 bits (the blocks of span.cuh): packing, unpacking, and the SwiGLU
 // backward that reads [G|U] from one. Streams, all HBM-bound.
 #include <algorithm>
+#include <initializer_list>
 
 #include "moe_common.cuh"
 #include "moe_internal.h"
@@ -11,17 +12,35 @@ namespace moe {
 constexpr int CK_THREADS = 256;
 constexpr int CK_U = 4;  // blocks in flight per group of lanes
 
-// A group of 128 / VW lanes takes a block of 128 columns of a row, VW consecutive ones a lane; with
-// VW = 1 (rows that no 16-byte access fits) a warp takes it, four columns a lane, 32 apart.
-template <typename T, int VW> struct CkptMap {
-    static constexpr int LANES = VW == 1 ? 32 : CKPT_BLOCK / VW;
-    static constexpr int GROUPS = CK_THREADS / LANES;
-    static constexpr int SPANS = VW == 1 ? 4 : 1;
-    __device__ static __forceinline__ int col(int lane, int i) { return VW == 1 ? i * 32 + lane : lane * VW; }
+// Quotient of v < 2^31 by a fixed d: (v mul) >> (31 + s) with 2^s >= d and mul = ceil(2^(31+s) / d), which is
+// exact since mul d exceeds 2^(31+s) by less than 2^s.
+struct Divisor {
+    uint32_t d, mul, s;
+    explicit Divisor(uint32_t d_) : d(d_), mul(0), s(0) {
+        while ((1ull << s) < d) ++s;
+        if (s) mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t v) const { return s ? __umulhi(v, mul) >> (s - 1) : v; }
 };
 
+// A group of LANES lanes takes a block of 128 columns of a row: VW = 16 / sizeof(T) consecutive ones a lane (half a warp
+// or a warp a block), or in rows that no 16-byte access fits 2 or 1, 32 lanes of them in turn.
+template <typename T, int VW> struct CkptMap {
+    static constexpr int LANES = VW > 2 ? CKPT_BLOCK / VW : 32;
+    static constexpr int GROUPS = CK_THREADS / LANES;
+    static constexpr int SPANS = CKPT_BLOCK / (LANES * VW);
+    __device__ static __forceinline__ int col(int lane, int i) { return (i * LANES + lane) * VW; }
+};
+
+template <int VW> __device__ __forceinline__ void store_q(int8_t* p, const float (&f)[VW], float inv) {
+    if constexpr (VW == 8) *reinterpret_cast<uint2*>(p) = make_uint2(quant4(f[0], f[1], f[2], f[3], inv), quant4(f[4], f[5], f[6], f[7], inv));
+    else if constexpr (VW == 4) *reinterpret_cast<uint32_t*>(p) = quant4(f[0], f[1], f[2], f[3], inv);
+    else if constexpr (VW == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)quant4(f[0], f[1], 0.f, 0.f, inv);
+    else *p = quant1(f[0], inv);
+}
+
 template <typename T, int VW>
-__global__ void __launch_bounds__(CK_THREADS) ckpt_pack_kernel(const T* __restrict__ x, uint32_t blocks, int cols, uint32_t nb,
+__global__ void __launch_bounds__(CK_THREADS) ckpt_pack_kernel(const T* __restrict__ x, uint32_t blocks, int cols, Divisor nb,
                                                                int8_t* __restrict__ q, float* __restrict__ scale) {
     pdl_begin();
     using M = CkptMap<T, VW>;
@@ -33,7 +52,7 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_pack_kernel(const T* __restri
 #pragma unroll
     for (int u = 0; u < CK_U; ++u) {
         const uint32_t b = b0 + u * M::GROUPS;
-        const uint32_t row = b / nb, blk = b - row * nb;
+        const uint32_t row = nb(b), blk = b - row * nb.d;
         at[u] = (int64_t)row * cols + blk * CKPT_BLOCK;
         left[u] = b < blocks ? cols - (int)blk * CKPT_BLOCK : 0;
 #pragma unroll
@@ -43,35 +62,32 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_pack_kernel(const T* __restri
             else s[u][i].zero();
         }
     }
+    float sc, inv[CK_U];
+    block_scales<M::LANES, CK_U>(
+        [&](int u) {
+            uint32_t m = 0;
 #pragma unroll
-    for (int u = 0; u < CK_U; ++u) {
-        float f[M::SPANS][VW], sc, inv;
-        uint32_t m = 0;
+            for (int i = 0; i < M::SPANS; ++i) m = max(m, s[u][i].largest_bits());
+            return m;
+        },
+        sc, inv);
+    if (lane < CK_U && b0 + lane * M::GROUPS < blocks) scale[b0 + lane * M::GROUPS] = sc;
 #pragma unroll
-        for (int i = 0; i < M::SPANS; ++i) {
-            s[u][i].unpack(f[i]);
-            m = max(m, largest_bits(f[i]));
-        }
-        block_scale(lanes_max<M::LANES>(m), sc, inv);
+    for (int u = 0; u < CK_U; ++u)
 #pragma unroll
         for (int i = 0; i < M::SPANS; ++i) {
             const int c = M::col(lane, i);
             if (c < left[u]) {
-                int8_t* p = q + at[u] + c;
-                if constexpr (VW == 8)
-                    *reinterpret_cast<uint2*>(p) = make_uint2(quant4(f[i][0], f[i][1], f[i][2], f[i][3], inv),
-                                                              quant4(f[i][4], f[i][5], f[i][6], f[i][7], inv));
-                else if constexpr (VW == 4) *reinterpret_cast<uint32_t*>(p) = quant4(f[i][0], f[i][1], f[i][2], f[i][3], inv);
-                else *p = quant1(f[i][0], inv);
+                float f[VW];
+                s[u][i].unpack(f);
+                store_q<VW>(q + at[u] + c, f, inv[u]);
             }
         }
-        if (lane == 0 && left[u] > 0) scale[b0 + u * M::GROUPS] = sc;
-    }
 }
 
 template <typename T, int VW>
 __global__ void __launch_bounds__(CK_THREADS) ckpt_unpack_kernel(const int8_t* __restrict__ q, const float* __restrict__ scale,
-                                                                 uint32_t blocks, int cols, uint32_t nb, T* __restrict__ x) {
+                                                                 uint32_t blocks, int cols, Divisor nb, T* __restrict__ x) {
     pdl_begin();
     using M = CkptMap<T, VW>;
     const int lane = threadIdx.x % M::LANES;
@@ -83,7 +99,7 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_unpack_kernel(const int8_t* _
 #pragma unroll
     for (int u = 0; u < CK_U; ++u) {
         const uint32_t b = b0 + u * M::GROUPS;
-        const uint32_t row = b / nb, blk = b - row * nb;
+        const uint32_t row = nb(b), blk = b - row * nb.d;
         at[u] = (int64_t)row * cols + blk * CKPT_BLOCK;
         left[u] = b < blocks ? cols - (int)blk * CKPT_BLOCK : 0;
         if (left[u] > 0) sc[u] = scale[b];
@@ -108,35 +124,39 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_unpack_kernel(const int8_t* _
         }
 }
 
+template <int VW> constexpr int swiglu_spans() { return VW == 8 ? 2 : 4; }
+
 // SwiGLU backward from the checkpoint of [G|U] (rows of 2F columns in one run of blocks):
 //   s = sigmoid(G), act = G s U, dU = dA G s, dG = dA U s (1 + G (1 - s)).
-// Two spans a thread. The sigmoid of bf16 results takes the fast exponential and quotient (errors of a few
-// 2^-23, results rounded to 2^-8); with the full-precision ones their instructions, not HBM, are the bound.
+// The sigmoid of bf16 results takes the fast exponential and quotient (errors of a few 2^-23, results rounded to
+// 2^-8); with the full-precision ones their instructions, not HBM, are the bound.
 template <typename T, int VW>
 __global__ void __launch_bounds__(CK_THREADS) ckpt_swiglu_bwd_kernel(const int8_t* __restrict__ q, const float* __restrict__ scale,
-                                                                     const T* __restrict__ dact, uint32_t spans, uint32_t per_row,
+                                                                     const T* __restrict__ dact, uint32_t spans, Divisor per_row,
                                                                      int F, int nb, T* __restrict__ act, T* __restrict__ dh) {
     pdl_begin();
-    constexpr int U = 2;
+    constexpr int U = swiglu_spans<VW>();
     Span<T, VW> sd[U];
     uint32_t wg[U][(VW + 3) / 4], wu[U][(VW + 3) / 4];
     float cg[U], cu[U];
-    uint32_t row[U];
-    int col[U];
+    int64_t at[U];  // in rows of F; in rows of 2F
+    int64_t at2[U];
     bool on[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint32_t v = blockIdx.x * (CK_THREADS * U) + u * CK_THREADS + threadIdx.x;
         on[u] = v < spans;
-        row[u] = v / per_row;
-        col[u] = (int)(v - row[u] * per_row) * VW;
+        const uint32_t row = per_row(v);
+        const int col = (int)(v - row * per_row.d) * VW;
+        at[u] = (int64_t)v * VW;
+        at2[u] = at[u] + (int64_t)row * F;
         if (on[u]) {
-            const int8_t* p = q + (int64_t)row[u] * 2 * F + col[u];
-            load_q<VW>(p, wg[u]);
-            load_q<VW>(p + F, wu[u]);
-            cg[u] = scale[(int64_t)row[u] * nb + col[u] / CKPT_BLOCK];
-            cu[u] = scale[(int64_t)row[u] * nb + (F + col[u]) / CKPT_BLOCK];
-            sd[u].load(dact + (int64_t)row[u] * F + col[u]);
+            load_q<VW>(q + at2[u], wg[u]);
+            load_q<VW>(q + at2[u] + F, wu[u]);
+            const float* sc = scale + (int64_t)row * nb;
+            cg[u] = sc[col / CKPT_BLOCK];
+            cu[u] = sc[(F + col) / CKPT_BLOCK];
+            sd[u].load(dact + at[u]);
         }
     }
 #pragma unroll
@@ -156,12 +176,11 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_swiglu_bwd_kernel(const int8_
         }
         Span<T, VW> o;
         o.pack(a);
-        o.store(act + (int64_t)row[u] * F + col[u]);
-        T* out = dh + (int64_t)row[u] * 2 * F + col[u];
+        o.store(act + at[u]);
         o.pack(dg);
-        o.store(out);
+        o.store(dh + at2[u]);
         o.pack(du);
-        o.store(out + F);
+        o.store(dh + at2[u] + F);
     }
 }
 
@@ -185,7 +204,7 @@ static cudaError_t pack_t(const T* x, int64_t rows, int cols, int8_t* q, float* 
     constexpr int PER = CkptMap<T, VW>::GROUPS * CK_U;
     return by_rows(rows, nb, [&](int64_t r, int64_t n) {
         (void)launch_pdl(ckpt_pack_kernel<T, VW>, dim3((unsigned)((n * nb + PER - 1) / PER)), dim3(CK_THREADS), 0, s, x + r * cols,
-                         (uint32_t)(n * nb), cols, (uint32_t)nb, q + r * cols, scale + r * nb);
+                         (uint32_t)(n * nb), cols, Divisor((uint32_t)nb), q + r * cols, scale + r * nb);
     });
 }
 template <typename T, int VW>
@@ -194,36 +213,49 @@ static cudaError_t unpack_t(const int8_t* q, const float* scale, int64_t rows, i
     constexpr int PER = CkptMap<T, VW>::GROUPS * CK_U;
     return by_rows(rows, nb, [&](int64_t r, int64_t n) {
         (void)launch_pdl(ckpt_unpack_kernel<T, VW>, dim3((unsigned)((n * nb + PER - 1) / PER)), dim3(CK_THREADS), 0, s, q + r * cols,
-                         scale + r * nb, (uint32_t)(n * nb), cols, (uint32_t)nb, x + r * cols);
+                         scale + r * nb, (uint32_t)(n * nb), cols, Divisor((uint32_t)nb), x + r * cols);
     });
 }
 template <typename T, int VW>
 static cudaError_t swiglu_t(const int8_t* q, const float* scale, const T* dact, int64_t rows, int F, T* act, T* dh, cudaStream_t s) {
     const int64_t per_row = F / VW, nb = (2 * (int64_t)F + CKPT_BLOCK - 1) / CKPT_BLOCK;
-    constexpr int PER = 2 * CK_THREADS;
+    constexpr int PER = swiglu_spans<VW>() * CK_THREADS;
     return by_rows(rows, per_row, [&](int64_t r, int64_t n) {
         (void)launch_pdl(ckpt_swiglu_bwd_kernel<T, VW>, dim3((unsigned)((n * per_row + PER - 1) / PER)), dim3(CK_THREADS), 0, s,
-                         q + r * 2 * F, scale + r * nb, dact + r * F, (uint32_t)(n * per_row), (uint32_t)per_row, F, (int)nb,
+                         q + r * 2 * F, scale + r * nb, dact + r * F, (uint32_t)(n * per_row), Divisor((uint32_t)per_row), F, (int)nb,
                          act + r * F, dh + r * 2 * F);
     });
 }
 
+// The widest span that all of a row's accesses are aligned to: 16 bytes, two elements or one
+template <typename T> static int span_of(int cols, std::initializer_list<const void*> elems, const int8_t* q) {
+    for (int vw : {16 / (int)sizeof(T), 2}) {
+        bool ok = cols % vw == 0 && aligned_to(q, vw);
+        for (const void* p : elems) ok = ok && aligned_to(p, vw * sizeof(T));
+        if (ok) return vw;
+    }
+    return 1;
+}
+#define MOE_BY_SPAN(vw, CALL) (vw > 2 ? CALL(16 / (int)sizeof(T)) : vw == 2 ? CALL(2) : CALL(1))
+
 template <typename T> static cudaError_t pack_any(const void* x, int64_t rows, int cols, int8_t* q, float* scale, cudaStream_t s) {
-    constexpr int VW = 16 / sizeof(T);
-    if (cols % VW == 0 && aligned_to(x, 16) && aligned_to(q, VW)) return pack_t<T, VW>((const T*)x, rows, cols, q, scale, s);
-    return pack_t<T, 1>((const T*)x, rows, cols, q, scale, s);
+    const int vw = span_of<T>(cols, {x}, q);
+#define MOE_CK(V) pack_t<T, V>((const T*)x, rows, cols, q, scale, s)
+    return MOE_BY_SPAN(vw, MOE_CK);
+#undef MOE_CK
 }
 template <typename T> static cudaError_t unpack_any(const int8_t* q, const float* scale, int64_t rows, int cols, void* x, cudaStream_t s) {
-    constexpr int VW = 16 / sizeof(T);
-    if (cols % VW == 0 && aligned_to(x, 16) && aligned_to(q, VW)) return unpack_t<T, VW>(q, scale, rows, cols, (T*)x, s);
-    return unpack_t<T, 1>(q, scale, rows, cols, (T*)x, s);
+    const int vw = span_of<T>(cols, {x}, q);
+#define MOE_CK(V) unpack_t<T, V>(q, scale, rows, cols, (T*)x, s)
+    return MOE_BY_SPAN(vw, MOE_CK);
+#undef MOE_CK
 }
 template <typename T>
 static cudaError_t swiglu_any(const int8_t* q, const float* scale, const void* dact, int64_t rows, int F, void* act, void* dh, cudaStream_t s) {
-    constexpr int VW = 16 / sizeof(T);
-    if (F % VW == 0 && aligned_to(q, VW) && aligned_to(dact, 16) && aligned_to(act, 16) && aligned_to(dh, 16))
-        return swiglu_t<T, VW>(q, scale, (const T*)dact, rows, F, (T*)act, (T*)dh, s);
-    return swiglu_t<T, 1>(q, scale, (const T*)dact, rows, F, (T*)act, (T*)dh, s);
+    const int vw = span_of<T>(F, {dact, act, dh}, q);
+#define MOE_CK(V) swiglu_t<T, V>(q, scale, (const T*)dact, rows, F, (T*)act, (T*)dh, s)
+    return MOE_BY_SPAN(vw, MOE_CK);
+#undef MOE_CK
 }
 
 cudaError_t launch_ckpt_pack(const void* x, int64_t rows, int cols, bool bf16, int8_t* q, float* scale, cudaStream_t s) {

@@ -2,12 +2,17 @@
 // in the choice only, expert groups of which some are kept, k picks, renormalised and scaled
 // weights; their backward; the balance bias's update.
 //
-// A token's scores live in the registers of LPT lanes (8, 16 or 32: several tokens a warp for small
-// pools), NV per lane. Each group of experts owns an equal, power-of-two share of the token's
-// lanes and its experts lie in them in ascending order, so that a group's key is a reduction over
-// aligned lanes and, among equal keys, the lowest (lane, place) is the lowest expert.
-// The loads are few (a token's row once); what bounds these kernels is instructions per score and, for
-// short batches, the launch.
+// A token's keys live in the registers of LPT lanes (8, 16 or 32: several tokens a warp), up to 32 a
+// lane, each group of experts in an equal, power-of-two share of the lanes, so that a group's key
+// is a reduction over aligned lanes. The k largest keys come out of sorting networks: every lane sorts its
+// own, then lanes merge pairwise, each merge keeping the KT (2, 4, 8) largest of two sorted lists; no
+// step waits for the one before it as k rounds of "largest left" would.
+//
+// Picks are decided by exact keys. The networks sort approximate ones, 24 bits of distance from the row's
+// largest with the expert in the 8 below: enough wherever the keys that decide lie further apart than the
+// approximation, which is checked; a token of closer ones (equal keys, or about one in 500 of random ones) is decided
+// by a whole warp from exact keys, one pick after the other. What bounds the kernel is instructions, some
+// tens per expert, not the row's one read.
 #include <algorithm>
 
 #include "moe_common.cuh"
@@ -16,6 +21,7 @@
 namespace moe {
 
 constexpr int GT_THREADS = 256;
+constexpr int GT_RESIDENT = 3;  // CTAs per SM (65536 tokens, E = 256, 8 groups: 54.6 us; 4: 59.3, 5: 66.6, whose registers spill)
 
 template <int LPT> __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
@@ -27,15 +33,6 @@ template <int LPT> __device__ __forceinline__ float lanes_maxf(float v) {
     for (int o = LPT / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
-template <int LPT> __device__ __forceinline__ uint32_t lanes_maxu(uint32_t v) {
-    if constexpr (LPT == 32) {
-        return __reduce_max_sync(0xffffffffu, v);
-    } else {
-#pragma unroll
-        for (int o = LPT / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
-        return v;
-    }
-}
 
 // Floats in the order of unsigned integers; -0 counts as +0. The lowest is -inf, above 0.
 __device__ __forceinline__ uint32_t ordered(float f) {
@@ -43,16 +40,196 @@ __device__ __forceinline__ uint32_t ordered(float f) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-template <int NV, int LPT, bool SIG>
-__global__ void __launch_bounds__(GT_THREADS) gate_kernel(GateArgs a, int lpg, int nv, int chunk, bool whole) {
+__device__ __forceinline__ float unordered(uint32_t u) {
+    return __uint_as_float((u & 0x80000000u) ? u ^ 0x80000000u : ~u);
+}
+constexpr uint32_t KEY_NINF = 0x007fffffu;  // ordered(-inf)
+
+// ---------------------------------------------------------------- sorting networks, descending
+__device__ __forceinline__ void cswap(uint32_t& a, uint32_t& b) {
+    const uint32_t hi = max(a, b), lo = min(a, b);
+    a = hi;
+    b = lo;
+}
+// a bitonic list of N (a power of two)
+template <int N> __device__ __forceinline__ void sort_bitonic(uint32_t* v) {
+#pragma unroll
+    for (int h = N / 2; h > 0; h >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (!(i & h)) cswap(v[i], v[i + h]);
+}
+// any list of N, odd-even merge sort
+template <int N> __device__ __forceinline__ void sort_any(uint32_t* v) {
+#pragma unroll
+    for (int p = 1; p < N; p <<= 1)
+#pragma unroll
+        for (int h = p; h > 0; h >>= 1)
+#pragma unroll
+            for (int j = h % p; j + h < N; j += 2 * h)
+#pragma unroll
+                for (int i = 0; i < h; ++i)
+                    if (i + j + h < N && (i + j) / (2 * p) == (i + j + h) / (2 * p)) cswap(v[i + j], v[i + j + h]);
+}
+// a <- the N largest of two sorted lists, sorted
+template <int N> __device__ __forceinline__ void merge_top(uint32_t* a, const uint32_t* b) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) a[i] = max(a[i], b[N - 1 - i]);
+    sort_bitonic<N>(a);
+}
+
+// Score of one logit: softmax with the row's largest m and 1 / sum, or sigmoid.
+template <bool SIG> __device__ __forceinline__ float score_of(float z, float m, float inv) {
+    return SIG ? 1.f / (1.f + expf(-z)) : expf(z - m) * inv;
+}
+
+// 2^x and 1 / x by one instruction each: off by at most 2^-22 and 2^-23 of the result
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float LOG2E = 1.4426950408889634f;
+// exp(x), off by 2^-22 + |x| 2^-24 of the result
+__device__ __forceinline__ float fast_exp(float x) { return fast_exp2(x * LOG2E); }
+
+// How far two groups' keys, sums of up to two keys, have to be apart for their order to be sure. A fast sigmoid is off
+// by s (1 - s) (2^-22 + |z| 2^-24) + 2^-23 < 2.5e-7 and the exact one by as much, a sum with a bias by 2^-24 of
+// itself on both sides.
+__device__ __forceinline__ float sum_margin(float a, float b) { return fmaf(fabsf(a) + fabsf(b), 5e-7f, 2.4e-6f); }
+
+// Keys for sorting: the distance of a key below the largest, in units of KEY_RANGE / 2^23 up to KEY_RANGE
+// (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
+// the top down, and bit 31; an expert's 255 - id below. Two keys of the exact order can come out the other way
+// round only within KEY_SURE: 4 units of the fast sigmoid's error, 3 of the roundings here.
+template <bool SIG> __device__ __forceinline__ uint32_t sort_key(float key, float most, int id) {
+    constexpr float RANGE = SIG ? 2.f : 16.f;
+    const float t = __saturatef(fmaf(key - most, 1.f / RANGE, 1.f));
+    return __byte_perm(__float_as_uint(fmaf(t, 16777214.f, 16777216.f)), (uint32_t)(255 - id), 0x2104);
+}
+constexpr uint32_t KEY_SURE = 9u << 8;
+
+// Where a lane's slots lie in its group, in spans of 4 (VEC) or single places, the group's lanes in turn
+template <bool VEC> struct Slots {
+    int lpg, lg, cnt;  // lanes of the group, this one's place among them, the slots it holds
+    __device__ __forceinline__ Slots(int lpg_, int lg_, int size) : lpg(lpg_), lg(lg_) {
+        cnt = VEC ? (size / 4 - lg + lpg - 1) / lpg * 4 : (size - lg + lpg - 1) / lpg;
+        cnt = size == 0 ? 0 : max(cnt, 0);
+    }
+    __device__ __forceinline__ int at(int i) const { return VEC ? ((i / 4) * lpg + lg) * 4 + i % 4 : i * lpg + lg; }
+    // values of the slots from p (of the group's first expert); `none` past them
+    template <int NV> __device__ __forceinline__ void load(const float* p, bool on, float none, float (&z)[NV]) const {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < NV; i += 4) {
+                float4 v = make_float4(none, none, none, none);
+                if (on && i < cnt) v = *reinterpret_cast<const float4*>(p + at(i));
+                z[i] = v.x; z[i + 1] = v.y; z[i + 2] = v.z; z[i + 3] = v.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) z[i] = on && i < cnt ? p[at(i)] : none;
+        }
+    }
+};
+
+// the two largest of a group's keys, in all its lanes
+template <typename V> __device__ __forceinline__ void group_best(V& b1, V& b2, int lpg) {
+    for (int o = lpg >> 1; o > 0; o >>= 1) {
+        const V c1 = __shfl_xor_sync(0xffffffffu, b1, o), c2 = __shfl_xor_sync(0xffffffffu, b2, o);
+        b2 = max(min(b1, c1), max(b2, c2));
+        b1 = max(b1, c1);
+    }
+}
+
+constexpr int GT_CAND = 24;  // keys too close to tell that a token's own lanes decide
+struct Candidates {
+    int n, id[GT_CAND];
+    uint32_t key[GT_CAND];
+};
+
+// The picks of one token by exact keys, by a whole warp: one after the other, the lowest id of the largest key
+template <bool SIG>
+__device__ __noinline__ void exact_token(const GateArgs& a, int64_t t, int* picks) {
+    constexpr float NINF = -INFINITY;
+    constexpr int NV = 16;  // of 256 experts over 32 lanes, of which a number of groups past a power of two leaves up to half idle
+    int groups2 = 1;
+    while (groups2 < a.groups) groups2 *= 2;
+    const int lane = threadIdx.x & 31, lpg = 32 / groups2, grp = lane / lpg, gs = a.E / a.groups, first = grp * gs;
+    const Slots<false> slots(lpg, lane % lpg, grp < a.groups ? gs : 0);
+    const float* row = a.logits + t * a.E + first;
+    const float* bias = a.bias ? a.bias + (int64_t)party_of(a.po, a.P, t) * a.E + first : nullptr;
+    uint32_t u[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const float z = i < slots.cnt ? row[slots.at(i)] : NINF;
+        float key = SIG ? score_of<true>(z, 0.f, 1.f) : z;
+        if (bias && i < slots.cnt) key = __fadd_rn(key, bias[slots.at(i)]);
+        u[i] = i >= slots.cnt ? 0u : z > NINF ? ordered(key) : KEY_NINF;
+    }
+    if (a.top_groups < a.groups) {
+        uint32_t b1 = 0, b2 = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            b2 = max(b2, min(b1, u[i]));
+            b1 = max(b1, u[i]);
+        }
+        group_best(b1, b2, lpg);
+        const uint32_t mine = a.group_top == 2 ? ordered(unordered(b1) + unordered(b2)) : b1;
+        int rank = 0;
+        for (int g = 0; g < a.groups; ++g) {
+            const uint32_t other = __shfl_sync(0xffffffffu, mine, g * lpg);
+            rank += other > mine || (other == mine && g < grp);
+        }
+        if (rank >= a.top_groups) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) u[i] = 0u;
+        }
+    }
+    uint32_t best = 0, id = 0;  // the lane's largest and 256 less its lowest id
+    auto scan = [&]() {
+        best = id = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (u[i] > best) {
+                best = u[i];
+                id = (uint32_t)(256 - (first + slots.at(i)));
+            }
+    };
+    scan();
+    for (int j = 0; j < a.k; ++j) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+        const uint32_t low = __reduce_max_sync(0xffffffffu, best == top ? id : 0u);
+        if (lane == 0) picks[j] = 256 - (int)low;
+        if (id == low) {  // one lane: its largest goes
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if ((uint32_t)(256 - (first + slots.at(i))) == low) u[i] = 0u;
+            scan();
+        }
+    }
+    __syncwarp();
+}
+
+template <int NV, int LPT, int KT, bool VEC, bool SIG>
+__global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __grid_constant__ GateArgs a, int lpg, int chunk,
+                                                                         bool whole) {
     pdl_begin();
-    __shared__ int hist[256];
     constexpr float NINF = -INFINITY;
     constexpr int TPW = 32 / LPT, TPC = GT_THREADS / LPT;  // tokens per warp and per CTA at a time
+    __shared__ int hist[256];
+    __shared__ int s_pick[TPC][8];
+    __shared__ Candidates s_cand[TPC];
     const int lane = threadIdx.x & 31, l = lane % LPT, base = lane - l;
-    const int E = a.E, k = a.k, gs = E / a.groups;
-    const int grp = l / lpg, lg = l % lpg, e0 = grp * gs + lg * nv;
-    const int cnt = grp < a.groups ? min(max(gs - lg * nv, 0), nv) : 0;
+    const int E = a.E, k = a.k, gs = E / a.groups, grp = l / lpg, first = grp * gs;
+    const Slots<VEC> slots(lpg, l % lpg, grp < a.groups ? gs : 0);
+    int* picks = s_pick[threadIdx.x / LPT];
+    Candidates& cand = s_cand[threadIdx.x / LPT];
     const int64_t t0 = (int64_t)blockIdx.x * chunk, t1 = min64(t0 + chunk, a.T);
     const int p0 = party_of(a.po, a.P, t0);
     for (int e = threadIdx.x; e < E; e += GT_THREADS) hist[e] = 0;
@@ -62,108 +239,161 @@ __global__ void __launch_bounds__(GT_THREADS) gate_kernel(GateArgs a, int lpg, i
         const int64_t t = tw + lane / LPT;
         const bool on = t < t1;
         const int party = on ? party_of(a.po, a.P, t) : p0;
-        float z[NV], s[NV];
-        const float* row = a.logits + t * E + e0;
-        if (a.vec) {
+        const float* row = a.logits + t * E + first;
+        const float* bias = a.bias ? a.bias + (int64_t)party * E + first : nullptr;
+        float key[NV], m = 0.f, inv = 1.f;
+        slots.template load<NV>(row, on, NINF, key);
+        if constexpr (!SIG) {
+            m = NINF;
 #pragma unroll
-            for (int i = 0; i < NV; i += 4) {
-                float4 v = make_float4(NINF, NINF, NINF, NINF);
-                if (on && i < cnt) v = *reinterpret_cast<const float4*>(row + i);
-                z[i] = v.x;
-                if (i + 1 < NV) z[i + 1] = v.y;
-                if (i + 2 < NV) z[i + 2] = v.z;
-                if (i + 3 < NV) z[i + 3] = v.w;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) z[i] = on && i < cnt ? row[i] : NINF;
-        }
-#pragma unroll
-        for (int i = 0; i < NV; ++i) z[i] = z[i] == z[i] ? z[i] : NINF;  // NaN: out of reach
-        if constexpr (SIG) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) s[i] = 1.f / (1.f + expf(-z[i]));
-        } else {
-            float m = NINF, sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) m = fmaxf(m, z[i]);
+            for (int i = 0; i < NV; ++i) m = fmaxf(m, key[i]);  // (passes over NaN)
             m = lanes_maxf<LPT>(m);
             m = m == NINF ? 0.f : m;
+            float sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                s[i] = expf(z[i] - m);
-                sum += s[i];
-            }
+            for (int i = 0; i < NV; ++i) sum += fast_exp(fmaxf(key[i] - m, NINF));  // NaN: 0
             sum = lanes_sum<LPT>(sum);
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) s[i] *= inv;
+            inv = sum == 0.f ? 0.f : 1.f / sum;
         }
         if (a.scores && on) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (i < cnt) a.scores[t * E + e0 + i] = s[i];
+                if (i < slots.cnt)
+                    a.scores[t * E + first + slots.at(i)] = key[i] > NINF ? score_of<SIG>(key[i], m, inv) : 0.f;
         }
-        // keys, and the two best of the lane
-        float key[NV], b1 = NINF, b2 = NINF;
-        const float* bias = a.bias ? a.bias + (int64_t)party * E + e0 : nullptr;
+        {
+            float b[NV];
+            if (bias) slots.template load<NV>(bias, true, 0.f, b);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            key[i] = SIG ? s[i] : z[i];
-            if (bias && i < cnt) key[i] = __fadd_rn(key[i], bias[i]);
-            if (!(z[i] > NINF) || key[i] != key[i]) key[i] = NINF;
-            b2 = fmaxf(b2, fminf(b1, key[i]));
-            b1 = fmaxf(b1, key[i]);
+            for (int i = 0; i < NV; ++i) {
+                const bool reach = key[i] > NINF;  // (a NaN is out of reach)
+                if constexpr (SIG) key[i] = fast_rcp(1.f + fast_exp(-key[i]));
+                if (bias) key[i] += b[i];
+                key[i] = reach ? key[i] : NINF;
+            }
         }
         bool kept = true;
         if (a.top_groups < a.groups) {
-            for (int o = lpg >> 1; o > 0; o >>= 1) {
-                const float c1 = __shfl_xor_sync(0xffffffffu, b1, o), c2 = __shfl_xor_sync(0xffffffffu, b2, o);
-                b2 = fmaxf(fminf(b1, c1), fmaxf(b2, c2));
-                b1 = fmaxf(b1, c1);
-            }
-            const uint32_t mine = ordered(a.group_top == 2 ? b1 + b2 : b1);
-            int rank = 0;
-            for (int g = 0; g < a.groups; ++g) {
-                const uint32_t other = __shfl_sync(0xffffffffu, mine, base + g * lpg);
-                rank += other > mine || (other == mine && g < grp);
-            }
-            kept = rank < a.top_groups;
-        }
-        uint32_t u[NV];
+            bool sure = true;
+            for (int pass = 0; pass < 2; ++pass) {
+                float b1 = NINF, b2 = NINF;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) u[i] = kept && i < cnt ? ordered(key[i]) : 0u;  // 0: not to be picked
-        // pick j stays in lane j
-        int pe = 0;
+                for (int i = 0; i < NV; ++i) {
+                    b2 = fmaxf(b2, fminf(b1, key[i]));
+                    b1 = fmaxf(b1, key[i]);
+                }
+                group_best(b1, b2, lpg);
+                const float mine = a.group_top == 2 ? b1 + b2 : b1, margin = sum_margin(b1, a.group_top == 2 ? b2 : 0.f);
+                int rank = 0;
+                for (int g = 0; g < a.groups; ++g) {
+                    const float other = __shfl_sync(0xffffffffu, mine, base + g * lpg);
+                    rank += other > mine || (other == mine && g < grp);
+                    sure &= g == grp || fabsf(other - mine) > margin;  // (not so for two of -inf)
+                }
+                kept = rank < a.top_groups;
+                // exact keys in their place, and once more, where two groups are too close
+                if (pass == 1 || !__any_sync(0xffffffffu, on && !sure && grp < a.groups)) break;
+                slots.template load<NV>(row, on, NINF, key);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const bool reach = key[i] > NINF;
+                    if constexpr (SIG) key[i] = score_of<true>(key[i], 0.f, 1.f);
+                    if (bias && i < slots.cnt) key[i] = __fadd_rn(key[i], bias[slots.at(i)]);
+                    key[i] = reach ? key[i] : NINF;
+                }
+            }
+        }
+        float most = key[0];
+#pragma unroll
+        for (int i = 1; i < NV; ++i) most = fmaxf(most, key[i]);
+        most = fmaxf(lanes_maxf<LPT>(most), -3.4e38f);
+        uint32_t u[NV];  // 0 where there is nothing to pick
+#pragma unroll
+        for (int i = 0; i < NV; ++i) u[i] = kept && i < slots.cnt ? sort_key<SIG>(key[i], most, first + slots.at(i)) : 0u;
+        uint32_t v[KT];
+#pragma unroll
+        for (int i = 0; i < KT; ++i) v[i] = i < NV ? u[i] : 0u;
+        sort_any<KT>(v);
+#pragma unroll
+        for (int c = KT; c < NV; c += KT) {
+            uint32_t w[KT];
+#pragma unroll
+            for (int i = 0; i < KT; ++i) w[i] = u[c + i];
+            sort_any<KT>(w);
+            merge_top<KT>(v, w);
+        }
+#pragma unroll
+        for (int o = 1; o < LPT; o <<= 1) {
+            uint32_t w[KT];
+#pragma unroll
+            for (int i = 0; i < KT; ++i) w[i] = __shfl_xor_sync(0xffffffffu, v[i], o);
+            merge_top<KT>(v, w);
+        }
+        // Sure where each of the k largest is clear of the next, and the last of all others, by their count
+        uint32_t mine = v[0], last = v[0];
+        bool sure = true;
+#pragma unroll
+        for (int i = 1; i < KT; ++i) {
+            if (i < k) {
+                sure &= last - v[i] >= KEY_SURE;
+                last = v[i];
+                mine = l == i ? v[i] : mine;
+            }
+        }
+        last -= KEY_SURE;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) n += u[i] >= last;
+#pragma unroll
+        for (int o = 1; o < LPT; o <<= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
+        sure &= n == k;
+        int pe = 255 - (int)(mine & 0xffu);
+        if (__any_sync(0xffffffffu, on && !sure)) {
+            // the few that are not clear of the k largest, by exact keys against each other
+            if (l == 0) cand.n = 0;
+            __syncwarp();
+#pragma unroll 1
+            for (int i = 0; i < NV; ++i) {
+                uint32_t ui = 0;
+#pragma unroll
+                for (int j = 0; j < NV; ++j) ui = i == j ? u[j] : ui;
+                if (ui >= last && n <= GT_CAND) cand.id[atomicAdd(&cand.n, 1)] = 255 - (int)(ui & 0xffu);
+            }
+            __syncwarp();
+            if (on && n <= GT_CAND) {
+                for (int c = l; c < n; c += LPT) {
+                    const int e = cand.id[c];
+                    const float z = a.logits[t * E + e];
+                    float x = SIG ? score_of<true>(z, 0.f, 1.f) : z;
+                    if (bias) x = __fadd_rn(x, bias[e - first]);
+                    cand.key[c] = z > NINF ? ordered(x) : KEY_NINF;
+                }
+            }
+            __syncwarp();
+            if (on && n <= GT_CAND) {
+                for (int c = l; c < n; c += LPT) {
+                    int rank = 0;
+                    for (int o = 0; o < n; ++o)
+                        rank += cand.key[o] > cand.key[c] || (cand.key[o] == cand.key[c] && cand.id[o] < cand.id[c]);
+                    if (rank < k) picks[rank] = cand.id[c];
+                }
+            }
+            __syncwarp();
+            // many that are not (equal keys): each such token by the whole warp
+            const uint32_t many = __ballot_sync(0xffffffffu, on && n > GT_CAND);
+#pragma unroll 1
+            for (int j = 0; j < TPW; ++j)
+                if ((many >> (j * LPT)) & 1u) exact_token<SIG>(a, tw + j, s_pick[(threadIdx.x / 32) * TPW + j]);
+            if (l < k) pe = picks[l];
+            __syncwarp();
+        }
+        // pick j in lane j
         float ps = 0.f;
-        for (int j = 0; j < k; ++j) {
-            uint32_t m = u[0];
-#pragma unroll
-            for (int i = 1; i < NV; ++i) m = max(m, u[i]);
-            const uint32_t best = lanes_maxu<LPT>(m);
-            const uint32_t who = __ballot_sync(0xffffffffu, m == best) >> base;
-            const int owner = base + __ffs(LPT == 32 ? who : who & ((1u << LPT) - 1)) - 1;
-            int e = 0;
-            float sv = 0.f;
-            if (lane == owner) {
-                bool found = false;
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-                    if (!found && u[i] == best) {
-                        found = true;
-                        e = e0 + i;
-                        sv = s[i];
-                        u[i] = 0u;
-                    }
-            }
-            e = __shfl_sync(0xffffffffu, e, owner);
-            sv = __shfl_sync(0xffffffffu, sv, owner);
-            if (l == j) {
-                pe = e;
-                ps = sv;
-            }
+        if (on && l < k) {
+            const float pz = a.logits[t * E + pe];
+            ps = pz > NINF ? score_of<SIG>(pz, m, inv) : 0.f;
         }
-        const float total = a.normalize ? lanes_sum<8>(l < k ? ps : 0.f) : 1.f;  // the picks are in a token's first 8 lanes
+        const float total = a.normalize ? lanes_sum<8>(ps) : 1.f;  // the picks are in a token's first 8 lanes
         if (on && l < k) {
             a.topk_idx[t * k + l] = pe;
             a.topk_w[t * k + l] = total == 0.f ? 0.f : a.scale * ps / total;
@@ -178,15 +408,23 @@ __global__ void __launch_bounds__(GT_THREADS) gate_kernel(GateArgs a, int lpg, i
     }
 }
 
-// dlogits of a token by LPT lanes, spans of SP = 4 (or single) scores a lane. The picks' gradients go
-// to their places through shared memory, on top of aux_coef.
-template <int NV, int LPT, int SP, bool SIG>
-__global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(GateBwdArgs a, __nv_bfloat16* dz16, int EP, int32_t* chunk_off, int CH,
-                                                              int nchunk) {
+__global__ void __launch_bounds__(256) gate_zero_kernel(int32_t* counts, int n) {
+    pdl_begin();
+    const int i = blockIdx.x * 256 + threadIdx.x;
+    if (i < n) counts[i] = 0;
+}
+
+// dlogits of a token by 8 lanes (four tokens a warp), NV scores a lane in spans of SP = 4 (or single ones).
+// The picks' gradients touch k places of a row: the row is written as if there were none (but for
+// their part in softmax's <ds, s>), then lane j writes pick j's place again. One read and one write of a
+// row; fast exponentials (2^-22 of the result, as the row's sum).
+constexpr int GB_LPT = 8;
+template <int NV, int SP, bool SIG>
+__global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(const __grid_constant__ GateBwdArgs a, __nv_bfloat16* dz16, int EP,
+                                                              int32_t* chunk_off, int CH, int nchunk) {
     pdl_begin();
     constexpr float NINF = -INFINITY;
-    constexpr int TPC = GT_THREADS / LPT;
-    __shared__ float4 s_dp[GT_THREADS * NV / 4];
+    constexpr int LPT = GB_LPT, TPC = GT_THREADS / LPT;
     if (chunk_off && blockIdx.x == 0 && threadIdx.x == 0) {  // the chunks of the weight gradient's contraction
         int c = 0;
         for (int q = 0; q < a.P; ++q) {
@@ -198,97 +436,91 @@ __global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(GateBwdArgs a, __n
     const int E = a.E, k = a.k, l = threadIdx.x % LPT;
     const int64_t t = (int64_t)blockIdx.x * TPC + threadIdx.x / LPT;
     const bool on = t < a.T;
-    float* dps = reinterpret_cast<float*>(s_dp) + (threadIdx.x / LPT) * (NV * LPT);
-    const int party = on && a.aux_coef ? party_of(a.po, a.P, t) : 0;
+    const float* row = a.logits + t * E;
+    const float* aux = a.aux_coef && on ? a.aux_coef + (int64_t)party_of(a.po, a.P, t) * E : nullptr;
     float z[NV];
 #pragma unroll
     for (int i = 0; i < NV; i += SP) {
         const int e = i * LPT + l * SP;
         if constexpr (SP == 4) {
-            float4 v = make_float4(NINF, NINF, NINF, NINF), c = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (on && e < E) v = *reinterpret_cast<const float4*>(a.logits + t * E + e);
-            if (on && e < E && a.aux_coef) c = *reinterpret_cast<const float4*>(a.aux_coef + (int64_t)party * E + e);
+            float4 v = make_float4(NINF, NINF, NINF, NINF);
+            if (on && e < E) v = *reinterpret_cast<const float4*>(row + e);
             z[i] = v.x; z[i + 1] = v.y; z[i + 2] = v.z; z[i + 3] = v.w;
-            *reinterpret_cast<float4*>(dps + e) = c;
         } else {
-            z[i] = on && e < E ? a.logits[t * E + e] : NINF;
-            dps[e] = on && e < E && a.aux_coef ? a.aux_coef[(int64_t)party * E + e] : 0.f;
+            z[i] = on && e < E ? row[e] : NINF;
         }
     }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) z[i] = z[i] == z[i] ? z[i] : NINF;
     // lane j < k holds pick j
-    const bool has = on && l < k;
-    int pe = has ? a.topk_idx[t * k + l] : 0;
-    float g = has ? a.dtopk_w[t * k + l] : 0.f;
-    bool ok = has;
-    if (has && (pe < 0 || pe >= E)) {
+    int pe = on && l < k ? a.topk_idx[t * k + l] : 0;
+    float g = on && l < k ? a.dtopk_w[t * k + l] : 0.f;
+    bool ok = on && l < k;
+    if (ok && (pe < 0 || pe >= E)) {
         record_status(MOE_ERR_DEVICE_CHECK);
         ok = false;
-        g = 0.f;
-        pe = 0;
     }
-    float pz = ok ? a.logits[t * E + pe] : NINF;
-    pz = pz == pz ? pz : NINF;
-    float m = 0.f, inv = 1.f, s[NV], ps;
-    if constexpr (SIG) {
-        ps = 1.f / (1.f + expf(-pz));
-    } else {
+    g = ok ? g : 0.f;
+    pe = ok ? pe : 0;
+    const float pz = ok ? fmaxf(row[pe], NINF) : NINF;
+    const float pa = ok && aux ? aux[pe] : 0.f;
+    float m = 0.f, inv = 1.f;
+    if constexpr (!SIG) {
         m = NINF;
-        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) m = fmaxf(m, z[i]);
+        for (int i = 0; i < NV; ++i) m = fmaxf(m, z[i]);  // (passes over NaN)
         m = lanes_maxf<LPT>(m);
         m = m == NINF ? 0.f : m;
+        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            s[i] = expf(z[i] - m);
-            sum += s[i];
+            z[i] = fast_exp(fmaxf(z[i] - m, NINF));  // NaN: 0
+            sum += z[i];
         }
         sum = lanes_sum<LPT>(sum);
         inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) s[i] *= inv;
-        ps = expf(pz - m) * inv;
+        for (int i = 0; i < NV; ++i) z[i] *= inv;
     }
+    const float ps = pz > NINF ? score_of<SIG>(pz, m, inv) : 0.f;
     float ds = a.scale * g;
     if (a.normalize) {
         const float total = lanes_sum<8>(ok ? ps : 0.f);
-        const float inner = lanes_sum<8>(ok ? g * (a.scale * ps / total) : 0.f);
-        ds = total == 0.f ? 0.f : (ds - inner) / total;
+        const float inner = lanes_sum<8>(ok ? g * (a.scale * ps) : 0.f);
+        ds = total == 0.f ? 0.f : (ds - inner / total) / total;
     }
-    __syncwarp();
-    if (ok) atomicAdd(&dps[pe], ds);  // the picks of a token differ: one addition per place
-    __syncwarp();
-    float dp[NV], dot = 0.f;
+    float dot = 0.f;
+    float c[NV];
 #pragma unroll
     for (int i = 0; i < NV; i += SP) {
         const int e = i * LPT + l * SP;
         if constexpr (SP == 4) {
-            const float4 v = *reinterpret_cast<const float4*>(dps + e);
-            dp[i] = v.x; dp[i + 1] = v.y; dp[i + 2] = v.z; dp[i + 3] = v.w;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (aux && e < E) v = *reinterpret_cast<const float4*>(aux + e);
+            c[i] = v.x; c[i + 1] = v.y; c[i + 2] = v.z; c[i + 3] = v.w;
         } else {
-            dp[i] = dps[e];
+            c[i] = aux && e < E ? aux[e] : 0.f;
         }
     }
     if constexpr (!SIG) {
+        dot = ok ? ds * ps : 0.f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) dot = fmaf(dp[i], s[i], dot);
+        for (int i = 0; i < NV; ++i) dot = fmaf(c[i], z[i], dot);
         dot = lanes_sum<LPT>(dot);
     }
+    // ds s (1 - s), without the difference's cancellation, or s (ds - <ds, s>)
+    auto grad = [&](float zs, float d) {
+        if constexpr (SIG) {
+            const float q = fast_exp2(fmaxf(-fabsf(zs) * LOG2E, NINF));  // NaN: 0
+            return d * q * fast_rcp((1.f + q) * (1.f + q));
+        } else {
+            return zs * (d - dot);
+        }
+    };
 #pragma unroll
     for (int i = 0; i < NV; i += SP) {
         const int e = i * LPT + l * SP;
         float o[SP];
 #pragma unroll
-        for (int j = 0; j < SP; ++j) {
-            if constexpr (SIG) {  // s (1 - s) without the difference's cancellation
-                const float q = expf(-fabsf(z[i + j]));
-                o[j] = dp[i + j] * q / ((1.f + q) * (1.f + q));
-            } else {
-                o[j] = s[i + j] * (dp[i + j] - dot);
-            }
-        }
+        for (int j = 0; j < SP; ++j) o[j] = grad(z[i + j], c[i + j]);
         if (on && e < E) {
             if constexpr (SP == 4) *reinterpret_cast<float4*>(a.dlogits + t * E + e) = make_float4(o[0], o[1], o[2], o[3]);
             else a.dlogits[t * E + e] = o[0];
@@ -301,6 +533,12 @@ __global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(GateBwdArgs a, __n
     }
     if (on && dz16)
         for (int e = NV * LPT + l; e < EP; e += LPT) dz16[t * EP + e] = __float2bfloat16_rn(0.f);
+    __syncwarp();  // the picks' places are written after the row
+    if (ok) {
+        const float o = grad(SIG ? pz : ps, pa + ds);
+        a.dlogits[t * E + pe] = o;
+        if (dz16) dz16[t * EP + pe] = __float2bfloat16_rn(o);
+    }
 }
 
 // out = in + rate * sign(mean - count), the comparison in whole numbers; one CTA per party
@@ -331,55 +569,60 @@ static int pow2_ceil(int v) {
     return p;
 }
 
-template <int NV, int LPT>
-static cudaError_t launch_gate_t(const GateArgs& a, int lpg, int nv, cudaStream_t s) {
+template <int NV, int LPT, int KT, bool VEC>
+static cudaError_t launch_gate_t(const GateArgs& a, int lpg, cudaStream_t s) {
     constexpr int TPC = GT_THREADS / LPT;
-    // one pass of a CTA per token while that gives no more than eight CTAs per SM, then several
-    int64_t ctas = (a.T + TPC - 1) / TPC;
-    const int64_t most = 8 * (int64_t)sm_count();
-    const int chunk = (int)(ctas <= most ? TPC : (ctas + most - 1) / most * TPC);
-    ctas = (a.T + chunk - 1) / chunk;
+    // all CTAs resident at once, each with as many passes as the others
+    const int64_t passes = (a.T + TPC - 1) / TPC, most = GT_RESIDENT * (int64_t)sm_count();
+    const int chunk = (int)((passes + most - 1) / most * TPC);
+    const int64_t ctas = (a.T + chunk - 1) / chunk;
     const bool whole = ctas == 1 && a.P == 1;  // the counts are this CTA's: stored, not added
     if (!whole) {
-        const cudaError_t e = cudaMemsetAsync(a.counts, 0, sizeof(int32_t) * a.P * a.E, s);
+        (void)launch_pdl(gate_zero_kernel, dim3((a.P * a.E + 255) / 256), dim3(256), 0, s, a.counts, a.P * a.E);
+        const cudaError_t e = cudaGetLastError();
         if (e != cudaSuccess) return e;
     }
     if (a.sigmoid)
-        (void)launch_pdl(gate_kernel<NV, LPT, true>, dim3((unsigned)ctas), dim3(GT_THREADS), 0, s, a, lpg, nv, chunk, whole);
+        (void)launch_pdl(gate_kernel<NV, LPT, KT, VEC, true>, dim3((unsigned)ctas), dim3(GT_THREADS), 0, s, a, lpg, chunk, whole);
     else
-        (void)launch_pdl(gate_kernel<NV, LPT, false>, dim3((unsigned)ctas), dim3(GT_THREADS), 0, s, a, lpg, nv, chunk, whole);
+        (void)launch_pdl(gate_kernel<NV, LPT, KT, VEC, false>, dim3((unsigned)ctas), dim3(GT_THREADS), 0, s, a, lpg, chunk, whole);
     return cudaGetLastError();
 }
 
-// Lanes per token: the fewest (8, 16, 32) that give every group a lane and hold the pool with at most
-// eight scores a lane; 32 lanes hold up to 16 a lane (groups that are no power of two leave lanes idle).
-cudaError_t launch_gate(const GateArgs& a0, cudaStream_t s) {
-    GateArgs a = a0;
+// Lanes per token: the fewest (8, 16, 32) that give every group a lane and hold the pool with at
+// most 16 keys a lane, or 8 while even that leaves every warp resident: fewer lanes a token are fewer
+// instructions, more are a shorter chain of them (E = 256, 8 groups: 65536 tokens 58 us with 16 keys a lane, 76
+// with 8; 2999 tokens 11.7 and 8.6).
+cudaError_t launch_gate(const GateArgs& a, cudaStream_t s) {
     if (a.T == 0) return cudaMemsetAsync(a.counts, 0, sizeof(int32_t) * a.P * a.E, s);
     const int Gp = pow2_ceil(a.groups), gs = a.E / a.groups;
-    int lpt = 8;
-    while (lpt < 32 && (lpt < Gp || (gs + lpt / Gp - 1) / (lpt / Gp) > 8)) lpt *= 2;
+    auto lanes = [&](int keys) {
+        int n = 8;
+        while (n < 32 && (n < Gp || (gs + n / Gp - 1) / (n / Gp) > keys)) n *= 2;
+        return n;
+    };
+    int lpt = lanes(8);
+    if (a.T * lpt / GT_THREADS > GT_RESIDENT * (int64_t)sm_count()) lpt = lanes(16);
     const int lpg = lpt / Gp;
     int nv = (gs + lpg - 1) / lpg;
-    if (nv > 2 && gs % 4 == 0) nv = (nv + 3) / 4 * 4;  // whole 16-byte spans (the last lanes of a group hold fewer)
-    a.vec = nv % 4 == 0 && gs % 4 == 0 && (uintptr_t)a.logits % 16 == 0;
-#define MOE_GATE(NV)                                              \
-    (lpt == 8 ? launch_gate_t<NV, 8>(a, lpg, nv, s)               \
-              : lpt == 16 ? launch_gate_t<NV, 16>(a, lpg, nv, s) : launch_gate_t<NV, 32>(a, lpg, nv, s))
-    if (nv <= 2) return MOE_GATE(2);
-    if (nv <= 4) return MOE_GATE(4);
-    if (nv <= 8) return MOE_GATE(8);
-    return launch_gate_t<16, 32>(a, lpg, nv, s);
+    const bool vec = nv > 2 && gs % 4 == 0 && (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.bias % 16 == 0;
+    if (vec) nv = (gs / 4 + lpg - 1) / lpg * 4;
+#define MOE_GATE_K(NV, LPT, VEC) (a.k <= 2 ? launch_gate_t<NV, LPT, 2, VEC>(a, lpg, s) : launch_gate_t<NV, LPT, 8, VEC>(a, lpg, s))
+#define MOE_GATE(NV, LPT) (vec ? MOE_GATE_K(NV, LPT, true) : MOE_GATE_K(NV, LPT, false))
+    if (lpt == 8) return nv <= 2 ? MOE_GATE_K(2, 8, false) : nv <= 4 ? MOE_GATE(4, 8) : nv <= 8 ? MOE_GATE(8, 8) : MOE_GATE(16, 8);
+    if (lpt == 16) return nv <= 8 ? MOE_GATE(8, 16) : MOE_GATE(16, 16);
+    return nv <= 8 ? MOE_GATE(8, 32) : MOE_GATE(16, 32);
 #undef MOE_GATE
+#undef MOE_GATE_K
 }
 
-template <int NV, int LPT>
+template <int NV>
 static cudaError_t launch_gate_bwd_t(const GateBwdArgs& a, __nv_bfloat16* dz16, int EP, int32_t* chunk_off, int CH, int nchunk,
                                      cudaStream_t s) {
-    const unsigned ctas = (unsigned)((a.T + GT_THREADS / LPT - 1) / (GT_THREADS / LPT));
+    const unsigned ctas = (unsigned)((a.T + GT_THREADS / GB_LPT - 1) / (GT_THREADS / GB_LPT));
     const bool vec = a.E % 4 == 0 && (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.dlogits % 16 == 0 && (uintptr_t)a.aux_coef % 16 == 0;
 #define MOE_GB(SP, SIG)                                                                                                        \
-    (void)launch_pdl(gate_bwd_kernel<NV, LPT, SP, SIG>, dim3(ctas), dim3(GT_THREADS), 0, s, a, dz16, EP, chunk_off, CH, nchunk)
+    (void)launch_pdl(gate_bwd_kernel<NV, SP, SIG>, dim3(ctas), dim3(GT_THREADS), 0, s, a, dz16, EP, chunk_off, CH, nchunk)
     if (a.sigmoid) {
         if (vec) MOE_GB(4, true);
         else MOE_GB(1, true);
@@ -392,10 +635,10 @@ static cudaError_t launch_gate_bwd_t(const GateBwdArgs& a, __nv_bfloat16* dz16, 
 }
 
 cudaError_t launch_gate_bwd(const GateBwdArgs& a, __nv_bfloat16* dz16, int EP, int32_t* chunk_off, int CH, int nchunk, cudaStream_t s) {
-    if (a.E <= 32) return launch_gate_bwd_t<4, 8>(a, dz16, EP, chunk_off, CH, nchunk, s);
-    if (a.E <= 64) return launch_gate_bwd_t<8, 8>(a, dz16, EP, chunk_off, CH, nchunk, s);
-    if (a.E <= 128) return launch_gate_bwd_t<8, 16>(a, dz16, EP, chunk_off, CH, nchunk, s);
-    return launch_gate_bwd_t<8, 32>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    if (a.E <= 32) return launch_gate_bwd_t<4>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    if (a.E <= 64) return launch_gate_bwd_t<8>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    if (a.E <= 128) return launch_gate_bwd_t<16>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    return launch_gate_bwd_t<32>(a, dz16, EP, chunk_off, CH, nchunk, s);
 }
 
 cudaError_t launch_gate_balance(const int32_t* counts, int P, int E, float rate, const float* in, float* out, cudaStream_t s) {

@@ -56,7 +56,6 @@ struct GateArgs {
     int32_t* topk_idx;
     float* topk_w;
     int32_t* counts;  // [P,E]
-    bool vec;         // set by the launcher: 16-byte loads
 };
 struct GateBwdArgs {
     const float* logits;

@@ -105,14 +105,17 @@ __device__ __forceinline__ float sum_margin(float a, float b) { return fmaf(fabs
 
 // Keys for sorting: the distance of a key below the largest, in units of KEY_RANGE / 2^23 up to KEY_RANGE
 // (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
-// the top down, and bit 31; an expert's 255 - id below. Two keys of the exact order can come out the other way
-// round only within KEY_SURE: 4 units of the fast sigmoid's error, 3 of the roundings here.
-template <bool SIG> __device__ __forceinline__ uint32_t sort_key(float key, float most, int id) {
+// the top down, and bit 31; an expert's 255 - id below, so that equal ones come in the order of their ids. Two
+// keys of the exact order can come out the other way round only within KEY_SURE: 4 units of the fast sigmoid's
+// error, 3 of the roundings here. FLOOR: no finite key in the lowest 16 units, which are left to those out of reach.
+template <bool SIG, bool FLOOR> __device__ __forceinline__ uint32_t sort_key(float key, float most, int id) {
     constexpr float RANGE = SIG ? 2.f : 16.f;
-    const float t = __saturatef(fmaf(key - most, 1.f / RANGE, 1.f));
-    return __byte_perm(__float_as_uint(fmaf(t, 16777214.f, 16777216.f)), (uint32_t)(255 - id), 0x2104);
+    float t = __saturatef(fmaf(key - most, 1.f / RANGE, 1.f));
+    if (FLOOR) t = fmaxf(t, 0x1p-19f);
+    return __float_as_uint(fmaf(t, 16777214.f, 16777216.f)) * 256u + (uint32_t)(255 - id);
 }
 constexpr uint32_t KEY_SURE = 9u << 8;
+constexpr uint32_t KEY_OUT = 0x80000000u;  // a key out of reach, with its 255 - id
 
 // Where a lane's slots lie in its group, in spans of 4 (VEC) or single places, the group's lanes in turn
 template <bool VEC> struct Slots {
@@ -243,6 +246,11 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
         const float* bias = a.bias ? a.bias + (int64_t)party * E + first : nullptr;
         float key[NV], m = 0.f, inv = 1.f;
         slots.template load<NV>(row, on, NINF, key);
+        // whether every slot of the warp holds an expert within reach: no test of single ones then
+        float zero = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) zero = fmaf(key[i], 0.f, zero);  // NaN with an infinity or a NaN
+        const bool clean = __all_sync(0xffffffffu, slots.cnt == NV && zero == 0.f);
         if constexpr (!SIG) {
             m = NINF;
 #pragma unroll
@@ -264,12 +272,20 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
         {
             float b[NV];
             if (bias) slots.template load<NV>(bias, true, 0.f, b);
+            if (clean) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const bool reach = key[i] > NINF;  // (a NaN is out of reach)
-                if constexpr (SIG) key[i] = fast_rcp(1.f + fast_exp(-key[i]));
-                if (bias) key[i] += b[i];
-                key[i] = reach ? key[i] : NINF;
+                for (int i = 0; i < NV; ++i) {
+                    if constexpr (SIG) key[i] = fast_rcp(1.f + fast_exp(-key[i]));
+                    if (bias) key[i] += b[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const bool reach = key[i] > NINF;  // (a NaN is out of reach)
+                    if constexpr (SIG) key[i] = fast_rcp(1.f + fast_exp(-key[i]));
+                    if (bias) key[i] += b[i];
+                    key[i] = reach ? key[i] : NINF;
+                }
             }
         }
         bool kept = true;
@@ -288,7 +304,7 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
                 for (int g = 0; g < a.groups; ++g) {
                     const float other = __shfl_sync(0xffffffffu, mine, base + g * lpg);
                     rank += other > mine || (other == mine && g < grp);
-                    sure &= g == grp || fabsf(other - mine) > margin;  // (not so for two of -inf)
+                    sure &= g == grp || fabsf(other - mine) > margin || (other == mine && mine == NINF);
                 }
                 kept = rank < a.top_groups;
                 // exact keys in their place, and once more, where two groups are too close
@@ -307,9 +323,18 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
 #pragma unroll
         for (int i = 1; i < NV; ++i) most = fmaxf(most, key[i]);
         most = fmaxf(lanes_maxf<LPT>(most), -3.4e38f);
-        uint32_t u[NV];  // 0 where there is nothing to pick
+        uint32_t u[NV];  // 0 where there is no expert
+        if (clean) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) u[i] = kept && i < slots.cnt ? sort_key<SIG>(key[i], most, first + slots.at(i)) : 0u;
+            for (int i = 0; i < NV; ++i) u[i] = sort_key<SIG, false>(key[i], most, first + slots.at(i));
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int id = first + slots.at(i);
+                u[i] = key[i] > NINF ? sort_key<SIG, true>(key[i], most, id) : KEY_OUT + (uint32_t)(255 - id);
+                if (i >= slots.cnt) u[i] = 0u;
+            }
+        }
         uint32_t v[KT];
 #pragma unroll
         for (int i = 0; i < KT; ++i) v[i] = i < NV ? u[i] : 0u;
@@ -322,6 +347,10 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
             sort_any<KT>(w);
             merge_top<KT>(v, w);
         }
+        if (a.top_groups < a.groups) {
+#pragma unroll
+            for (int i = 0; i < KT; ++i) v[i] = kept ? v[i] : 0u;
+        }
 #pragma unroll
         for (int o = 1; o < LPT; o <<= 1) {
             uint32_t w[KT];
@@ -329,24 +358,27 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
             for (int i = 0; i < KT; ++i) w[i] = __shfl_xor_sync(0xffffffffu, v[i], o);
             merge_top<KT>(v, w);
         }
-        // Sure where each of the k largest is clear of the next, and the last of all others, by their count
+        // Sure where each of the k largest is clear of the next, and the last of all others, by their count; keys out
+        // of reach are equal, and in the order of their ids
         uint32_t mine = v[0], last = v[0];
         bool sure = true;
 #pragma unroll
         for (int i = 1; i < KT; ++i) {
             if (i < k) {
-                sure &= last - v[i] >= KEY_SURE;
+                sure &= last - v[i] >= KEY_SURE || (!clean && last < KEY_OUT + 256);
                 last = v[i];
                 mine = l == i ? v[i] : mine;
             }
         }
+        const bool out = !clean && last < KEY_OUT + 256;
         last -= KEY_SURE;
         int n = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) n += u[i] >= last;
+        n = kept ? n : 0;
 #pragma unroll
         for (int o = 1; o < LPT; o <<= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
-        sure &= n == k;
+        sure &= n == k || out;
         int pe = 255 - (int)(mine & 0xffu);
         if (__any_sync(0xffffffffu, on && !sure)) {
             // the few that are not clear of the k largest, by exact keys against each other
@@ -357,7 +389,7 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
                 uint32_t ui = 0;
 #pragma unroll
                 for (int j = 0; j < NV; ++j) ui = i == j ? u[j] : ui;
-                if (ui >= last && n <= GT_CAND) cand.id[atomicAdd(&cand.n, 1)] = 255 - (int)(ui & 0xffu);
+                if (kept && ui >= last && n <= GT_CAND) cand.id[atomicAdd(&cand.n, 1)] = 255 - (int)(ui & 0xffu);
             }
             __syncwarp();
             if (on && n <= GT_CAND) {

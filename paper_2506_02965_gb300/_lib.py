@@ -297,24 +297,40 @@ def moe_dispatch_bwd(cfg, dx_perm, slot_of, dx_router, dx_sh, dx, stream=None):
 
 # ------------------------------------------------------------------ operators around the layer
 # These also check what a tensor is before its address is taken: on the GPU, dense, of the right
-# element type and as many elements as the call's sizes say.
-_TORCH_TYPES = {}
+# element type and as many elements as the call's sizes say. The kinds: MOE_F32, MOE_BF16 and
+_I32T, _I8T = 2, 3
+_kinds = None
 
 
-def _types():
-    import torch
-    _TORCH_TYPES.update({MOE_F32: torch.float32, MOE_BF16: torch.bfloat16, "f32": torch.float32, "i32": torch.int32, "i8": torch.int8})
-    return _TORCH_TYPES
+def _check_arr(fn, name, t, kind, n):
+    """Address of a dense GPU tensor of n elements of `kind`; an address or None as it is."""
+    if t is None or type(t) is int:
+        return t
+    global _kinds
+    if _kinds is None:
+        import torch
+        _kinds = (torch.float32, torch.bfloat16, torch.int32, torch.int8)
+    if t.numel() == n and t.is_cuda and t.is_contiguous() and t.dtype is _kinds[kind]:
+        return t.data_ptr()
+    raise MoEError(MOE_ERR_INVALID_ARG, fn, f"{name}: expected a dense GPU tensor of {n} elements of {_kinds[kind]}, got "
+                                            f"{tuple(t.shape)} {t.dtype}, strides {t.stride()}, on {t.device}")
 
 
 def _arr(fn, name, t, kind, n):
-    """Address of a dense GPU tensor of n elements of `kind` (a moe_dtype, "f32", "i32" or "i8")."""
+    """_check_arr; from the first tensor on in C++ (csrc/marshal.cpp), where that is built for this torch."""
+    global _arr
     if t is None or type(t) is int:
         return t
-    if t.numel() == n and t.is_cuda and t.is_contiguous() and t.dtype is (_TORCH_TYPES or _types())[kind]:
-        return t.data_ptr()
-    raise MoEError(MOE_ERR_INVALID_ARG, fn, f"{name}: expected a dense GPU tensor of {n} elements of {_types()[kind]}, got "
-                                            f"{tuple(t.shape)} {t.dtype}, strides {t.stride()}, on {t.device}")
+    import torch  # noqa: F401  (whose libraries the module links against)
+    from importlib import machinery, util
+    try:
+        spec = util.spec_from_loader("_marshal", machinery.ExtensionFileLoader("_marshal", os.path.join(HERE, "_marshal.so")))
+        m = util.module_from_spec(spec)
+        m.set_slow(_check_arr)
+        _arr = m.addr
+    except (ImportError, OSError):
+        _arr = _check_arr
+    return _arr(fn, name, t, kind, n)
 
 
 def _dtype_of(fn, dtype):
@@ -334,10 +350,10 @@ def make_gate_rule(score=MOE_SCORE_SOFTMAX, n_groups=1, top_groups=1, group_top=
 
 def _gate_arrays(fn, cfg, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts):
     T, E, k, Pn = cfg.T, cfg.n_experts, cfg.top_k, cfg.n_parties
-    return (_arr(fn, "logits", logits, "f32", T * E), _arr(fn, "balance_bias", balance_bias, "f32", Pn * E),
-            _arr(fn, "party_offsets", party_offsets, "i32", Pn + 1), _arr(fn, "scores", scores, "f32", T * E),
-            _arr(fn, "topk_idx", topk_idx, "i32", T * k), _arr(fn, "topk_w", topk_w, "f32", T * k),
-            _arr(fn, "counts", counts, "i32", Pn * E))
+    return (_arr(fn, "logits", logits, MOE_F32, T * E), _arr(fn, "balance_bias", balance_bias, MOE_F32, Pn * E),
+            _arr(fn, "party_offsets", party_offsets, _I32T, Pn + 1), _arr(fn, "scores", scores, MOE_F32, T * E),
+            _arr(fn, "topk_idx", topk_idx, _I32T, T * k), _arr(fn, "topk_w", topk_w, MOE_F32, T * k),
+            _arr(fn, "counts", counts, _I32T, Pn * E))
 
 
 def moe_gate(cfg, rule, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts, stream=None):
@@ -353,7 +369,7 @@ def moe_route_gate(cfg, rule, x, w_router, router_bias, balance_bias, party_offs
         fn, cfg, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts)
     dt = _dtype_of(fn, cfg.dtype)
     _check(_lib.moe_route_gate(cfg, rule, _arr(fn, "x", x, dt, T * d), _arr(fn, "w_router", w_router, dt, Pn * E * d),
-                               _arr(fn, "router_bias", router_bias, "f32", Pn * E), balance_bias, party_offsets, logits, scores,
+                               _arr(fn, "router_bias", router_bias, MOE_F32, Pn * E), balance_bias, party_offsets, logits, scores,
                                topk_idx, topk_w, counts, _stream(stream)), fn)
 
 
@@ -362,19 +378,19 @@ def moe_gate_bwd(cfg, rule, logits, topk_idx, dtopk_w, aux_coef, party_offsets, 
     fn = "moe_gate_bwd"
     T, E, d, k, Pn = cfg.T, cfg.n_experts, cfg.d_model, cfg.top_k, cfg.n_parties
     dt = _dtype_of(fn, cfg.dtype)
-    _check(_lib.moe_gate_bwd(cfg, rule, _arr(fn, "logits", logits, "f32", T * E), _arr(fn, "topk_idx", topk_idx, "i32", T * k),
-                             _arr(fn, "dtopk_w", dtopk_w, "f32", T * k), _arr(fn, "aux_coef", aux_coef, "f32", Pn * E),
-                             _arr(fn, "party_offsets", party_offsets, "i32", Pn + 1), _arr(fn, "dlogits", dlogits, "f32", T * E),
+    _check(_lib.moe_gate_bwd(cfg, rule, _arr(fn, "logits", logits, MOE_F32, T * E), _arr(fn, "topk_idx", topk_idx, _I32T, T * k),
+                             _arr(fn, "dtopk_w", dtopk_w, MOE_F32, T * k), _arr(fn, "aux_coef", aux_coef, MOE_F32, Pn * E),
+                             _arr(fn, "party_offsets", party_offsets, _I32T, Pn + 1), _arr(fn, "dlogits", dlogits, MOE_F32, T * E),
                              _arr(fn, "x", x, dt, T * d), _arr(fn, "w_router", w_router, dt, Pn * E * d),
-                             _arr(fn, "dw_router", dw_router, dt, Pn * E * d), _arr(fn, "dbias", dbias, "f32", Pn * E),
+                             _arr(fn, "dw_router", dw_router, dt, Pn * E * d), _arr(fn, "dbias", dbias, MOE_F32, Pn * E),
                              _arr(fn, "dx_router", dx_router, dt, T * d), _ptr(workspace), int(workspace_bytes),
                              _stream(stream)), fn)
 
 
 def moe_gate_balance(cfg, counts, rate, bias_in, bias_out, stream=None):
     fn, n = "moe_gate_balance", cfg.n_parties * cfg.n_experts
-    _check(_lib.moe_gate_balance(cfg, _arr(fn, "counts", counts, "i32", n), rate, _arr(fn, "bias_in", bias_in, "f32", n),
-                                 _arr(fn, "bias_out", bias_out, "f32", n), _stream(stream)), fn)
+    _check(_lib.moe_gate_balance(cfg, _arr(fn, "counts", counts, _I32T, n), rate, _arr(fn, "bias_in", bias_in, MOE_F32, n),
+                                 _arr(fn, "bias_out", bias_out, MOE_F32, n), _stream(stream)), fn)
 
 
 def moe_layer_norm_workspace_size(rows, d) -> int:
@@ -388,44 +404,44 @@ def moe_layer_norm_fwd(rows, d, dtype, x, residual, gamma, beta, eps, h, y, mean
     fn, n = "moe_layer_norm_fwd", rows * d
     dt = _dtype_of(fn, dtype)
     _check(_lib.moe_layer_norm_fwd(rows, d, dt, _arr(fn, "x", x, dt, n), _arr(fn, "residual", residual, dt, n),
-                                   _arr(fn, "gamma", gamma, "f32", d), _arr(fn, "beta", beta, "f32", d), eps,
-                                   _arr(fn, "h", h, dt, n), _arr(fn, "y", y, dt, n), _arr(fn, "mean", mean, "f32", rows),
-                                   _arr(fn, "rstd", rstd, "f32", rows), _arr(fn, "h_q", h_q, "i8", n),
-                                   _arr(fn, "h_scale", h_scale, "f32", rows * ckpt_blocks(d)), _stream(stream)), fn)
+                                   _arr(fn, "gamma", gamma, MOE_F32, d), _arr(fn, "beta", beta, MOE_F32, d), eps,
+                                   _arr(fn, "h", h, dt, n), _arr(fn, "y", y, dt, n), _arr(fn, "mean", mean, MOE_F32, rows),
+                                   _arr(fn, "rstd", rstd, MOE_F32, rows), _arr(fn, "h_q", h_q, _I8T, n),
+                                   _arr(fn, "h_scale", h_scale, MOE_F32, rows * ckpt_blocks(d)), _stream(stream)), fn)
 
 
 def moe_layer_norm_bwd(rows, d, dtype, dy, h, h_q, h_scale, mean, rstd, gamma, dh, dx, dgamma, dbeta, workspace,
                        workspace_bytes, stream=None):
     fn, n = "moe_layer_norm_bwd", rows * d
     dt = _dtype_of(fn, dtype)
-    _check(_lib.moe_layer_norm_bwd(rows, d, dt, _arr(fn, "dy", dy, dt, n), _arr(fn, "h", h, dt, n), _arr(fn, "h_q", h_q, "i8", n),
-                                   _arr(fn, "h_scale", h_scale, "f32", rows * ckpt_blocks(d)), _arr(fn, "mean", mean, "f32", rows),
-                                   _arr(fn, "rstd", rstd, "f32", rows), _arr(fn, "gamma", gamma, "f32", d),
-                                   _arr(fn, "dh", dh, dt, n), _arr(fn, "dx", dx, dt, n), _arr(fn, "dgamma", dgamma, "f32", d),
-                                   _arr(fn, "dbeta", dbeta, "f32", d), _ptr(workspace), int(workspace_bytes),
+    _check(_lib.moe_layer_norm_bwd(rows, d, dt, _arr(fn, "dy", dy, dt, n), _arr(fn, "h", h, dt, n), _arr(fn, "h_q", h_q, _I8T, n),
+                                   _arr(fn, "h_scale", h_scale, MOE_F32, rows * ckpt_blocks(d)), _arr(fn, "mean", mean, MOE_F32, rows),
+                                   _arr(fn, "rstd", rstd, MOE_F32, rows), _arr(fn, "gamma", gamma, MOE_F32, d),
+                                   _arr(fn, "dh", dh, dt, n), _arr(fn, "dx", dx, dt, n), _arr(fn, "dgamma", dgamma, MOE_F32, d),
+                                   _arr(fn, "dbeta", dbeta, MOE_F32, d), _ptr(workspace), int(workspace_bytes),
                                    _stream(stream)), fn)
 
 
 def moe_ckpt_pack(rows, cols, dtype, x, q, scale, stream=None):
     fn, n = "moe_ckpt_pack", rows * cols
     dt = _dtype_of(fn, dtype)
-    _check(_lib.moe_ckpt_pack(rows, cols, dt, _arr(fn, "x", x, dt, n), _arr(fn, "q", q, "i8", n),
-                              _arr(fn, "scale", scale, "f32", rows * ckpt_blocks(cols)), _stream(stream)), fn)
+    _check(_lib.moe_ckpt_pack(rows, cols, dt, _arr(fn, "x", x, dt, n), _arr(fn, "q", q, _I8T, n),
+                              _arr(fn, "scale", scale, MOE_F32, rows * ckpt_blocks(cols)), _stream(stream)), fn)
 
 
 def moe_ckpt_unpack(rows, cols, dtype, q, scale, x, stream=None):
     fn, n = "moe_ckpt_unpack", rows * cols
     dt = _dtype_of(fn, dtype)
-    _check(_lib.moe_ckpt_unpack(rows, cols, dt, _arr(fn, "q", q, "i8", n),
-                                _arr(fn, "scale", scale, "f32", rows * ckpt_blocks(cols)), _arr(fn, "x", x, dt, n),
+    _check(_lib.moe_ckpt_unpack(rows, cols, dt, _arr(fn, "q", q, _I8T, n),
+                                _arr(fn, "scale", scale, MOE_F32, rows * ckpt_blocks(cols)), _arr(fn, "x", x, dt, n),
                                 _stream(stream)), fn)
 
 
 def moe_ckpt_swiglu_bwd(rows, d_ff, dtype, q, scale, dact, act, dh, stream=None):
     fn, n = "moe_ckpt_swiglu_bwd", rows * d_ff
     dt = _dtype_of(fn, dtype)
-    _check(_lib.moe_ckpt_swiglu_bwd(rows, d_ff, dt, _arr(fn, "q", q, "i8", 2 * n),
-                                    _arr(fn, "scale", scale, "f32", rows * ckpt_blocks(2 * d_ff)),
+    _check(_lib.moe_ckpt_swiglu_bwd(rows, d_ff, dt, _arr(fn, "q", q, _I8T, 2 * n),
+                                    _arr(fn, "scale", scale, MOE_F32, rows * ckpt_blocks(2 * d_ff)),
                                     _arr(fn, "dact", dact, dt, n), _arr(fn, "act", act, dt, n), _arr(fn, "dh", dh, dt, 2 * n),
                                     _stream(stream)), fn)
 

@@ -3,13 +3,17 @@
 Each translation unit under ``csrc/`` is compiled in parallel to an object file
 (``-gencode arch=compute_103a,code=sm_103a``), then linked into a shared library
 next to this file. Rebuilds only what changed (source or header newer than object).
+Beside it the binding's argument checks (``csrc/marshal.cpp``, host C++ on torch's headers) become
+``_marshal.so``, without which the binding makes the same checks in Python.
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -30,6 +34,21 @@ def nvcc() -> str:
         if cand and os.path.exists(cand):
             return cand
     raise RuntimeError("nvcc not found: the CUDA library cannot be built")
+
+
+MARSHAL_SRC, MARSHAL = os.path.join(CSRC, "marshal.cpp"), os.path.join(HERE, "_marshal.so")
+
+
+def _marshal_cmd():
+    """The command that builds _marshal.so; None without torch or a host compiler."""
+    spec, cxx = importlib.util.find_spec("torch"), os.environ.get("CXX") or shutil.which("g++") or shutil.which("c++")
+    if spec is None or not spec.origin or not cxx:
+        return None
+    torch = os.path.dirname(spec.origin)
+    inc = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+           sysconfig.get_paths()["include"]]
+    return [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", *["-I" + i for i in inc], "-L" + os.path.join(torch, "lib"), MARSHAL_SRC,
+            "-o", MARSHAL, "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
 def _stale(obj: str, src: str) -> bool:
@@ -56,12 +75,18 @@ def build(verbose: bool = False, extra: list[str] | None = None) -> str:
         r = subprocess.run(cmd, capture_output=True, text=True)
         return cmd, r
 
-    with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 4)) as ex:
+    marshal = None
+    if not os.path.exists(MARSHAL) or os.path.getmtime(MARSHAL_SRC) > os.path.getmtime(MARSHAL):
+        marshal = _marshal_cmd()
+    with ThreadPoolExecutor(max_workers=min(len(SOURCES) + 1, os.cpu_count() or 4)) as ex:
+        aside = ex.submit(run, marshal) if marshal else None
         for cmd, r in ex.map(run, jobs):
             if verbose or r.returncode:
                 sys.stderr.write(" ".join(cmd[-3:]) + "\n" + r.stdout + r.stderr)
             if r.returncode:
                 raise RuntimeError(f"nvcc failed on {cmd[-3]}")
+        if aside is not None and aside.result()[1].returncode:
+            sys.stderr.write("_marshal.so was not built (the binding checks its arguments in Python):\n" + aside.result()[1].stderr[-2000:])
     objs = [os.path.join(BUILD, s.replace(".cu", ".o")) for s in SOURCES]
     if jobs or not os.path.exists(LIB):
         cmd = [cc, *ARCH, "-shared", "-o", LIB, *objs, "-cudart=static"]

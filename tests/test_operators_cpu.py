@@ -114,3 +114,17 @@ def test_tensors_are_looked_at():
 def test_rule_struct_layout():
     assert ctypes.sizeof(L.moe_gate_rule) == 20
     assert [f[0] for f in L.moe_gate_rule._fields_] == ["score", "n_groups", "top_groups", "group_top", "scale"]
+
+
+def test_argument_checks_in_both_languages():
+    """The C++ form of the checks, where it is built, refuses what the Python form refuses, with its words."""
+    torch = pytest.importorskip("torch")
+    x = torch.zeros(4, 8)
+    assert L._arr("f", "x", None, L.MOE_F32, 32) is None and L._arr("f", "x", 48, L.MOE_F32, 32) == 48
+    for bad in (x, x.bool(), x.t(), torch.sparse_coo_tensor(size=(4, 8)), torch.empty(4, 8, device="meta")):
+        said = []
+        for check in (L._arr, L._check_arr):
+            with pytest.raises(Exception) as e:
+                check("f", "x", bad, L.MOE_F32, 32)
+            said.append((type(e.value), str(e.value)))
+        assert said[0] == said[1]

@@ -21,7 +21,7 @@
 namespace moe {
 
 constexpr int GT_THREADS = 256;
-constexpr int GT_RESIDENT = 3;  // CTAs per SM (65536 tokens, E = 256, 8 groups: 54.6 us; 4: 59.3, 5: 66.6, whose registers spill)
+constexpr int GT_RESIDENT = 3;  // CTAs per SM (65536 tokens, E = 256, 8 groups: 48.1 us; with 4, whose registers spill, 52.4)
 
 template <int LPT> __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
@@ -77,6 +77,12 @@ template <int N> __device__ __forceinline__ void merge_top(uint32_t* a, const ui
     for (int i = 0; i < N; ++i) a[i] = max(a[i], b[N - 1 - i]);
     sort_bitonic<N>(a);
 }
+// a <- the N largest of two sorted lists, sorted; `rest`: the largest of the others, if that is larger
+template <int N> __device__ __forceinline__ void merge_top(uint32_t* a, const uint32_t* b, uint32_t& rest) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) rest = max(rest, min(a[i], b[N - 1 - i]));
+    merge_top<N>(a, b);
+}
 
 // Score of one logit: softmax with the row's largest m and 1 / sum, or sigmoid.
 template <bool SIG> __device__ __forceinline__ float score_of(float z, float m, float inv) {
@@ -98,24 +104,22 @@ constexpr float LOG2E = 1.4426950408889634f;
 // exp(x), off by 2^-22 + |x| 2^-24 of the result
 __device__ __forceinline__ float fast_exp(float x) { return fast_exp2(x * LOG2E); }
 
-// How far two groups' keys, sums of up to two keys, have to be apart for their order to be sure. A fast sigmoid is off
-// by s (1 - s) (2^-22 + |z| 2^-24) + 2^-23 < 2.5e-7 and the exact one by as much, a sum with a bias by 2^-24 of
-// itself on both sides.
-__device__ __forceinline__ float sum_margin(float a, float b) { return fmaf(fabsf(a) + fabsf(b), 5e-7f, 2.4e-6f); }
-
-// Keys for sorting: the distance of a key below the largest, in units of KEY_RANGE / 2^23 up to KEY_RANGE
-// (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
+// Keys for sorting: the distance of a key below `top` (no key is above it), in units of KEY_RANGE / 2^23 up to
+// KEY_RANGE (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
 // the top down, and bit 31; an expert's 255 - id below, so that equal ones come in the order of their ids. Two
-// keys of the exact order can come out the other way round only within KEY_SURE: 4 units of the fast sigmoid's
-// error, 3 of the roundings here. FLOOR: no finite key in the lowest 16 units, which are left to those out of reach.
-template <bool SIG, bool FLOOR> __device__ __forceinline__ uint32_t sort_key(float key, float most, int id) {
+// keys of the exact order can come out the other way round only within KEY_SURE: a fast sigmoid is off by
+// s (1 - s) (2^-22 + |z| 2^-24) + 2^-23 < 2.5e-7, a unit, and the exact one by half of that, the sums with the
+// bias by 2^-24 of themselves on both sides; the roundings here are 3 units. (Keys past the range come out equal, and so not
+// sure.) FLOOR: no finite key in the lowest 16 units, which are left to those out of reach.
+template <bool SIG, bool FLOOR> __device__ __forceinline__ uint32_t sort_key(float key, float top, int id) {
     constexpr float RANGE = SIG ? 2.f : 16.f;
-    float t = __saturatef(fmaf(key - most, 1.f / RANGE, 1.f));
+    float t = __saturatef(fmaf(key - top, 1.f / RANGE, 1.f));
     if (FLOOR) t = fmaxf(t, 0x1p-19f);
     return __float_as_uint(fmaf(t, 16777214.f, 16777216.f)) * 256u + (uint32_t)(255 - id);
 }
 constexpr uint32_t KEY_SURE = 9u << 8;
 constexpr uint32_t KEY_OUT = 0x80000000u;  // a key out of reach, with its 255 - id
+__device__ __forceinline__ int key_units(uint32_t u) { return (int)(u >> 8) & 0x7fffff; }
 
 // Where a lane's slots lie in its group, in spans of 4 (VEC) or single places, the group's lanes in turn
 template <bool VEC> struct Slots {
@@ -237,6 +241,8 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
     const int p0 = party_of(a.po, a.P, t0);
     for (int e = threadIdx.x; e < E; e += GT_THREADS) hist[e] = 0;
     __syncthreads();
+    int key_party = -1;
+    float most_key = 1.f;
     // whole warps stay in the loop together: a token past the end computes nothing that is written
     for (int64_t tw = t0 + (threadIdx.x / 32) * TPW; tw < t1; tw += TPC) {
         const int64_t t = tw + lane / LPT;
@@ -271,7 +277,16 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
         }
         {
             float b[NV];
-            if (bias) slots.template load<NV>(bias, true, 0.f, b);
+            if (bias) {
+                slots.template load<NV>(bias, true, NINF, b);
+                if (SIG && __any_sync(0xffffffffu, party != key_party)) {  // the most a key of this party can be
+                    key_party = party;
+                    most_key = b[0];
+#pragma unroll
+                    for (int i = 1; i < NV; ++i) most_key = fmaxf(most_key, b[i]);
+                    most_key = 1.f + lanes_maxf<LPT>(most_key);
+                }
+            }
             if (clean) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
@@ -288,69 +303,82 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
                 }
             }
         }
+        float top = bias ? most_key : 1.f;
+        if constexpr (!SIG) {
+            top = key[0];
+#pragma unroll
+            for (int i = 1; i < NV; ++i) top = fmaxf(top, key[i]);
+            top = lanes_maxf<LPT>(top);
+        }
+        top = fmaxf(top, -3.4e38f);
+        // the lane's KT largest, sorted, and the largest of its others; 0 where there is no expert
+        uint32_t v[KT], rest = 0;
+        {
+            uint32_t u[NV];
+            if (clean) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) u[i] = sort_key<SIG, false>(key[i], top, first + slots.at(i));
+            } else {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int id = first + slots.at(i);
+                    u[i] = key[i] > NINF ? sort_key<SIG, true>(key[i], top, id) : KEY_OUT + (uint32_t)(255 - id);
+                    if (i >= slots.cnt) u[i] = 0u;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < KT; ++i) v[i] = i < NV ? u[i] : 0u;
+            sort_any<KT>(v);
+#pragma unroll
+            for (int c = KT; c < NV; c += KT) {
+                uint32_t w[KT];
+#pragma unroll
+                for (int i = 0; i < KT; ++i) w[i] = u[c + i];
+                sort_any<KT>(w);
+                merge_top<KT>(v, w, rest);
+            }
+        }
         bool kept = true;
         if (a.top_groups < a.groups) {
-            bool sure = true;
-            for (int pass = 0; pass < 2; ++pass) {
-                float b1 = NINF, b2 = NINF;
+            // groups by the units of their best keys, 0 for one out of reach
+            uint32_t b1 = v[0], b2 = v[1];
+            group_best(b1, b2, lpg);
+            const int n1 = key_units(b1), n2 = a.group_top == 2 ? key_units(b2) : n1;
+            const int mine = !clean && min(n1, n2) == 0 ? 0 : 1 + n1 + (a.group_top == 2 ? n2 : 0);
+            bool sure = mine == 0 || min(n1, n2) >= 32;  // (not at the end of the range)
+            int rank = 0;
+            for (int g = 0; g < a.groups; ++g) {
+                const int other = __shfl_sync(0xffffffffu, mine, base + g * lpg);
+                rank += other > mine || (other == mine && g < grp);
+                sure &= g == grp || abs(other - mine) > 2 * (int)(KEY_SURE >> 8) || (mine == 0 && other == 0);
+            }
+            if (__any_sync(0xffffffffu, on && !sure && grp < a.groups)) {  // two groups too close: by exact keys
+                float z[NV], c1 = NINF, c2 = NINF;
+                slots.template load<NV>(row, on, NINF, z);
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    b2 = fmaxf(b2, fminf(b1, key[i]));
-                    b1 = fmaxf(b1, key[i]);
+                    float x = SIG ? score_of<true>(z[i], 0.f, 1.f) : z[i];
+                    if (bias && i < slots.cnt) x = __fadd_rn(x, bias[slots.at(i)]);
+                    x = z[i] > NINF ? x : NINF;
+                    c2 = fmaxf(c2, fminf(c1, x));
+                    c1 = fmaxf(c1, x);
                 }
-                group_best(b1, b2, lpg);
-                const float mine = a.group_top == 2 ? b1 + b2 : b1, margin = sum_margin(b1, a.group_top == 2 ? b2 : 0.f);
-                int rank = 0;
+                group_best(c1, c2, lpg);
+                const float sum = a.group_top == 2 ? c1 + c2 : c1;
+                rank = 0;
                 for (int g = 0; g < a.groups; ++g) {
-                    const float other = __shfl_sync(0xffffffffu, mine, base + g * lpg);
-                    rank += other > mine || (other == mine && g < grp);
-                    sure &= g == grp || fabsf(other - mine) > margin || (other == mine && mine == NINF);
-                }
-                kept = rank < a.top_groups;
-                // exact keys in their place, and once more, where two groups are too close
-                if (pass == 1 || !__any_sync(0xffffffffu, on && !sure && grp < a.groups)) break;
-                slots.template load<NV>(row, on, NINF, key);
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const bool reach = key[i] > NINF;
-                    if constexpr (SIG) key[i] = score_of<true>(key[i], 0.f, 1.f);
-                    if (bias && i < slots.cnt) key[i] = __fadd_rn(key[i], bias[slots.at(i)]);
-                    key[i] = reach ? key[i] : NINF;
+                    const float other = __shfl_sync(0xffffffffu, sum, base + g * lpg);
+                    rank += other > sum || (other == sum && g < grp);
                 }
             }
-        }
-        float most = key[0];
-#pragma unroll
-        for (int i = 1; i < NV; ++i) most = fmaxf(most, key[i]);
-        most = fmaxf(lanes_maxf<LPT>(most), -3.4e38f);
-        uint32_t u[NV];  // 0 where there is no expert
-        if (clean) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) u[i] = sort_key<SIG, false>(key[i], most, first + slots.at(i));
-        } else {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int id = first + slots.at(i);
-                u[i] = key[i] > NINF ? sort_key<SIG, true>(key[i], most, id) : KEY_OUT + (uint32_t)(255 - id);
-                if (i >= slots.cnt) u[i] = 0u;
-            }
-        }
-        uint32_t v[KT];
-#pragma unroll
-        for (int i = 0; i < KT; ++i) v[i] = i < NV ? u[i] : 0u;
-        sort_any<KT>(v);
-#pragma unroll
-        for (int c = KT; c < NV; c += KT) {
-            uint32_t w[KT];
-#pragma unroll
-            for (int i = 0; i < KT; ++i) w[i] = u[c + i];
-            sort_any<KT>(w);
-            merge_top<KT>(v, w);
-        }
-        if (a.top_groups < a.groups) {
+            kept = rank < a.top_groups;
 #pragma unroll
             for (int i = 0; i < KT; ++i) v[i] = kept ? v[i] : 0u;
+            rest = kept ? rest : 0u;
         }
+        uint32_t own[KT];  // the lane's, of which the next keeps the token's
+#pragma unroll
+        for (int i = 0; i < KT; ++i) own[i] = v[i];
 #pragma unroll
         for (int o = 1; o < LPT; o <<= 1) {
             uint32_t w[KT];
@@ -372,10 +400,9 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
         }
         const bool out = !clean && last < KEY_OUT + 256;
         last -= KEY_SURE;
-        int n = 0;
+        int n = rest >= last ? 1024 : 0;  // (keys that no list holds)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) n += u[i] >= last;
-        n = kept ? n : 0;
+        for (int i = 0; i < KT; ++i) n += own[i] >= last;
 #pragma unroll
         for (int o = 1; o < LPT; o <<= 1) n += __shfl_xor_sync(0xffffffffu, n, o);
         sure &= n == k || out;
@@ -384,15 +411,11 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
             // the few that are not clear of the k largest, by exact keys against each other
             if (l == 0) cand.n = 0;
             __syncwarp();
-#pragma unroll 1
-            for (int i = 0; i < NV; ++i) {
-                uint32_t ui = 0;
 #pragma unroll
-                for (int j = 0; j < NV; ++j) ui = i == j ? u[j] : ui;
-                if (kept && ui >= last && n <= GT_CAND) cand.id[atomicAdd(&cand.n, 1)] = 255 - (int)(ui & 0xffu);
-            }
+            for (int i = 0; i < KT; ++i)
+                if (own[i] >= last && !sure && n <= GT_CAND) cand.id[atomicAdd(&cand.n, 1)] = 255 - (int)(own[i] & 0xffu);
             __syncwarp();
-            if (on && n <= GT_CAND) {
+            if (on && !sure && n <= GT_CAND) {
                 for (int c = l; c < n; c += LPT) {
                     const int e = cand.id[c];
                     const float z = a.logits[t * E + e];
@@ -402,7 +425,7 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
                 }
             }
             __syncwarp();
-            if (on && n <= GT_CAND) {
+            if (on && !sure && n <= GT_CAND) {
                 for (int c = l; c < n; c += LPT) {
                     int rank = 0;
                     for (int o = 0; o < n; ++o)
@@ -412,11 +435,11 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
             }
             __syncwarp();
             // many that are not (equal keys): each such token by the whole warp
-            const uint32_t many = __ballot_sync(0xffffffffu, on && n > GT_CAND);
+            const uint32_t many = __ballot_sync(0xffffffffu, on && !sure && n > GT_CAND);
 #pragma unroll 1
             for (int j = 0; j < TPW; ++j)
                 if ((many >> (j * LPT)) & 1u) exact_token<SIG>(a, tw + j, s_pick[(threadIdx.x / 32) * TPW + j]);
-            if (l < k) pe = picks[l];
+            if (l < k && !sure) pe = picks[l];
             __syncwarp();
         }
         // pick j in lane j

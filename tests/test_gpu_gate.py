@@ -311,3 +311,50 @@ def test_no_tokens(L):
     assert status(L) == 0 and int(counts.abs().max()) == 0
     L.moe_gate_bwd(cfg, L.make_gate_rule(), None, None, None, None, po, None)
     assert status(L) == 0
+
+
+def exact_by_sorting(L, z, b, k, sigmoid, G=1, top=1, best=1):
+    """Picks from exact 32-bit keys by stable sorts (the scores in torch's 32-bit arithmetic)."""
+    T, E = z.shape
+    z = torch.where(torch.isnan(z), -float("inf"), z)
+    key = 1.0 / (1.0 + torch.exp(-z)) if sigmoid else z
+    key = torch.where(z == -float("inf"), z, key + b if b is not None else key)
+    g = torch.sort(key.view(T, G, E // G), dim=2, descending=True, stable=True).values[..., :best].sum(2)
+    order = torch.sort(g, dim=1, descending=True, stable=True).indices[:, :top]
+    kept = torch.zeros(T, G, dtype=torch.int32, device="cuda").scatter_(1, order, 1).repeat_interleave(E // G, 1)
+    idx = torch.sort(key, dim=1, descending=True, stable=True).indices
+    last = torch.sort(kept.gather(1, idx), dim=1, descending=True, stable=True).indices
+    return idx.gather(1, last)[:, :k].int()
+
+
+@pytest.mark.parametrize("E,k,G,top,best", [(256, 8, 8, 4, 2), (256, 8, 1, 1, 1), (128, 2, 1, 1, 1), (64, 6, 4, 2, 1), (16, 2, 1, 1, 1),
+                                            (96, 8, 3, 2, 2), (248, 5, 31, 7, 2), (30, 4, 5, 3, 1)])
+@pytest.mark.parametrize("T", [37, 20011])
+@pytest.mark.parametrize("sigmoid", [False, True])
+def test_picks_of_close_equal_and_crowded_keys(L, E, k, G, top, best, T, sigmoid):
+    """Keys that the networks' approximate keys cannot tell apart (some units of the last place apart), equal ones
+    few and many, all picks in one lane's experts, ranges past the sort keys', -inf in the bias: exact picks."""
+    gen = torch.Generator(device="cuda").manual_seed(E + k + T)
+    z = torch.randn(T, E, generator=gen, device="cuda")
+    b = 0.05 * torch.randn(1, E, generator=gen, device="cuda")
+    kind = torch.arange(T, device="cuda") % 9
+    base = torch.randn(T, 1, generator=gen, device="cuda")
+    near = (base * (1 + torch.randint(-6, 7, (T, E), generator=gen, device="cuda") * 2.0 ** -23))  # units of the last place
+    z = torch.where((kind == 1)[:, None], near, z)
+    z = torch.where((kind == 2)[:, None], base.expand(T, E), z)                    # all equal
+    z = torch.where((kind == 3)[:, None] & (torch.rand(T, E, generator=gen, device="cuda") < 0.1), 40.0, z)  # saturated
+    first = torch.zeros(T, E, device="cuda")
+    first[:, :16] = 6.0
+    z = torch.where((kind == 4)[:, None], z + first, z)                            # neighbours
+    first.zero_()
+    first[:, ::16] = 6.0
+    z = torch.where((kind == 5)[:, None], z + first, z)                            # 16 apart
+    z = torch.where((kind == 6)[:, None], 30 * z, z)                               # past 16 below the largest
+    z = torch.where((kind == 7)[:, None] & (torch.arange(E, device="cuda") > 1), -float("inf"), z)  # two within reach
+    z = torch.where((kind == 8)[:, None], torch.round(4 * z) / 4, z)               # many equal ones
+    for bias in (None, b, torch.where(torch.rand(1, E, generator=gen, device="cuda") < 0.2, -float("inf"), 3 * b), 40 * b):
+        _, _, _, idx, w, counts, _ = run(L, T, E, k, z, bias, sigmoid, G, top, best)
+        want = exact_by_sorting(L, z, bias, k, sigmoid, G, top, best)
+        bad = (idx != want).any(1)
+        assert not bad.any(), (int(bad.sum()), sorted(set(kind[bad].tolist())), idx[bad][:2].tolist(), want[bad][:2].tolist())
+        assert torch.equal(torch.bincount(idx.flatten().long(), minlength=E), counts[0].long())

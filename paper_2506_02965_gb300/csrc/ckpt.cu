@@ -128,8 +128,8 @@ template <int VW> constexpr int swiglu_spans() { return VW == 8 ? 2 : 4; }
 
 // SwiGLU backward from the checkpoint of [G|U] (rows of 2F columns in one run of blocks):
 //   s = sigmoid(G), act = G s U, dU = dA G s, dG = dA U s (1 + G (1 - s)).
-// The sigmoid of bf16 results takes the fast exponential and quotient (errors of a few 2^-23, results rounded to
-// 2^-8); with the full-precision ones their instructions, not HBM, are the bound.
+// The sigmoid is the fast one (a few 2^-23 of it, far below what 8 bits left of G and U): with full-precision
+// exponentials and quotients their instructions, not HBM, are the bound.
 template <typename T, int VW>
 __global__ void __launch_bounds__(CK_THREADS) ckpt_swiglu_bwd_kernel(const int8_t* __restrict__ q, const float* __restrict__ scale,
                                                                      const T* __restrict__ dact, uint32_t spans, Divisor per_row,
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_swiglu_bwd_kernel(const int8_
         sd[u].unpack(d);
 #pragma unroll
         for (int j = 0; j < VW; ++j) {
-            const float s = sizeof(T) == 2 ? __fdividef(1.f, 1.f + __expf(-G[j])) : sigmoidf_(G[j]);
+            const float s = fast_sigmoid(G[j]);
             const float gs = G[j] * s;
             a[j] = gs * Uv[j];
             du[j] = d[j] * gs;

@@ -89,21 +89,6 @@ template <bool SIG> __device__ __forceinline__ float score_of(float z, float m, 
     return SIG ? 1.f / (1.f + expf(-z)) : expf(z - m) * inv;
 }
 
-// 2^x and 1 / x by one instruction each: off by at most 2^-22 and 2^-23 of the result
-__device__ __forceinline__ float fast_exp2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float fast_rcp(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-constexpr float LOG2E = 1.4426950408889634f;
-// exp(x), off by 2^-22 + |x| 2^-24 of the result
-__device__ __forceinline__ float fast_exp(float x) { return fast_exp2(x * LOG2E); }
-
 // Keys for sorting: the distance of a key below `top` (no key is above it), in units of KEY_RANGE / 2^23 up to
 // KEY_RANGE (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
 // the top down, and bit 31; an expert's 255 - id below, so that equal ones come in the order of their ids. Two
@@ -290,14 +275,14 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
             if (clean) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    if constexpr (SIG) key[i] = fast_rcp(1.f + fast_exp(-key[i]));
+                    if constexpr (SIG) key[i] = fast_sigmoid(key[i]);
                     if (bias) key[i] += b[i];
                 }
             } else {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
                     const bool reach = key[i] > NINF;  // (a NaN is out of reach)
-                    if constexpr (SIG) key[i] = fast_rcp(1.f + fast_exp(-key[i]));
+                    if constexpr (SIG) key[i] = fast_sigmoid(key[i]);
                     if (bias) key[i] += b[i];
                     key[i] = reach ? key[i] : NINF;
                 }

@@ -152,4 +152,20 @@ __device__ __forceinline__ int party_of(const int32_t* po, int P, int64_t t) {
 
 __device__ __forceinline__ float sigmoidf_(float g) { return 1.0f / (1.0f + expf(-g)); }
 
+// 2^x and 1 / x by one instruction each: off by at most 2^-22 and 2^-23 of the result
+__device__ __forceinline__ float fast_exp2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float fast_rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+constexpr float LOG2E = 1.4426950408889634f;
+// exp(x), off by 2^-22 + |x| 2^-24 of the result; 1 / (1 + exp(-x)), off by that and 2^-23
+__device__ __forceinline__ float fast_exp(float x) { return fast_exp2(x * LOG2E); }
+__device__ __forceinline__ float fast_sigmoid(float x) { return fast_rcp(1.f + fast_exp(-x)); }
+
 }  // namespace moe

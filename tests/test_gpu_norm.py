@@ -139,6 +139,34 @@ def test_many_rows_and_repeats(L, name):
     within("dbeta", a[2], dy.sum(0), 512 * U * dy.abs().sum(0))
 
 
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("R,d", [(3001, 333), (6007, 77), (2500, 1003), (1001, 4099), (700, 7001), (9001, 13), (40000, 6)])
+def test_many_rows_of_odd_widths(L, R, d, name):
+    """Rows that start at every element of a 16-byte span, many per team (bounds as above; a column's sum runs through
+    R / 152 rows of a CTA at most, 10 partials of a slice and 16 slices: below 512 additions)."""
+    c = case(R, d, name, R)
+    h64 = c["x"].double() + c["r"].double()
+    o = forward(L, c, R, d, name, ckpt=True)
+    var, mean = torch.var_mean(h64, dim=1, correction=0, keepdim=True)
+    rstd = 1 / torch.sqrt(var + EPS)
+    ref = (h64 - mean) * rstd * c["gamma"].double() + c["beta"].double()
+    top = h64.abs().amax(1, keepdim=True)
+    within("y", o["y"], ref, 256 * U * (c["gamma"].double().abs() * top * rstd + c["beta"].double().abs()) + rounding(name) * ref.abs())
+    held = o["q"].double() * o["scale"].double().repeat_interleave(128, 1)[:, :d]
+    rs, dy = o["rstd"].double()[:, None], c["dy"].double()
+    for h, kept in ((o["h"], o["h"].double()), (None, held)):
+        dx, dg, db = backward(L, R, d, name, c["dy"], h, None if h is not None else o["q"], None if h is not None else o["scale"],
+                              o["mean"], o["rstd"], c["gamma"], c["dh"])
+        xh = (kept - o["mean"].double()[:, None]) * rs
+        g = dy * c["gamma"].double()
+        ref = c["dh"].double() + rs * (g - g.mean(1, keepdim=True) - xh * (g * xh).mean(1, keepdim=True))
+        b = 512 * U * rs * g.abs().amax(1, keepdim=True) * (1 + xh.abs().amax(1, keepdim=True) ** 2) + 4 * U * c["dh"].double().abs()
+        within("dx", dx, ref, b + rounding(name) * ref.abs())
+        size = (dy * xh).abs().sum(0) + (dy.abs() * rs * kept.abs().amax(1, keepdim=True)).sum(0)
+        within("dgamma", dg, (dy * xh).sum(0), 1024 * U * size)
+        within("dbeta", db, dy.sum(0), 1024 * U * dy.abs().sum(0))
+
+
 @pytest.mark.parametrize("off", [1, 2, 4])
 @pytest.mark.parametrize("name", ["f32", "bf16"])
 def test_unaligned_buffers_equal_aligned_sizes(L, name, off):

@@ -24,7 +24,7 @@ struct Divisor {
 };
 
 // A group of LANES lanes takes a block of 128 columns of a row: VW = 16 / sizeof(T) consecutive ones a lane (half a warp
-// or a warp a block), or in rows that no 16-byte access fits 2 or 1, 32 lanes of them in turn.
+// or a warp a block), or in rows that no 16-byte access fits 4, 2 or 1, 32 lanes of them in turn.
 template <typename T, int VW> struct CkptMap {
     static constexpr int LANES = VW > 2 ? CKPT_BLOCK / VW : 32;
     static constexpr int GROUPS = CK_THREADS / LANES;
@@ -124,64 +124,78 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_unpack_kernel(const int8_t* _
         }
 }
 
-template <int VW> constexpr int swiglu_spans() { return VW == 8 ? 2 : 4; }
-
 // SwiGLU backward from the checkpoint of [G|U] (rows of 2F columns in one run of blocks):
 //   s = sigmoid(G), act = G s U, dU = dA G s, dG = dA U s (1 + G (1 - s)).
 // The sigmoid is the fast one (a few 2^-23 of it, far below what 8 bits left of G and U): with full-precision
 // exponentials and quotients their instructions, not HBM, are the bound.
+// A group of lanes takes 128 columns of G, one block of the checkpoint, and the same of U, which lie in one or two.
+template <int VW> constexpr int swiglu_u() { return VW > 1 ? 2 : 1; }  // such runs of columns in flight per group of lanes
+
 template <typename T, int VW>
 __global__ void __launch_bounds__(CK_THREADS) ckpt_swiglu_bwd_kernel(const int8_t* __restrict__ q, const float* __restrict__ scale,
-                                                                     const T* __restrict__ dact, uint32_t spans, Divisor per_row,
+                                                                     const T* __restrict__ dact, uint32_t runs, Divisor per_row,
                                                                      int F, int nb, T* __restrict__ act, T* __restrict__ dh) {
     pdl_begin();
-    constexpr int U = swiglu_spans<VW>();
-    Span<T, VW> sd[U];
-    uint32_t wg[U][(VW + 3) / 4], wu[U][(VW + 3) / 4];
-    float cg[U], cu[U];
-    int64_t at[U];  // in rows of F; in rows of 2F
-    int64_t at2[U];
-    bool on[U];
+    using M = CkptMap<T, VW>;
+    constexpr int U = swiglu_u<VW>();
+    const int lane = threadIdx.x % M::LANES;
+    const uint32_t r0 = blockIdx.x * (M::GROUPS * U) + threadIdx.x / M::LANES;
+    Span<T, VW> sd[U][M::SPANS];
+    uint32_t wg[U][M::SPANS][(VW + 3) / 4], wu[U][M::SPANS][(VW + 3) / 4];
+    float cg[U], cu[U][2];
+    int64_t at[U], at2[U];  // the run's first column in rows of F; in rows of 2F
+    int left[U], split[U];  // columns to the row's end; to U's second block
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint32_t v = blockIdx.x * (CK_THREADS * U) + u * CK_THREADS + threadIdx.x;
-        on[u] = v < spans;
-        const uint32_t row = per_row(v);
-        const int col = (int)(v - row * per_row.d) * VW;
-        at[u] = (int64_t)v * VW;
+        const uint32_t r = r0 + u * M::GROUPS;
+        const uint32_t row = per_row(r);
+        const int c0 = (int)(r - row * per_row.d) * CKPT_BLOCK, b = (F + c0) / CKPT_BLOCK;
+        at[u] = (int64_t)row * F + c0;
         at2[u] = at[u] + (int64_t)row * F;
-        if (on[u]) {
-            load_q<VW>(q + at2[u], wg[u]);
-            load_q<VW>(q + at2[u] + F, wu[u]);
+        left[u] = r < runs ? F - c0 : 0;
+        split[u] = (b + 1) * CKPT_BLOCK - (F + c0);
+        if (left[u] > 0) {
             const float* sc = scale + (int64_t)row * nb;
-            cg[u] = sc[col / CKPT_BLOCK];
-            cu[u] = sc[(F + col) / CKPT_BLOCK];
-            sd[u].load(dact + at[u]);
+            cg[u] = sc[c0 / CKPT_BLOCK];
+            cu[u][0] = sc[b];
+            cu[u][1] = split[u] < CKPT_BLOCK && b + 1 < nb ? sc[b + 1] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < M::SPANS; ++i) {
+            const int c = M::col(lane, i);
+            if (c < left[u]) {
+                load_q<VW>(q + at2[u] + c, wg[u][i]);
+                load_q<VW>(q + at2[u] + F + c, wu[u][i]);
+                sd[u][i].load(dact + at[u] + c);
+            }
         }
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        if (!on[u]) continue;
-        float G[VW], Uv[VW], d[VW], a[VW], dg[VW], du[VW];
-        unquant<VW>(wg[u], cg[u], G);
-        unquant<VW>(wu[u], cu[u], Uv);
-        sd[u].unpack(d);
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < VW; ++j) {
-            const float s = fast_sigmoid(G[j]);
-            const float gs = G[j] * s;
-            a[j] = gs * Uv[j];
-            du[j] = d[j] * gs;
-            dg[j] = d[j] * Uv[j] * (s + gs * (1.f - s));
+        for (int i = 0; i < M::SPANS; ++i) {
+            const int c = M::col(lane, i);
+            if (c >= left[u]) continue;
+            float G[VW], Uv[VW], d[VW], a[VW], dg[VW], du[VW];
+            unquant<VW>(wg[u][i], cg[u], G);
+            unquant<VW>(wu[u][i], c < split[u] ? cu[u][0] : cu[u][1], Uv);  // (a span lies in one block: F % VW == 0)
+            sd[u][i].unpack(d);
+#pragma unroll
+            for (int j = 0; j < VW; ++j) {
+                const float s = fast_sigmoid(G[j]);
+                const float gs = G[j] * s;
+                a[j] = gs * Uv[j];
+                du[j] = d[j] * gs;
+                dg[j] = d[j] * Uv[j] * (s + gs * (1.f - s));
+            }
+            Span<T, VW> o;
+            o.pack(a);
+            o.store(act + at[u] + c);
+            o.pack(dg);
+            o.store(dh + at2[u] + c);
+            o.pack(du);
+            o.store(dh + at2[u] + F + c);
         }
-        Span<T, VW> o;
-        o.pack(a);
-        o.store(act + at[u]);
-        o.pack(dg);
-        o.store(dh + at2[u]);
-        o.pack(du);
-        o.store(dh + at2[u] + F);
-    }
 }
 
 // ---------------------------------------------------------------------------- launchers
@@ -218,8 +232,8 @@ static cudaError_t unpack_t(const int8_t* q, const float* scale, int64_t rows, i
 }
 template <typename T, int VW>
 static cudaError_t swiglu_t(const int8_t* q, const float* scale, const T* dact, int64_t rows, int F, T* act, T* dh, cudaStream_t s) {
-    const int64_t per_row = F / VW, nb = (2 * (int64_t)F + CKPT_BLOCK - 1) / CKPT_BLOCK;
-    constexpr int PER = swiglu_spans<VW>() * CK_THREADS;
+    const int64_t per_row = ((int64_t)F + CKPT_BLOCK - 1) / CKPT_BLOCK, nb = (2 * (int64_t)F + CKPT_BLOCK - 1) / CKPT_BLOCK;
+    constexpr int PER = CkptMap<T, VW>::GROUPS * swiglu_u<VW>();
     return by_rows(rows, per_row, [&](int64_t r, int64_t n) {
         (void)launch_pdl(ckpt_swiglu_bwd_kernel<T, VW>, dim3((unsigned)((n * per_row + PER - 1) / PER)), dim3(CK_THREADS), 0, s,
                          q + r * 2 * F, scale + r * nb, dact + r * F, (uint32_t)(n * per_row), Divisor((uint32_t)per_row), F, (int)nb,
@@ -227,16 +241,16 @@ static cudaError_t swiglu_t(const int8_t* q, const float* scale, const T* dact, 
     });
 }
 
-// The widest span that all of a row's accesses are aligned to: 16 bytes, two elements or one
+// The widest span that all of a row's accesses are aligned to: 16 bytes, four elements, two or one
 template <typename T> static int span_of(int cols, std::initializer_list<const void*> elems, const int8_t* q) {
-    for (int vw : {16 / (int)sizeof(T), 2}) {
+    for (int vw : {16 / (int)sizeof(T), 4, 2}) {
         bool ok = cols % vw == 0 && aligned_to(q, vw);
         for (const void* p : elems) ok = ok && aligned_to(p, vw * sizeof(T));
         if (ok) return vw;
     }
     return 1;
 }
-#define MOE_BY_SPAN(vw, CALL) (vw > 2 ? CALL(16 / (int)sizeof(T)) : vw == 2 ? CALL(2) : CALL(1))
+#define MOE_BY_SPAN(vw, CALL) (vw > 4 ? CALL(16 / (int)sizeof(T)) : vw == 4 ? CALL(4) : vw == 2 ? CALL(2) : CALL(1))
 
 template <typename T> static cudaError_t pack_any(const void* x, int64_t rows, int cols, int8_t* q, float* scale, cudaStream_t s) {
     const int vw = span_of<T>(cols, {x}, q);

@@ -2,17 +2,23 @@
 // in the choice only, expert groups of which some are kept, k picks, renormalised and scaled
 // weights; their backward; the balance bias's update.
 //
-// A token's keys live in the registers of LPT lanes (8, 16 or 32: several tokens a warp), up to 32 a
-// lane, each group of experts in an equal, power-of-two share of the lanes, so that a group's key
+// Forward. A token's keys live in the registers of LPT lanes (8, 16 or 32: several tokens a warp), up to
+// 16 a lane, each group of experts in an equal, power-of-two share of the lanes, so that a group's key
 // is a reduction over aligned lanes. The k largest keys come out of sorting networks: every lane sorts its
-// own, then lanes merge pairwise, each merge keeping the KT (2, 4, 8) largest of two sorted lists; no
+// own, then lanes merge pairwise, each merge keeping the KT (2, 8) largest of two sorted lists; no
 // step waits for the one before it as k rounds of "largest left" would.
+// Picks are decided by exact keys. The networks sort approximate ones (scores by two instructions) in 23 bits,
+// with the expert in 8 bits below: enough wherever the keys that decide lie further apart than the approximation, which is
+// checked. Two groups too close (one token in 1000 of random ones) are decided by exact keys of their warp's
+// tokens; experts too close (one in 1000) by the exact keys of those few against each other, or, where they are
+// more than 24 (equal keys), by a whole warp, one pick after the other.
+// What bounds the forward is instructions, about 600 a token of 256 experts (0.65 of the issue slots, half of them on the
+// integer pipe at half rate), not the row's one read: 65536 tokens, 256 experts, 8 groups 43.8 us (the read: 10.5);
+// rounds of "largest left" in a warp per token with exact scores 94.7.
+// Also measured: keeping only keys above a floor, the k-th largest of the lanes' largest, and ranking those: 47 us, without groups 33
+// against 38, but 20 against 15 for 64 experts and 11 against 9 for 16.
 //
-// Picks are decided by exact keys. The networks sort approximate ones, 24 bits of distance from the row's
-// largest with the expert in the 8 below: enough wherever the keys that decide lie further apart than the
-// approximation, which is checked; a token of closer ones (equal keys, or about one in 500 of random ones) is decided
-// by a whole warp from exact keys, one pick after the other. What bounds the kernel is instructions, some
-// tens per expert, not the row's one read.
+// Backward: one read of the logits, one write of their gradient, HBM-bound (65536 x 256: 25.4 us, 0.80 of the copy rate).
 #include <algorithm>
 
 #include "moe_common.cuh"
@@ -21,7 +27,7 @@
 namespace moe {
 
 constexpr int GT_THREADS = 256;
-constexpr int GT_RESIDENT = 3;  // CTAs per SM (65536 tokens, E = 256, 8 groups: 48.1 us; with 4, whose registers spill, 52.4)
+constexpr int GT_RESIDENT = 3;  // CTAs per SM (with 4 the registers spill: 52 us against 48 for 65536 tokens, E = 256)
 
 template <int LPT> __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
@@ -224,6 +230,7 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
     Candidates& cand = s_cand[threadIdx.x / LPT];
     const int64_t t0 = (int64_t)blockIdx.x * chunk, t1 = min64(t0 + chunk, a.T);
     const int p0 = party_of(a.po, a.P, t0);
+    const bool one_party = party_of(a.po, a.P, t1 - 1) == p0;
     for (int e = threadIdx.x; e < E; e += GT_THREADS) hist[e] = 0;
     __syncthreads();
     int key_party = -1;
@@ -232,7 +239,7 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
     for (int64_t tw = t0 + (threadIdx.x / 32) * TPW; tw < t1; tw += TPC) {
         const int64_t t = tw + lane / LPT;
         const bool on = t < t1;
-        const int party = on ? party_of(a.po, a.P, t) : p0;
+        const int party = one_party || !on ? p0 : party_of(a.po, a.P, t);
         const float* row = a.logits + t * E + first;
         const float* bias = a.bias ? a.bias + (int64_t)party * E + first : nullptr;
         float key[NV], m = 0.f, inv = 1.f;
@@ -325,18 +332,20 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
         }
         bool kept = true;
         if (a.top_groups < a.groups) {
-            // groups by the units of their best keys, 0 for one out of reach
+            // groups by the units of their best keys, those out of reach below in their order
             uint32_t b1 = v[0], b2 = v[1];
             group_best(b1, b2, lpg);
+            constexpr int NEAR = 2 * (int)(KEY_SURE >> 8);
             const int n1 = key_units(b1), n2 = a.group_top == 2 ? key_units(b2) : n1;
-            const int mine = !clean && min(n1, n2) == 0 ? 0 : 1 + n1 + (a.group_top == 2 ? n2 : 0);
-            bool sure = mine == 0 || min(n1, n2) >= 32;  // (not at the end of the range)
-            int rank = 0;
+            const bool gone = !clean && min(n1, n2) == 0;
+            const int mine = gone ? -2 * NEAR * grp : 1 + NEAR + n1 + (a.group_top == 2 ? n2 : 0);
+            int rank = 0, close = 0;  // groups ahead of this one; groups too close to tell, itself among them
             for (int g = 0; g < a.groups; ++g) {
-                const int other = __shfl_sync(0xffffffffu, mine, base + g * lpg);
-                rank += other > mine || (other == mine && g < grp);
-                sure &= g == grp || abs(other - mine) > 2 * (int)(KEY_SURE >> 8) || (mine == 0 && other == 0);
+                const int d = __shfl_sync(0xffffffffu, mine, base + g * lpg) - mine;
+                rank += d > 0;
+                close += (uint32_t)(d + NEAR) <= 2u * NEAR;
             }
+            const bool sure = close == 1 && (gone || min(n1, n2) >= 32);  // (not at the end of the range)
             if (__any_sync(0xffffffffu, on && !sure && grp < a.groups)) {  // two groups too close: by exact keys
                 float z[NV], c1 = NINF, c2 = NINF;
                 slots.template load<NV>(row, on, NINF, z);
@@ -631,8 +640,8 @@ static cudaError_t launch_gate_t(const GateArgs& a, int lpg, cudaStream_t s) {
 
 // Lanes per token: the fewest (8, 16, 32) that give every group a lane and hold the pool with at
 // most 16 keys a lane, or 8 while even that leaves every warp resident: fewer lanes a token are fewer
-// instructions, more are a shorter chain of them (E = 256, 8 groups: 65536 tokens 58 us with 16 keys a lane, 76
-// with 8; 2999 tokens 11.7 and 8.6).
+// instructions, more are a shorter chain of them (E = 256, 8 groups, in an earlier state of the kernel: 65536 tokens 58 us
+// with 16 keys a lane, 76 with 8; 2999 tokens 11.7 and 8.6).
 cudaError_t launch_gate(const GateArgs& a, cudaStream_t s) {
     if (a.T == 0) return cudaMemsetAsync(a.counts, 0, sizeof(int32_t) * a.P * a.E, s);
     const int Gp = pow2_ceil(a.groups), gs = a.E / a.groups;

@@ -463,17 +463,16 @@ __global__ void __launch_bounds__(256) gate_zero_kernel(int32_t* counts, int n) 
     if (i < n) counts[i] = 0;
 }
 
-// dlogits of a token by 8 lanes (four tokens a warp), NV scores a lane in spans of SP = 4 (or single ones).
+// dlogits of a token by LPT lanes (several tokens a warp), NV scores a lane in spans of SP = 4 (or single ones).
 // The picks' gradients touch k places of a row: the row is written as if there were none (but for
 // their part in softmax's <ds, s>), then lane j writes pick j's place again. One read and one write of a
 // row; fast exponentials (2^-22 of the result, as the row's sum).
-constexpr int GB_LPT = 8;
-template <int NV, int SP, bool SIG>
+template <int NV, int LPT, int SP, bool SIG>
 __global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(const __grid_constant__ GateBwdArgs a, __nv_bfloat16* dz16, int EP,
                                                               int32_t* chunk_off, int CH, int nchunk) {
     pdl_begin();
     constexpr float NINF = -INFINITY;
-    constexpr int LPT = GB_LPT, TPC = GT_THREADS / LPT;
+    constexpr int TPC = GT_THREADS / LPT;
     if (chunk_off && blockIdx.x == 0 && threadIdx.x == 0) {  // the chunks of the weight gradient's contraction
         int c = 0;
         for (int q = 0; q < a.P; ++q) {
@@ -665,13 +664,13 @@ cudaError_t launch_gate(const GateArgs& a, cudaStream_t s) {
 #undef MOE_GATE_K
 }
 
-template <int NV>
+template <int NV, int LPT>
 static cudaError_t launch_gate_bwd_t(const GateBwdArgs& a, __nv_bfloat16* dz16, int EP, int32_t* chunk_off, int CH, int nchunk,
                                      cudaStream_t s) {
-    const unsigned ctas = (unsigned)((a.T + GT_THREADS / GB_LPT - 1) / (GT_THREADS / GB_LPT));
+    const unsigned ctas = (unsigned)((a.T + GT_THREADS / LPT - 1) / (GT_THREADS / LPT));
     const bool vec = a.E % 4 == 0 && (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.dlogits % 16 == 0 && (uintptr_t)a.aux_coef % 16 == 0;
 #define MOE_GB(SP, SIG)                                                                                                        \
-    (void)launch_pdl(gate_bwd_kernel<NV, SP, SIG>, dim3(ctas), dim3(GT_THREADS), 0, s, a, dz16, EP, chunk_off, CH, nchunk)
+    (void)launch_pdl(gate_bwd_kernel<NV, LPT, SP, SIG>, dim3(ctas), dim3(GT_THREADS), 0, s, a, dz16, EP, chunk_off, CH, nchunk)
     if (a.sigmoid) {
         if (vec) MOE_GB(4, true);
         else MOE_GB(1, true);
@@ -684,10 +683,10 @@ static cudaError_t launch_gate_bwd_t(const GateBwdArgs& a, __nv_bfloat16* dz16, 
 }
 
 cudaError_t launch_gate_bwd(const GateBwdArgs& a, __nv_bfloat16* dz16, int EP, int32_t* chunk_off, int CH, int nchunk, cudaStream_t s) {
-    if (a.E <= 32) return launch_gate_bwd_t<4>(a, dz16, EP, chunk_off, CH, nchunk, s);
-    if (a.E <= 64) return launch_gate_bwd_t<8>(a, dz16, EP, chunk_off, CH, nchunk, s);
-    if (a.E <= 128) return launch_gate_bwd_t<16>(a, dz16, EP, chunk_off, CH, nchunk, s);
-    return launch_gate_bwd_t<32>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    if (a.E <= 32) return launch_gate_bwd_t<4, 8>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    if (a.E <= 64) return launch_gate_bwd_t<8, 8>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    if (a.E <= 128) return launch_gate_bwd_t<16, 8>(a, dz16, EP, chunk_off, CH, nchunk, s);
+    return launch_gate_bwd_t<16, 16>(a, dz16, EP, chunk_off, CH, nchunk, s);
 }
 
 cudaError_t launch_gate_balance(const int32_t* counts, int P, int E, float rate, const float* in, float* out, cudaStream_t s) {

@@ -3,7 +3,7 @@
 // weights; their backward; the balance bias's update.
 //
 // Forward. A token's keys live in the registers of LPT lanes (8, 16 or 32: several tokens a warp), up to
-// 16 a lane, each group of experts in an equal, power-of-two share of the lanes, so that a group's key
+// 32 a lane, each group of experts in an equal, power-of-two share of the lanes, so that a group's key
 // is a reduction over aligned lanes. The k largest keys come out of sorting networks: every lane sorts its
 // own, then lanes merge pairwise, each merge keeping the KT (2, 8) largest of two sorted lists; no
 // step waits for the one before it as k rounds of "largest left" would.
@@ -12,13 +12,14 @@
 // checked. Two groups too close (one token in 1000 of random ones) are decided by exact keys of their warp's
 // tokens; experts too close (one in 1000) by the exact keys of those few against each other, or, where they are
 // more than 24 (equal keys), by a whole warp, one pick after the other.
-// What bounds the forward is instructions, about 600 a token of 256 experts (0.65 of the issue slots, half of them on the
-// integer pipe at half rate), not the row's one read: 65536 tokens, 256 experts, 8 groups 43.8 us (the read: 10.5);
-// rounds of "largest left" in a warp per token with exact scores 94.7.
-// Also measured: keeping only keys above a floor, the k-th largest of the lanes' largest, and ranking those: 47 us, without groups 33
-// against 38, but 20 against 15 for 64 experts and 11 against 9 for 16.
+// What bounds the forward is instructions, about 550 a token of 256 experts, half of them on the integer pipe
+// at half rate, not the row's one read: 65536 tokens, 256 experts, 8 groups, bias 39.6 us, without groups and bias 30.1
+// (the read: 10.5); rounds of "largest left" in a warp per token with exact scores 94.7.
+// Also measured: keeping only keys above a floor, the k-th largest of the lanes' largest, and ranking those (16 keys a lane):
+// 47 us against 44 of the networks, without groups 33 against 38, 20 against 15 for 64 experts and 11 against 9 for 16;
+// the next rows copied ahead to shared memory: 44 (the reads back cost more than the wait).
 //
-// Backward: one read of the logits, one write of their gradient, HBM-bound (65536 x 256: 25.4 us, 0.80 of the copy rate).
+// Backward: one read of the logits, one write of their gradient, HBM-bound (65536 x 256: 25.2 us, 0.81 of the copy rate).
 #include <algorithm>
 
 #include "moe_common.cuh"
@@ -27,7 +28,7 @@
 namespace moe {
 
 constexpr int GT_THREADS = 256;
-constexpr int GT_RESIDENT = 3;  // CTAs per SM (with 4 the registers spill: 52 us against 48 for 65536 tokens, E = 256)
+constexpr int gate_resident(int nv) { return nv > 16 ? 2 : 3; }  // CTAs per SM: 128 or 80 registers a thread (with less they spill)
 
 template <int LPT> __device__ __forceinline__ float lanes_sum(float v) {
 #pragma unroll
@@ -215,7 +216,7 @@ __device__ __noinline__ void exact_token(const GateArgs& a, int64_t t, int* pick
 }
 
 template <int NV, int LPT, int KT, bool VEC, bool SIG>
-__global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __grid_constant__ GateArgs a, int lpg, int chunk,
+__global__ void __launch_bounds__(GT_THREADS, gate_resident(NV)) gate_kernel(const __grid_constant__ GateArgs a, int lpg, int chunk,
                                                                          bool whole) {
     pdl_begin();
     constexpr float NINF = -INFINITY;
@@ -223,6 +224,8 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
     __shared__ int hist[256];
     __shared__ int s_pick[TPC][8];
     __shared__ Candidates s_cand[TPC];
+    // the bias of the CTA's first party, four floats of room after each group: the lanes' spans lie in different banks
+    __shared__ __align__(16) float s_bias[256 + 4 * 32];
     const int lane = threadIdx.x & 31, l = lane % LPT, base = lane - l;
     const int E = a.E, k = a.k, gs = E / a.groups, grp = l / lpg, first = grp * gs;
     const Slots<VEC> slots(lpg, l % lpg, grp < a.groups ? gs : 0);
@@ -231,7 +234,10 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
     const int64_t t0 = (int64_t)blockIdx.x * chunk, t1 = min64(t0 + chunk, a.T);
     const int p0 = party_of(a.po, a.P, t0);
     const bool one_party = party_of(a.po, a.P, t1 - 1) == p0;
-    for (int e = threadIdx.x; e < E; e += GT_THREADS) hist[e] = 0;
+    for (int e = threadIdx.x; e < E; e += GT_THREADS) {
+        hist[e] = 0;
+        if (a.bias) s_bias[e + e / gs * 4] = a.bias[(int64_t)p0 * E + e];
+    }
     __syncthreads();
     int key_party = -1;
     float most_key = 1.f;
@@ -270,7 +276,8 @@ __global__ void __launch_bounds__(GT_THREADS, GT_RESIDENT) gate_kernel(const __g
         {
             float b[NV];
             if (bias) {
-                slots.template load<NV>(bias, true, NINF, b);
+                if (party == p0) slots.template load<NV>(s_bias + grp * (gs + 4), true, NINF, b);
+                else slots.template load<NV>(bias, true, NINF, b);
                 if (SIG && __any_sync(0xffffffffu, party != key_party)) {  // the most a key of this party can be
                     key_party = party;
                     most_key = b[0];
@@ -621,7 +628,7 @@ template <int NV, int LPT, int KT, bool VEC>
 static cudaError_t launch_gate_t(const GateArgs& a, int lpg, cudaStream_t s) {
     constexpr int TPC = GT_THREADS / LPT;
     // all CTAs resident at once, each with as many passes as the others
-    const int64_t passes = (a.T + TPC - 1) / TPC, most = GT_RESIDENT * (int64_t)sm_count();
+    const int64_t passes = (a.T + TPC - 1) / TPC, most = gate_resident(NV) * (int64_t)sm_count();
     const int chunk = (int)((passes + most - 1) / most * TPC);
     const int64_t ctas = (a.T + chunk - 1) / chunk;
     const bool whole = ctas == 1 && a.P == 1;  // the counts are this CTA's: stored, not added
@@ -638,9 +645,9 @@ static cudaError_t launch_gate_t(const GateArgs& a, int lpg, cudaStream_t s) {
 }
 
 // Lanes per token: the fewest (8, 16, 32) that give every group a lane and hold the pool with at
-// most 16 keys a lane, or 8 while even that leaves every warp resident: fewer lanes a token are fewer
-// instructions, more are a shorter chain of them (E = 256, 8 groups, in an earlier state of the kernel: 65536 tokens 58 us
-// with 16 keys a lane, 76 with 8; 2999 tokens 11.7 and 8.6).
+// most 32 keys a lane, or 8 while even that leaves every warp resident: fewer lanes a token are fewer
+// instructions, more are a shorter chain of them (E = 256, 8 groups: 65536 tokens 39.6 us with 32 keys a lane, 43.8 with
+// 16, 66 with 8; 2999 tokens 15.6, 11.7 and 8.6 in an earlier state of the kernel).
 cudaError_t launch_gate(const GateArgs& a, cudaStream_t s) {
     if (a.T == 0) return cudaMemsetAsync(a.counts, 0, sizeof(int32_t) * a.P * a.E, s);
     const int Gp = pow2_ceil(a.groups), gs = a.E / a.groups;
@@ -650,15 +657,15 @@ cudaError_t launch_gate(const GateArgs& a, cudaStream_t s) {
         return n;
     };
     int lpt = lanes(8);
-    if (a.T * lpt / GT_THREADS > GT_RESIDENT * (int64_t)sm_count()) lpt = lanes(16);
+    if (a.T * lpt / GT_THREADS > gate_resident(8) * (int64_t)sm_count()) lpt = lanes(32);
     const int lpg = lpt / Gp;
     int nv = (gs + lpg - 1) / lpg;
     const bool vec = nv > 2 && gs % 4 == 0 && (uintptr_t)a.logits % 16 == 0 && (uintptr_t)a.bias % 16 == 0;
     if (vec) nv = (gs / 4 + lpg - 1) / lpg * 4;
 #define MOE_GATE_K(NV, LPT, VEC) (a.k <= 2 ? launch_gate_t<NV, LPT, 2, VEC>(a, lpg, s) : launch_gate_t<NV, LPT, 8, VEC>(a, lpg, s))
 #define MOE_GATE(NV, LPT) (vec ? MOE_GATE_K(NV, LPT, true) : MOE_GATE_K(NV, LPT, false))
-    if (lpt == 8) return nv <= 2 ? MOE_GATE_K(2, 8, false) : nv <= 4 ? MOE_GATE(4, 8) : nv <= 8 ? MOE_GATE(8, 8) : MOE_GATE(16, 8);
-    if (lpt == 16) return nv <= 8 ? MOE_GATE(8, 16) : MOE_GATE(16, 16);
+    if (lpt == 8) return nv <= 2 ? MOE_GATE_K(2, 8, false) : nv <= 4 ? MOE_GATE(4, 8) : nv <= 8 ? MOE_GATE(8, 8) : nv <= 16 ? MOE_GATE(16, 8) : MOE_GATE(32, 8);
+    if (lpt == 16) return nv <= 8 ? MOE_GATE(8, 16) : nv <= 16 ? MOE_GATE(16, 16) : MOE_GATE(32, 16);
     return nv <= 8 ? MOE_GATE(8, 32) : MOE_GATE(16, 32);
 #undef MOE_GATE
 #undef MOE_GATE_K

@@ -1,5 +1,8 @@
 // Activation checkpoints in 8 bits (the blocks of span.cuh): packing, unpacking, and the SwiGLU
-// backward that reads [G|U] from one. Streams, all HBM-bound.
+// backward that reads [G|U] from one. Streams, all HBM-bound: of the copy rate, 6781 GB/s, 32768 x 28672 bf16 packs in
+// 412.5 us (1.02), unpacks in 417 (1.01), and its SwiGLU backward takes 661 (1.06); 17994 x 2816 24.3, 24.5 and 37.9 us
+// (0.92 to 0.99). Rows of an odd number of elements move 2 bytes a lane: 20000 x 2002 packs at 0.58, the SwiGLU
+// backward of F = 1001 at 0.61, of 1004 (8 bytes a lane) at 0.77.
 #include <algorithm>
 #include <initializer_list>
 

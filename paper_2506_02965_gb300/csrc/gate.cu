@@ -12,9 +12,9 @@
 // checked. Two groups too close (one token in 1000 of random ones) are decided by exact keys of their warp's
 // tokens; experts too close (one in 1000) by the exact keys of those few against each other, or, where they are
 // more than 24 (equal keys), by a whole warp, one pick after the other.
-// What bounds the forward is instructions, about 550 a token of 256 experts, half of them on the integer pipe
-// at half rate, not the row's one read: 65536 tokens, 256 experts, 8 groups, bias 39.6 us, without groups and bias 30.1
-// (the read: 10.5); rounds of "largest left" in a warp per token with exact scores 94.7.
+// What bounds the forward is the chain of a token's instructions (370 a token of 256 experts; issue slots half busy with the
+// 16 warps an SM that 128 registers leave), not the row's one read: 65536 tokens, 256 experts, 8 groups, bias 39.6 us,
+// without groups and bias 30.1 (the read: 10.5); rounds of "largest left" in a warp per token with exact scores 94.7.
 // Also measured: keeping only keys above a floor, the k-th largest of the lanes' largest, and ranking those (16 keys a lane):
 // 47 us against 44 of the networks, without groups 33 against 38, 20 against 15 for 64 experts and 11 against 9 for 16;
 // the next rows copied ahead to shared memory: 44 (the reads back cost more than the wait).

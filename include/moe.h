@@ -398,7 +398,8 @@ moe_status moe_gate_balance(const moe_config* cfg, const int32_t* counts, float 
  *   h_q [rows,d] i8, h_scale [rows, ceil(d/128)] f32 out or NULL: the stored h as moe_ckpt_pack
  *     holds it
  * rows in [0, 2^31), d in [1, 16384] (MOE_ERR_UNSUPPORTED above), any alignment of whole elements;
- * 16-byte aligned buffers with a width of whole 16-byte vectors take the wide path.
+ * 16-byte aligned buffers take the wide path, rows of whole 16-byte vectors the widest. h and y may
+ * be x's or residual's buffers (h and y each another one).
  */
 moe_status moe_layer_norm_fwd(int64_t rows, int32_t d, moe_dtype dtype, const void* x,
                               const void* residual, const float* gamma, const float* beta, float eps,
@@ -415,7 +416,8 @@ moe_status moe_layer_norm_workspace_size(int64_t rows, int32_t d, size_t* bytes 
  *   dy [rows,d] dtype; h [rows,d] dtype, or h_q and h_scale (its checkpoint) with h NULL;
  *   mean, rstd [rows] from the forward; dh [rows,d] dtype or NULL: the gradient that reaches h
  *   past the norm; dx [rows,d] dtype out; dbeta may be NULL.
- * Deterministic: partial sums of fixed rows in the workspace, added in a fixed order.
+ * Deterministic: partial sums of fixed rows in the workspace, added in a fixed order. dx may be
+ * dy's or dh's buffer.
  */
 moe_status moe_layer_norm_bwd(int64_t rows, int32_t d, moe_dtype dtype, const void* dy,
                               const void* h, const int8_t* h_q, const float* h_scale,

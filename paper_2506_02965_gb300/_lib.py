@@ -321,13 +321,14 @@ def _arr(fn, name, t, kind, n):
     global _arr
     if t is None or type(t) is int:
         return t
-    import torch  # noqa: F401  (whose libraries the module links against)
+    import torch
     from importlib import machinery, util
     try:
         spec = util.spec_from_loader("_marshal", machinery.ExtensionFileLoader("_marshal", os.path.join(HERE, "_marshal.so")))
         m = util.module_from_spec(spec)
         m.set_slow(_check_arr)
-        _arr = m.addr
+        # one that was built for another torch does not read this one's tensors
+        _arr = m.addr if m.torch_version == torch.__version__.split("+")[0] else _check_arr
     except (ImportError, OSError):
         _arr = _check_arr
     return _arr(fn, name, t, kind, n)

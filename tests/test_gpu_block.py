@@ -204,3 +204,17 @@ def test_bad_stacks_are_refused(L):
         PreNormMoE(mi.MoEShape("b", 8, 128, 4, 128, 2, "bf16", n_shared=1, d_ff_shared=128), 1)
     with pytest.raises(ValueError, match="n_blocks"):
         PreNormMoE(mi.MoEShape("b", 8, 128, 4, 128, 2, "bf16"), 0)
+
+
+def test_no_tokens(L):
+    """A batch without tokens: weight gradients of zero, the bias as it was."""
+    sh = mi.MoEShape("b", 0, 128, 4, 128, 2, "bf16")
+    net, x, dout = build(sh, 2, L.make_gate_rule(L.MOE_SCORE_SIGMOID), 3)
+    bias = [b.balance_bias.clone() for b in net.blocks]
+    for b in net.blocks:
+        for g in b.grads().values():
+            g.fill_(3.0)
+    assert net.forward(x).numel() == 0 and net.backward(dout).numel() == 0
+    net.check_status()
+    for b, v in zip(net.blocks, bias):
+        assert all(float(g.float().abs().max()) == 0 for g in b.grads().values()) and torch.equal(b.balance_bias, v)

@@ -250,3 +250,50 @@ def test_other_stream(L):
     L.moe_layer_norm_fwd(R, d, L.MOE_BF16, x, None, c["gamma"], c["beta"], EPS, None, y, stream=s)
     s.synchronize()
     assert torch.equal(y, forward(L, c, R, d, "bf16", stats=False)["y"])
+
+
+def test_more_than_2_31_elements(L):
+    """Offsets past 32 bits, forward and backward: the first and last rows are those of a small call."""
+    R, d = 523_907, 4104
+    assert R * d > 1 << 31
+    n = 8
+    c = case(n, d, "bf16", 6, residual=False)
+    x = torch.zeros(R, d, dtype=torch.bfloat16, device="cuda")
+    x[:n], x[-n:] = c["x"], c["x"]
+    y, mean, rstd = torch.empty_like(x), torch.empty(R, device="cuda"), torch.empty(R, device="cuda")
+    L.moe_layer_norm_fwd(R, d, L.MOE_BF16, x, None, c["gamma"], c["beta"], EPS, None, y, mean, rstd)
+    o = forward(L, c, n, d, "bf16")
+    for part in (slice(0, n), slice(R - n, R)):
+        assert torch.equal(y[part], o["y"]) and torch.equal(mean[part], o["mean"]) and torch.equal(rstd[part], o["rstd"])
+    assert torch.equal(y[n:n + 1], c["beta"].bfloat16()[None]) and torch.equal(y[n], y[R - n - 1])
+    y.zero_()
+    y[:n], y[-n:] = c["dy"], c["dy"]
+    ws = torch.empty(L.moe_layer_norm_workspace_size(R, d), dtype=torch.uint8, device="cuda")
+    dg, db = torch.empty(d, device="cuda"), torch.empty(d, device="cuda")
+    L.moe_layer_norm_bwd(R, d, L.MOE_BF16, y, x, None, None, mean, rstd, c["gamma"], None, y, dg, db, ws, ws.numel())  # in place
+    dx, dg1, db1 = backward(L, n, d, "bf16", c["dy"], c["x"], None, None, o["mean"], o["rstd"], c["gamma"], None)
+    assert torch.equal(y[:n], dx) and torch.equal(y[-n:], dx) and float(y[n:-n].abs().max()) == 0
+    # each row counts twice; the sums run in another order
+    assert ((dg - 2 * dg1).abs() <= 64 * U * 2 * c["dy"].float().abs().sum(0) * 64).all()
+    assert ((db - 2 * db1).abs() <= 64 * U * 2 * c["dy"].float().abs().sum(0)).all()
+    del x, y
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("R,d", [(700, 512), (601, 333)])
+def test_in_place(L, R, d, name):
+    """h over x, y over the residual, dx over dh and over dy give what separate buffers give."""
+    c = case(R, d, name, 12)
+    o = forward(L, c, R, d, name)
+    mt = L.MOE_BF16 if name == "bf16" else L.MOE_F32
+    x, r = c["x"].clone(), c["r"].clone()
+    L.moe_layer_norm_fwd(R, d, mt, x, r, c["gamma"], c["beta"], EPS, x, r, o["mean"].clone(), o["rstd"].clone())
+    assert torch.equal(x, o["h"]) and torch.equal(r, o["y"])
+    dx, dg, db = backward(L, R, d, name, c["dy"], o["h"], None, None, o["mean"], o["rstd"], c["gamma"], c["dh"])
+    ws = torch.empty(L.moe_layer_norm_workspace_size(R, d), dtype=torch.uint8, device="cuda")
+    for over in ("dh", "dy"):
+        b = {m: c[m].clone() for m in ("dh", "dy")}
+        g, e = torch.empty_like(dg), torch.empty_like(db)
+        L.moe_layer_norm_bwd(R, d, mt, b["dy"], o["h"], None, None, o["mean"], o["rstd"], c["gamma"], b["dh"], b[over], g, e, ws, ws.numel())
+        assert status(L) == 0 and torch.equal(b[over], dx) and torch.equal(g, dg) and torch.equal(e, db)

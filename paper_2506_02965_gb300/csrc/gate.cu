@@ -100,9 +100,10 @@ template <bool SIG> __device__ __forceinline__ float score_of(float z, float m, 
 // KEY_RANGE (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
 // the top down, and bit 31; an expert's 255 - id below, so that equal ones come in the order of their ids. Two
 // keys of the exact order can come out the other way round only within KEY_SURE: a fast sigmoid is off by
-// s (1 - s) (2^-22 + |z| 2^-24) + 2^-23 < 2.5e-7, a unit, and the exact one by half of that, the sums with the
-// bias by 2^-24 of themselves on both sides; the roundings here are 3 units. (Keys past the range come out equal, and so not
-// sure.) FLOOR: no finite key in the lowest 16 units, which are left to those out of reach.
+// s (1 - s) (2^-22 + |z| 2^-24) + 2^-23 < 2.5e-7, a unit, and the exact one by half of that, and their sums with the
+// bias, below 4, can fall a spacing of at most a unit apart: 2.8 units a key; the roundings here are 3 for two keys. Past 4
+// sigmoid keys are not sure (fine_top), as they lie on a coarser grid than the units; logits are exact. (Keys past the
+// range come out equal, and so not sure.) FLOOR: no finite key in the lowest 16 units, which are left to those out of reach.
 template <bool SIG, bool FLOOR> __device__ __forceinline__ uint32_t sort_key(float key, float top, int id) {
     constexpr float RANGE = SIG ? 2.f : 16.f;
     float t = __saturatef(fmaf(key - top, 1.f / RANGE, 1.f));
@@ -110,6 +111,13 @@ template <bool SIG, bool FLOOR> __device__ __forceinline__ uint32_t sort_key(flo
     return __float_as_uint(fmaf(t, 16777214.f, 16777216.f)) * 256u + (uint32_t)(255 - id);
 }
 constexpr uint32_t KEY_SURE = 9u << 8;
+// Sums of two keys, of groups: 11 units for four sigmoid keys, two for each exact sum's own rounding (for logits below 80
+// four), 6 here.
+constexpr int SUM_SURE = 27;
+// The top of the sort keys' range, past every key where they are on a coarser grid than that, so that none is sure
+template <bool SIG> __device__ __forceinline__ float fine_top(float top, bool sums) {
+    return (SIG ? fabsf(top - 1.f) < 3.f : !sums || fabsf(top) < 64.f) ? fmaxf(top, -3e38f) : 3e38f;
+}
 constexpr uint32_t KEY_OUT = 0x80000000u;  // a key out of reach, with its 255 - id
 __device__ __forceinline__ int key_units(uint32_t u) { return (int)(u >> 8) & 0x7fffff; }
 
@@ -283,7 +291,7 @@ __global__ void __launch_bounds__(GT_THREADS, gate_resident(NV)) gate_kernel(con
                     most_key = b[0];
 #pragma unroll
                     for (int i = 1; i < NV; ++i) most_key = fmaxf(most_key, b[i]);
-                    most_key = 1.f + lanes_maxf<LPT>(most_key);
+                    most_key = fine_top<true>(1.f + lanes_maxf<LPT>(most_key), true);
                 }
             }
             if (clean) {
@@ -307,9 +315,8 @@ __global__ void __launch_bounds__(GT_THREADS, gate_resident(NV)) gate_kernel(con
             top = key[0];
 #pragma unroll
             for (int i = 1; i < NV; ++i) top = fmaxf(top, key[i]);
-            top = lanes_maxf<LPT>(top);
+            top = fine_top<false>(lanes_maxf<LPT>(top), a.top_groups < a.groups);
         }
-        top = fmaxf(top, -3.4e38f);
         // the lane's KT largest, sorted, and the largest of its others; 0 where there is no expert
         uint32_t v[KT], rest = 0;
         {
@@ -342,7 +349,7 @@ __global__ void __launch_bounds__(GT_THREADS, gate_resident(NV)) gate_kernel(con
             // groups by the units of their best keys, those out of reach below in their order
             uint32_t b1 = v[0], b2 = v[1];
             group_best(b1, b2, lpg);
-            constexpr int NEAR = 2 * (int)(KEY_SURE >> 8);
+            constexpr int NEAR = SUM_SURE;
             const int n1 = key_units(b1), n2 = a.group_top == 2 ? key_units(b2) : n1;
             const bool gone = !clean && min(n1, n2) == 0;
             const int mine = gone ? -2 * NEAR * grp : 1 + NEAR + n1 + (a.group_top == 2 ? n2 : 0);

@@ -358,3 +358,36 @@ def test_picks_of_close_equal_and_crowded_keys(L, E, k, G, top, best, T, sigmoid
         bad = (idx != want).any(1)
         assert not bad.any(), (int(bad.sum()), sorted(set(kind[bad].tolist())), idx[bad][:2].tolist(), want[bad][:2].tolist())
         assert torch.equal(torch.bincount(idx.flatten().long(), minlength=E), counts[0].long())
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,k,G,top,best", [(256, 8, 8, 4, 2), (64, 6, 1, 1, 1), (32, 2, 4, 2, 2)])
+def test_picks_under_large_biases_and_logits(L, E, k, G, top, best, sigmoid):
+    """Keys whose own spacing is coarser than the networks' units: a bias of 5 to 3000 (scores rounded to 5e-7 to 2e-4 in the
+    sum, many equal), logits of thousands (sums of two rounded again): exact picks all the same."""
+    T = 4001
+    gen = torch.Generator(device="cuda").manual_seed(E + k)
+    z = torch.randn(T, E, generator=gen, device="cuda")
+    for size in (5.0, 9.0, 40.0, 3000.0):
+        for sign in (1, -1):
+            b = sign * size + 0.01 * torch.randn(1, E, generator=gen, device="cuda")
+            zz = z if sigmoid else (z * size * 0.3 + sign * size)
+            _, _, _, idx, _, _, _ = run(L, T, E, k, zz, b, sigmoid, G, top, best)
+            want = exact_by_sorting(L, zz, b, k, sigmoid, G, top, best)
+            assert torch.equal(idx, want), (size, sign, int((idx != want).any(1).sum()))
+
+
+@pytest.mark.parametrize("T", [1, 7, 8, 9, 31, 32, 33, 64, 65, 127, 128, 129, 255, 256, 257, 300, 511, 512, 513])
+@pytest.mark.parametrize("E,k,P", [(256, 8, 1), (256, 8, 4), (64, 6, 2), (16, 2, 64), (20, 3, 3), (250, 4, 5)])
+def test_counts_of_every_batch_size(L, T, E, k, P):
+    """One CTA or several, one party or several: the counts of each party, over buffers that held something else."""
+    gen = torch.Generator(device="cuda").manual_seed(T * 7 + E + P)
+    z, b = torch.randn(T, E, generator=gen, device="cuda"), 0.1 * torch.randn(P, E, generator=gen, device="cuda")
+    cut = sorted([0, T] + [int(v) for v in torch.randint(0, T + 1, (P - 1,), generator=torch.Generator().manual_seed(T))])
+    _, _, _, idx, w, counts, _ = run(L, T, E, k, z, b, True, normalize=1, po=cut if P > 1 else None)
+    rows = torch.cat([torch.full((cut[p + 1] - cut[p],), p, device="cuda") for p in range(P)]).long()
+    key = 1.0 / (1.0 + torch.exp(-z)) + b[rows]
+    want = torch.sort(key, dim=1, descending=True, stable=True).indices[:, :k].int()
+    assert torch.equal(idx, want)
+    n = torch.zeros(P * E, dtype=torch.int64, device="cuda").index_add_(0, (rows[:, None] * E + idx).flatten(), torch.ones(T * k, dtype=torch.int64, device="cuda"))
+    assert torch.equal(counts.flatten().long(), n)

@@ -13,8 +13,8 @@
 // tokens; experts too close (one in 1000) by the exact keys of those few against each other, or, where they are
 // more than 24 (equal keys), by a whole warp, one pick after the other.
 // What bounds the forward is the chain of a token's instructions (370 a token of 256 experts; issue slots half busy with the
-// 16 warps an SM that 128 registers leave), not the row's one read: 65536 tokens, 256 experts, 8 groups, bias 39.6 us,
-// without groups and bias 30.1 (the read: 10.5); rounds of "largest left" in a warp per token with exact scores 94.7.
+// 16 warps an SM that 128 registers leave), not the row's one read: 65536 tokens, 256 experts, 8 groups, bias 41.5 us,
+// without groups and bias 30.6 (the read: 10.5); rounds of "largest left" in a warp per token with exact scores 94.7.
 // Also measured: keeping only keys above a floor, the k-th largest of the lanes' largest, and ranking those (16 keys a lane):
 // 47 us against 44 of the networks, without groups 33 against 38, 20 against 15 for 64 experts and 11 against 9 for 16;
 // the next rows copied ahead to shared memory: 44 (the reads back cost more than the wait).
@@ -99,11 +99,12 @@ template <bool SIG> __device__ __forceinline__ float score_of(float z, float m, 
 // Keys for sorting: the distance of a key below `top` (no key is above it), in units of KEY_RANGE / 2^23 up to
 // KEY_RANGE (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
 // the top down, and bit 31; an expert's 255 - id below, so that equal ones come in the order of their ids. Two
-// keys of the exact order can come out the other way round only within KEY_SURE: a fast sigmoid is off by
-// s (1 - s) (2^-22 + |z| 2^-24) + 2^-23 < 2.5e-7, a unit, and the exact one by half of that, and their sums with the
-// bias, below 4, can fall a spacing of at most a unit apart: 2.8 units a key; the roundings here are 3 for two keys. Past 4
-// sigmoid keys are not sure (fine_top), as they lie on a coarser grid than the units; logits are exact. (Keys past the
-// range come out equal, and so not sure.) FLOOR: no finite key in the lowest 16 units, which are left to those out of reach.
+// keys of the exact order can come out the other way round only within KEY_SURE. In units, for a sigmoid key: the fast
+// score is off by s (1 - s) (2^-22 + |z| 2^-24) + 1.5 2^-23 s, at most 0.85, the exact one by 0.55, and their sums with the
+// bias, below 4, can fall a spacing of at most 1 apart; the three roundings here are 1.25: 3.65 a key, 7.3 for two. Past 4
+// sigmoid keys are not sure (fine_top), as they lie on a coarser grid than the units. Logits are exact: the roundings, 1.5 a
+// key. (Keys past the range come out equal, and so not sure.) FLOOR: no finite key in the lowest 16 units, which are left
+// to those out of reach.
 template <bool SIG, bool FLOOR> __device__ __forceinline__ uint32_t sort_key(float key, float top, int id) {
     constexpr float RANGE = SIG ? 2.f : 16.f;
     float t = __saturatef(fmaf(key - top, 1.f / RANGE, 1.f));
@@ -111,9 +112,9 @@ template <bool SIG, bool FLOOR> __device__ __forceinline__ uint32_t sort_key(flo
     return __float_as_uint(fmaf(t, 16777214.f, 16777216.f)) * 256u + (uint32_t)(255 - id);
 }
 constexpr uint32_t KEY_SURE = 9u << 8;
-// Sums of two keys, of groups: 11 units for four sigmoid keys, two for each exact sum's own rounding (for logits below 80
-// four), 6 here.
-constexpr int SUM_SURE = 27;
+// Sums of two keys, of groups: 7.3 units for two sigmoid keys and 1 for the exact sum's own rounding below 8, 16.6 for two
+// sums; 3 and 4 for two logits below 80, 14.
+constexpr int SUM_SURE = 18;
 // The top of the sort keys' range, past every key where they are on a coarser grid than that, so that none is sure
 template <bool SIG> __device__ __forceinline__ float fine_top(float top, bool sums) {
     return (SIG ? fabsf(top - 1.f) < 3.f : !sums || fabsf(top) < 64.f) ? fmaxf(top, -3e38f) : 3e38f;
@@ -275,11 +276,21 @@ __global__ void __launch_bounds__(GT_THREADS, gate_resident(NV)) gate_kernel(con
             sum = lanes_sum<LPT>(sum);
             inv = sum == 0.f ? 0.f : 1.f / sum;
         }
-        if (a.scores && on) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < slots.cnt)
-                    a.scores[t * E + first + slots.at(i)] = key[i] > NINF ? score_of<SIG>(key[i], m, inv) : 0.f;
+        if (a.scores && on) {  // (rolled loops here and below, which read the row again: the kernel's code stays small)
+            float* out = a.scores + t * E + first;
+#pragma unroll 1
+            for (int i = 0; i < slots.cnt; i += VEC ? 4 : 1) {
+                if constexpr (VEC) {
+                    const float4 z = *reinterpret_cast<const float4*>(row + slots.at(i));
+                    auto of = [&](float x) { return x > NINF ? score_of<SIG>(x, m, inv) : 0.f; };
+                    const float4 o = make_float4(of(z.x), of(z.y), of(z.z), of(z.w));
+                    if (a.scores_vec) *reinterpret_cast<float4*>(out + slots.at(i)) = o;
+                    else out[slots.at(i)] = o.x, out[slots.at(i) + 1] = o.y, out[slots.at(i) + 2] = o.z, out[slots.at(i) + 3] = o.w;
+                } else {
+                    const float z = row[slots.at(i)];
+                    out[slots.at(i)] = z > NINF ? score_of<SIG>(z, m, inv) : 0.f;
+                }
+            }
         }
         {
             float b[NV];
@@ -361,16 +372,17 @@ __global__ void __launch_bounds__(GT_THREADS, gate_resident(NV)) gate_kernel(con
             }
             const bool sure = close == 1 && (gone || min(n1, n2) >= 32);  // (not at the end of the range)
             if (__any_sync(0xffffffffu, on && !sure && grp < a.groups)) {  // two groups too close: by exact keys
-                float z[NV], c1 = NINF, c2 = NINF;
-                slots.template load<NV>(row, on, NINF, z);
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    float x = SIG ? score_of<true>(z[i], 0.f, 1.f) : z[i];
-                    if (bias && i < slots.cnt) x = __fadd_rn(x, bias[slots.at(i)]);
-                    x = z[i] > NINF ? x : NINF;
+                float c1 = NINF, c2 = NINF;
+#pragma unroll 8
+                for (int i = 0; i < slots.cnt; ++i) {
+                    const float z = on ? row[slots.at(i)] : NINF;
+                    float x = SIG ? score_of<true>(z, 0.f, 1.f) : z;
+                    if (bias) x = __fadd_rn(x, bias[slots.at(i)]);
+                    x = z > NINF ? x : NINF;
                     c2 = fmaxf(c2, fminf(c1, x));
                     c1 = fmaxf(c1, x);
                 }
+                __syncwarp();
                 group_best(c1, c2, lpg);
                 const float sum = a.group_top == 2 ? c1 + c2 : c1;
                 rank = 0;
@@ -654,8 +666,10 @@ static cudaError_t launch_gate_t(const GateArgs& a, int lpg, cudaStream_t s) {
 // Lanes per token: the fewest (8, 16, 32) that give every group a lane and hold the pool with at
 // most 32 keys a lane, or 8 while even that leaves every warp resident: fewer lanes a token are fewer
 // instructions, more are a shorter chain of them (E = 256, 8 groups: 65536 tokens 39.6 us with 32 keys a lane, 43.8 with
-// 16, 66 with 8; 2999 tokens 15.6, 11.7 and 8.6 in an earlier state of the kernel).
-cudaError_t launch_gate(const GateArgs& a, cudaStream_t s) {
+// 16, 66 with 8, 2999 tokens 15.6, 11.7 and 8.6, in earlier states of the kernel).
+cudaError_t launch_gate(const GateArgs& a0, cudaStream_t s) {
+    GateArgs a = a0;
+    a.scores_vec = (uintptr_t)a.scores % 16 == 0;
     if (a.T == 0) return cudaMemsetAsync(a.counts, 0, sizeof(int32_t) * a.P * a.E, s);
     const int Gp = pow2_ceil(a.groups), gs = a.E / a.groups;
     auto lanes = [&](int keys) {

@@ -56,6 +56,7 @@ struct GateArgs {
     int32_t* topk_idx;
     float* topk_w;
     int32_t* counts;  // [P,E]
+    bool scores_vec;  // set by the launcher: 16-byte stores of the scores
 };
 struct GateBwdArgs {
     const float* logits;

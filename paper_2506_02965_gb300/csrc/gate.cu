@@ -557,9 +557,13 @@ __global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(const __grid_const
     const float ps = pz > NINF ? score_of<SIG>(pz, m, inv) : 0.f;
     float ds = a.scale * g;
     if (a.normalize) {
+        // a constant added to every pick's g changes nothing, for the weights' sum is the scale: taken from the first
+        // pick's on, the terms that cancel are small, and one pick alone has a gradient of exactly 0, not the roundings
+        // of two equal terms over a sum that may be small
         const float total = lanes_sum<8>(ok ? ps : 0.f);
-        const float inner = lanes_sum<8>(ok ? g * (a.scale * ps) : 0.f);
-        ds = total == 0.f ? 0.f : (ds - inner / total) / total;
+        const float g0 = g - __shfl_sync(0xffffffffu, g, 0, 8);
+        const float inner = lanes_sum<8>(ok ? g0 * ps : 0.f);
+        ds = total == 0.f ? 0.f : a.scale * (g0 - inner / total) / total;
     }
     float dot = 0.f;
     float c[NV];

@@ -391,3 +391,16 @@ def test_counts_of_every_batch_size(L, T, E, k, P):
     assert torch.equal(idx, want)
     n = torch.zeros(P * E, dtype=torch.int64, device="cuda").index_add_(0, (rows[:, None] * E + idx).flatten(), torch.ones(T * k, dtype=torch.int64, device="cuda"))
     assert torch.equal(counts.flatten().long(), n)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("scale", [1.0, 2.5])
+def test_one_renormalised_pick_has_no_gradient(L, sigmoid, scale):
+    """k = 1: the weight is the scale whatever the score, so its gradient is exactly 0."""
+    T, E = 3000, 40
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    z, g = torch.randn(T, E, generator=gen, device="cuda"), torch.randn(T, 1, generator=gen, device="cuda")
+    cfg, r, _, idx, w, _, _ = run(L, T, E, 1, z, None, sigmoid, normalize=1, scale=scale)
+    dz = torch.full_like(z, 7.0)
+    L.moe_gate_bwd(cfg, r, z, idx, g, None, None, dz)
+    assert status(L) == 0 and float((w - scale).abs().max()) <= scale * 2.0**-22 and float(dz.abs().max()) == 0

@@ -399,7 +399,7 @@ moe_status moe_gate_balance(const moe_config* cfg, const int32_t* counts, float 
  *     holds it
  * rows in [0, 2^31), d in [1, 16384] (MOE_ERR_UNSUPPORTED above), any alignment of whole elements;
  * 16-byte aligned buffers take the wide path, rows of whole 16-byte vectors the widest. h and y may
- * be x's or residual's buffers (h and y each another one).
+ * be x's or residual's buffers (h and y each another one); h_q and h_scale hold h all the same.
  */
 moe_status moe_layer_norm_fwd(int64_t rows, int32_t d, moe_dtype dtype, const void* x,
                               const void* residual, const float* gamma, const float* beta, float eps,

@@ -694,23 +694,27 @@ static cudaError_t norm_bwd_launch(NormBwdArgs a, int* ctas, cudaStream_t s) {
 template <typename T> static cudaError_t norm_fwd_t(const NormFwdArgs& a0, cudaStream_t s) {
     constexpr int VW = 16 / (int)sizeof(T);
     NormFwdArgs a = a0;
-    // whole spans per row, or the blocks of the checkpoint are not those of the threads: a pass of its own over h
-    const bool apart = a.q && (a.d % VW || !aligned_to(a.q, VW));
+    const bool spans = aligned_to(a.x, 16) && aligned_to(a.res, 16) && aligned_to(a.h, 16) && aligned_to(a.y, 16);
+    // The checkpoint is a pass of its own where rows are no whole spans or the blocks are not those of the threads: of x
+    // before the norm, which may write y over x, or with a residual of h after it
+    const bool apart = a.q && (!spans || a.d % VW || !aligned_to(a.q, VW));
+    auto pack = [&](const void* h) { return launch_ckpt_pack(h, a.rows, a.d, sizeof(T) == 2, a0.q, a.q_scale, s); };
     if (apart) a.q = nullptr;
+    if (apart && !a.res) {
+        const cudaError_t e = pack(a.x);
+        if (e != cudaSuccess) return e;
+    }
     auto run = [&]() -> cudaError_t {
-        if (aligned_to(a.x, 16) && aligned_to(a.res, 16) && aligned_to(a.h, 16) && aligned_to(a.y, 16)) {
+        if (spans) {
 #define MOE_NORM(VPT, TEAM) (a.d % VW ? norm_fwd_launch<T, VPT, TEAM, false>(a, s) : norm_fwd_launch<T, VPT, TEAM, true>(a, s))
             MOE_NORM_TEAM(MOE_NORM);
 #undef MOE_NORM
         }
-        const bool q = a.q != nullptr;
-        a.q = nullptr;
         (void)launch_pdl(norm_fwd_any_kernel<T>, dim3((unsigned)std::min<int64_t>(a.rows, 4 * (int64_t)sm_count())), dim3(NA_THREADS), 0, s, a);
-        const cudaError_t e = cudaGetLastError();
-        return e != cudaSuccess || !q ? e : launch_ckpt_pack(a.res ? a.h : a.x, a.rows, a.d, sizeof(T) == 2, a0.q, a.q_scale, s);
+        return cudaGetLastError();
     };
     const cudaError_t e = run();
-    return e != cudaSuccess || !apart ? e : launch_ckpt_pack(a.res ? a.h : a.x, a.rows, a.d, sizeof(T) == 2, a0.q, a.q_scale, s);
+    return e == cudaSuccess && apart && a.res ? pack(a.h) : e;
 }
 
 cudaError_t launch_norm_fwd(int64_t rows, int d, bool bf16, const void* x, const void* res, const float* gamma, const float* beta,

@@ -297,3 +297,30 @@ def test_in_place(L, R, d, name):
         g, e = torch.empty_like(dg), torch.empty_like(db)
         L.moe_layer_norm_bwd(R, d, mt, b["dy"], o["h"], None, None, o["mean"], o["rstd"], c["gamma"], b["dh"], b[over], g, e, ws, ws.numel())
         assert status(L) == 0 and torch.equal(b[over], dx) and torch.equal(g, dg) and torch.equal(e, db)
+
+
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+@pytest.mark.parametrize("R,d", [(700, 512), (601, 333), (60, 130), (2, 16383)])
+@pytest.mark.parametrize("off", ["", "x", "q"])
+def test_checkpoint_of_x_when_y_lies_over_it(L, R, d, name, off):
+    """Without a residual the stored h is x: its checkpoint and y are the same bits whether y is another buffer or x's own,
+    at widths of whole 16-byte spans and others, with x or h_q off their alignment or not."""
+    c = case(R, d, name, 5 * R + d, residual=False)
+    mt = L.MOE_BF16 if name == "bf16" else L.MOE_F32
+    q, scale = torch.empty(R, d, dtype=torch.int8, device="cuda"), torch.empty(R, -(-d // 128), device="cuda")
+    L.moe_ckpt_pack(R, d, mt, c["x"], q, scale)
+
+    def shifted(dt, by):
+        return torch.zeros(R * d + by, dtype=dt, device="cuda")[by:].view(R, d)
+
+    got = []
+    for over in (False, True):
+        x = shifted(dtype_of(name), 1 if off == "x" else 0)
+        x.copy_(c["x"])
+        y = x if over else torch.empty_like(c["x"])
+        qq, ss = shifted(torch.int8, 1 if off == "q" else 0), torch.zeros_like(scale)
+        mean, rstd = torch.empty(R, device="cuda"), torch.empty(R, device="cuda")
+        L.moe_layer_norm_fwd(R, d, mt, x, None, c["gamma"], c["beta"], EPS, None, y, mean, rstd, qq, ss)
+        assert status(L) == 0 and torch.equal(qq, q) and torch.equal(ss, scale), over
+        got.append((y, mean, rstd))
+    assert all(torch.equal(a, b) for a, b in zip(*got))

@@ -5,7 +5,8 @@ Output :  LN_out(h_n + m_n), with h_1 = x + 0.
 
 Every block routes by the gating rule of the stack (``_lib.make_gate_rule``) with a balance bias of
 its own in place of an auxiliary loss, and runs its experts through one ``MoELayer`` whose
-buffers all blocks share. What a block keeps for its backward is in 8 bits: its hidden states
+scratch buffers all blocks share; a pass lends the layer the blocks' weights and tables and takes
+them back. What a block keeps for its backward is in 8 bits: its hidden states
 h, the experts' [G|U] and their outputs (one byte a value and four per 128 of them), beside the
 norm's statistics, the router logits and the picks. The backward makes y and the permuted rows anew
 from h, the activations from [G|U], and adds up the gradients in the order of the calls:
@@ -15,6 +16,8 @@ from h, the activations from [G|U], and adds up the gradients in the order of th
             -> moe_gate_bwd -> moe_dispatch_bwd -> moe_layer_norm_bwd
 """
 from __future__ import annotations
+
+from contextlib import contextmanager
 
 import torch
 
@@ -95,10 +98,26 @@ class PreNormMoE:
         # hidden states in flight, their gradient, dA
         self._h = [torch.empty_like(self.out) for _ in range(2)]
         self._dh = [torch.empty_like(self.out) for _ in range(2)]
-        self._y = lay.x  # the layer's input buffer holds the normed states
+        # the normed states and the layer's output: not lay.x and lay.out, in which a caller may hold x
+        self._y, self._m = torch.empty_like(lay.x), torch.empty_like(lay.out)
         self._dact = torch.empty_like(lay.act)
         self.ws_bytes = L.moe_layer_norm_workspace_size(T, d)
         self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+
+    _LENT = ("x", "out", "w_router", "w1", "w2", "dw1", "dw2", "topk_idx", "topk_w", "counts", "logits")
+
+    @contextmanager
+    def _lent(self):
+        """The layer for one pass: on the stack's buffers and, block by block (``_use``), their weights and tables; its own
+        ones are back afterwards."""
+        lay = self.layer
+        own = {name: getattr(lay, name) for name in self._LENT}
+        lay.x, lay.out = self._y, self._m
+        try:
+            yield lay
+        finally:
+            for name, t in own.items():
+                setattr(lay, name, t)
 
     def _use(self, b):
         """The layer runs on block b's weights and tables."""
@@ -109,8 +128,11 @@ class PreNormMoE:
     def forward(self, x, stream=None):
         """x [T,d] device tensor of the layer's dtype (read only) -> self.out."""
         s = stream if stream is not None else torch.cuda.current_stream()
-        sh, lay = self.shape, self.layer
-        T, d = sh.T, sh.d_model
+        with self._lent() as lay:
+            return self._forward(x, lay, s)
+
+    def _forward(self, x, lay, s):
+        T, d = self.shape.T, self.shape.d_model
         h, m = x, None
         for i, b in enumerate(self.blocks):
             self._use(b)
@@ -134,8 +156,11 @@ class PreNormMoE:
         """dout [T,d]: the gradient of self.out. Writes every block's gradients and updates its balance
         bias from the batch's counts; returns the gradient of x."""
         s = stream if stream is not None else torch.cuda.current_stream()
-        sh, lay = self.shape, self.layer
-        T, d = sh.T, sh.d_model
+        with self._lent() as lay:
+            return self._backward(dout, lay, s)
+
+    def _backward(self, dout, lay, s):
+        T, d = self.shape.T, self.shape.d_model
         dh = self._dh[0]
         L.moe_layer_norm_bwd(T, d, self.dtype, dout, None, self.h_out.q, self.h_out.scale, self.mean, self.rstd, self.gamma, None,
                              dh, self.dgamma, self.dbeta, self.workspace, self.ws_bytes, stream=s)

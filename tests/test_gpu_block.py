@@ -218,3 +218,37 @@ def test_no_tokens(L):
     net.check_status()
     for b, v in zip(net.blocks, bias):
         assert all(float(g.float().abs().max()) == 0 for g in b.grads().values()) and torch.equal(b.balance_bias, v)
+
+
+@pytest.mark.parametrize("which", ["x", "out"])
+@pytest.mark.parametrize("n", [1, 2, 3])
+def test_input_in_the_layers_own_buffers(L, n, which):
+    """x may lie in the input or the output buffer of the stack's layer: the same bits as from a buffer of its own, and x as it was."""
+    sh = mi.MoEShape("b", 130, 128, 8, 128, 2, "bf16", normalize_topk=1)
+    net, x, dout = build(sh, n, L.make_gate_rule(L.MOE_SCORE_SIGMOID), 17)
+    bias = [b.balance_bias.clone() for b in net.blocks]
+    out, dx = net.forward(x).clone(), net.backward(dout).clone()
+    grads = [{m: g.clone() for m, g in b.grads().items()} for b in net.blocks]
+    for b, v in zip(net.blocks, bias):
+        b.balance_bias.copy_(v)
+    buf = getattr(net.layer, which)
+    buf.copy_(x)
+    assert torch.equal(net.forward(buf), out) and torch.equal(net.backward(dout), dx)
+    net.check_status()
+    assert all(torch.equal(g, grads[i][m]) for i, b in enumerate(net.blocks) for m, g in b.grads().items())
+    assert torch.equal(buf, x)
+
+
+def test_the_layers_own_weights_are_not_the_blocks(L):
+    """A pass lends the layer the blocks' weights and tables and takes them back: what a caller puts into the layer between two
+    passes does not reach a block."""
+    sh = mi.MoEShape("b", 40, 128, 8, 128, 2, "bf16", normalize_topk=1)
+    net, x, dout = build(sh, 2, L.make_gate_rule(L.MOE_SCORE_SIGMOID), 18)
+    want = [{m: p.clone() for m, p in b.params().items()} for b in net.blocks]
+    for step in (lambda: net.forward(x), lambda: net.backward(dout)):
+        step()
+        for t in (net.layer.w_router, net.layer.w1, net.layer.w2, net.layer.dw1, net.layer.dw2):
+            t.fill_(3.0)
+        for b, v in zip(net.blocks, want):
+            assert all(torch.equal(p, v[m]) for m, p in b.params().items())
+    assert all(float((g.float() - 3).abs().max()) > 0 for b in net.blocks for g in b.grads().values())

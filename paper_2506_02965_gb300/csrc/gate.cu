@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(256) gate_zero_kernel(int32_t* counts, int n) 
 
 // dlogits of a token by LPT lanes (several tokens a warp), NV scores a lane in spans of SP = 4 (or single ones).
 // The picks' gradients touch k places of a row: the row is written as if there were none (but for
-// their part in softmax's <ds, s>), then lane j writes pick j's place again. One read and one write of a
+// their part in softmax's <ds, s>), then lane j writes pick j's place again (equal picks the same value). One read and one write of a
 // row; fast exponentials (2^-22 of the result, as the row's sum).
 template <int NV, int LPT, int SP, bool SIG>
 __global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(const __grid_constant__ GateBwdArgs a, __nv_bfloat16* dz16, int EP,
@@ -565,6 +565,21 @@ __global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(const __grid_const
         const float inner = lanes_sum<8>(ok ? g0 * ps : 0.f);
         ds = total == 0.f ? 0.f : a.scale * (g0 - inner / total) / total;
     }
+    // Picks that a caller brings may be equal: what all of an expert add to its score's gradient, in their order in each
+    // of their lanes. Four steps round the eight lanes meet every pair, and a warp that has none goes on.
+    float added = ds;
+    const int pid = ok ? pe : -1 - l;
+    bool twice = false;
+#pragma unroll
+    for (int o = 1; o <= 4; ++o) twice |= __shfl_sync(0xffffffffu, pid, (l + o) & 7, 8) == pid;
+    if (__any_sync(0xffffffffu, twice)) {
+        added = 0.f;
+        for (int j = 0; j < k; ++j) {
+            const int id = __shfl_sync(0xffffffffu, pid, j, 8);
+            const float d = __shfl_sync(0xffffffffu, ds, j, 8);
+            added += id == pid ? d : 0.f;
+        }
+    }
     float dot = 0.f;
     float c[NV];
 #pragma unroll
@@ -613,7 +628,7 @@ __global__ void __launch_bounds__(GT_THREADS) gate_bwd_kernel(const __grid_const
         for (int e = NV * LPT + l; e < EP; e += LPT) dz16[t * EP + e] = __float2bfloat16_rn(0.f);
     __syncwarp();  // the picks' places are written after the row
     if (ok) {
-        const float o = grad(SIG ? pz : ps, pa + ds);
+        const float o = grad(SIG ? pz : ps, pa + added);
         a.dlogits[t * E + pe] = o;
         if (dz16) dz16[t * EP + pe] = __float2bfloat16_rn(o);
     }

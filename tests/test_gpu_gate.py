@@ -404,3 +404,48 @@ def test_one_renormalised_pick_has_no_gradient(L, sigmoid, scale):
     dz = torch.full_like(z, 7.0)
     L.moe_gate_bwd(cfg, r, z, idx, g, None, None, dz)
     assert status(L) == 0 and float((w - scale).abs().max()) <= scale * 2.0**-22 and float(dz.abs().max()) == 0
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("normalize", [0, 1])
+@pytest.mark.parametrize("E,k", [(24, 4), (25, 8), (40, 3), (250, 8), (256, 2), (8, 8)])
+def test_equal_picks_add_up(L, sigmoid, normalize, E, k):
+    """Picks that a caller brings may name an expert several times: its logit's gradient is that of their sum, and so are the
+    router's products. k equal picks add k terms of the bound of one; the products' operands are rounded to bf16."""
+    T, d, scale = 333, 128, 1.5
+    gen = torch.Generator(device="cuda").manual_seed(E + k)
+    z, g = torch.randn(T, E, generator=gen, device="cuda"), torch.randn(T, k, generator=gen, device="cuda")
+    z[torch.rand(T, E, generator=gen, device="cuda") < 0.1] = -float("inf")
+    aux = 0.1 * torch.rand(1, E, generator=gen, device="cuda")
+    idx = torch.randint(0, E, (T, k), generator=gen, device="cuda", dtype=torch.int32)
+    idx[::2] = idx[::2] % 3  # few experts, so that most of these picks are equal ones
+    idx[::5] = idx[::5, :1]  # all of a token
+    cfg = L.make_config(T, d, E, 128, k, normalize_topk=normalize)
+    r = rule(L, sigmoid, 1, 1, 1, scale)
+    dz = torch.full((T, E), 9.0, device="cuda")
+    L.moe_gate_bwd(cfg, r, z, idx, g, aux, None, dz)
+    assert status(L) == 0
+    zh, gh, ah, ih, dzh = (t.double().cpu().numpy() for t in (z, g, aux[0], idx, dz))
+    for t in range(T):
+        I = ih[t].astype(int)
+        zt, s = scores(zh[t], sigmoid)
+        S = s[I].sum() if normalize else 1.0
+        add = scale * gh[t]
+        if normalize:
+            w = scale * s[I] / S if S > 0 else np.zeros(k)
+            add = (add - (gh[t] * w).sum()) / S if S > 0 else np.zeros(k)
+        ds = ah.copy()
+        np.add.at(ds, I, add)
+        with np.errstate(all="ignore"):
+            ref = ds * s / (1 + np.exp(zt)) if sigmoid else s * (ds - (ds * s).sum())
+        size = scale * np.abs(gh[t]).max() * (2 / S if normalize and S > 0 else 1) + np.abs(ah).max()
+        assert (np.abs(dzh[t] - ref) <= 256 * k * U * size).all(), (t, I, np.abs(dzh[t] - ref).max(), size)
+    x, wr = torch.randn(T, d, generator=gen, device="cuda").bfloat16(), torch.randn(1, E, d, generator=gen, device="cuda").bfloat16()
+    ws = torch.empty(L.moe_workspace_size(cfg), dtype=torch.uint8, device="cuda")
+    dz2, dw, db, dx = torch.empty_like(dz), torch.empty_like(wr), torch.empty(1, E, device="cuda"), torch.empty_like(x)
+    L.moe_gate_bwd(cfg, r, z, idx, g, aux, None, dz2, x, wr, dw, db, dx, ws, ws.numel())
+    assert status(L) == 0 and torch.equal(dz2, dz)
+    D, X, W = dz.double(), x.double(), wr[0].double()
+    assert ((dw[0].double() - D.T @ X).abs() <= 2.0 ** -7 * (D.abs().T @ X.abs())).all()
+    assert ((dx.double() - D @ W).abs() <= 2.0 ** -7 * (D.abs() @ W.abs())).all()
+    assert ((db[0].double() - D.sum(0)).abs() <= 1e-5 * D.abs().sum(0) + 1e-9).all()

@@ -297,7 +297,8 @@ def moe_dispatch_bwd(cfg, dx_perm, slot_of, dx_router, dx_sh, dx, stream=None):
 
 # ------------------------------------------------------------------ operators around the layer
 # These also check what a tensor is before its address is taken: on the GPU, dense, of the right
-# element type and as many elements as the call's sizes say. The kinds: MOE_F32, MOE_BF16 and
+# element type and as many elements as the call's sizes say (moe_expert_ffn_bwd_ckpt's: at least as many; a
+# workspace: of at least the bytes that the call is told). The kinds: MOE_F32, MOE_BF16 and
 _I32T, _I8T = 2, 3
 _kinds = None
 
@@ -332,6 +333,23 @@ def _arr(fn, name, t, kind, n):
     except (ImportError, OSError):
         _arr = _check_arr
     return _arr(fn, name, t, kind, n)
+
+
+def _room(fn, name, t, kind, n):
+    """_arr for a buffer that may hold more than n elements."""
+    if t is None or isinstance(t, int):
+        return t
+    return _arr(fn, name, t, kind, max(n, t.numel()))
+
+
+def _work(fn, t, nbytes):
+    """Address of a dense GPU tensor, of any element type, that holds nbytes; an address or None as it is."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.is_cuda and t.is_contiguous() and t.numel() * t.element_size() >= nbytes:
+        return t.data_ptr()
+    raise MoEError(MOE_ERR_INVALID_ARG, fn, f"workspace: expected a dense GPU tensor of {nbytes} bytes, got {tuple(t.shape)} {t.dtype}, "
+                                            f"strides {t.stride()}, on {t.device}")
 
 
 def _dtype_of(fn, dtype):
@@ -384,7 +402,8 @@ def moe_gate_bwd(cfg, rule, logits, topk_idx, dtopk_w, aux_coef, party_offsets, 
                              _arr(fn, "party_offsets", party_offsets, _I32T, Pn + 1), _arr(fn, "dlogits", dlogits, MOE_F32, T * E),
                              _arr(fn, "x", x, dt, T * d), _arr(fn, "w_router", w_router, dt, Pn * E * d),
                              _arr(fn, "dw_router", dw_router, dt, Pn * E * d), _arr(fn, "dbias", dbias, MOE_F32, Pn * E),
-                             _arr(fn, "dx_router", dx_router, dt, T * d), _ptr(workspace), int(workspace_bytes),
+                             _arr(fn, "dx_router", dx_router, dt, T * d),
+                             _work(fn, workspace, workspace_bytes) if dw_router is not None else None, int(workspace_bytes),
                              _stream(stream)), fn)
 
 
@@ -419,7 +438,7 @@ def moe_layer_norm_bwd(rows, d, dtype, dy, h, h_q, h_scale, mean, rstd, gamma, d
                                    _arr(fn, "h_scale", h_scale, MOE_F32, rows * ckpt_blocks(d)), _arr(fn, "mean", mean, MOE_F32, rows),
                                    _arr(fn, "rstd", rstd, MOE_F32, rows), _arr(fn, "gamma", gamma, MOE_F32, d),
                                    _arr(fn, "dh", dh, dt, n), _arr(fn, "dx", dx, dt, n), _arr(fn, "dgamma", dgamma, MOE_F32, d),
-                                   _arr(fn, "dbeta", dbeta, MOE_F32, d), _ptr(workspace), int(workspace_bytes),
+                                   _arr(fn, "dbeta", dbeta, MOE_F32, d), _work(fn, workspace, workspace_bytes), int(workspace_bytes),
                                    _stream(stream)), fn)
 
 
@@ -450,5 +469,23 @@ def moe_ckpt_swiglu_bwd(rows, d_ff, dtype, q, scale, dact, act, dh, stream=None)
 def moe_expert_ffn_bwd_ckpt(cfg, x_perm, offsets, w1, w2, gu_q, gu_scale, dy_perm, dact, act, dh, dx_perm, dw1, dw2, x=None,
                             dout=None, ws1=None, ws2=None, h_gu_sh=None, act_sh=None, dh_sh=None, dx_sh=None, dws1=None,
                             dws2=None, group_expert=None, stream=None):
-    _call("moe_expert_ffn_bwd_ckpt", cfg, x_perm, offsets, w1, w2, gu_q, gu_scale, dy_perm, dact, act, dh, dx_perm, dw1, dw2, x,
-          dout, ws1, ws2, h_gu_sh, act_sh, dh_sh, dx_sh, dws1, dws2, group_expert, stream=stream)
+    fn = "moe_expert_ffn_bwd_ckpt"
+    T, d, E, F, S, Fs, dt = cfg.T, cfg.d_model, cfg.n_experts, cfg.d_ff, cfg.n_shared, cfg.d_ff_shared, _dtype_of(fn, cfg.dtype)
+    TK, some = T * cfg.top_k, T > 0
+
+    # what the call does not use (without tokens all but the weights' gradients, without shared experts theirs) is not looked at
+    def at(name, t, n, kind=dt, used=some):
+        return _room(fn, name, t, kind, n) if used else None
+
+    def sh(name, t, n, used=some):
+        return at(name, t, n, used=S > 0 and used)
+
+    _check(_lib.moe_expert_ffn_bwd_ckpt(
+        cfg, at("x_perm", x_perm, TK * d), at("offsets", offsets, E + 1, _I32T), at("w1", w1, E * 2 * F * d),
+        at("w2", w2, E * d * F), at("gu_q", gu_q, TK * 2 * F, _I8T), at("gu_scale", gu_scale, TK * ckpt_blocks(2 * F), MOE_F32),
+        at("dy_perm", dy_perm, TK * d), at("dact", dact, TK * F), at("act", act, TK * F), at("dh", dh, TK * 2 * F),
+        at("dx_perm", dx_perm, TK * d), at("dw1", dw1, E * 2 * F * d, used=True), at("dw2", dw2, E * d * F, used=True),
+        sh("x", x, T * d), sh("dout", dout, T * d), sh("ws1", ws1, S * 2 * Fs * d), sh("ws2", ws2, S * d * Fs),
+        sh("h_gu_sh", h_gu_sh, S * T * 2 * Fs), sh("act_sh", act_sh, S * T * Fs), sh("dh_sh", dh_sh, S * T * 2 * Fs),
+        sh("dx_sh", dx_sh, S * T * d), sh("dws1", dws1, S * 2 * Fs * d, used=True), sh("dws2", dws2, S * d * Fs, used=True),
+        at("group_expert", group_expert, E, _I32T), _stream(stream)), fn)

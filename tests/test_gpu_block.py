@@ -252,3 +252,42 @@ def test_the_layers_own_weights_are_not_the_blocks(L):
         for b, v in zip(net.blocks, want):
             assert all(torch.equal(p, v[m]) for m, p in b.params().items())
     assert all(float((g.float() - 3).abs().max()) > 0 for b in net.blocks for g in b.grads().values())
+
+
+def test_buffers_of_the_expert_backward(L):
+    """Buffers with room to spare give the same bits; too small, strided or of another type are refused before any of them is
+    written, and so is a workspace smaller than its bytes."""
+    T, d, E, F, k = 200, 128, 4, 256, 2
+    cfg, TK, bf = L.make_config(T, d, E, F, k), T * k, torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(3)
+
+    def normal(*s, std=1.0):
+        return torch.empty(*s, device="cuda").normal_(0.0, std, generator=g).to(bf)
+
+    q, sc = torch.empty(TK, 2 * F, dtype=torch.int8, device="cuda"), torch.empty(TK, L.ckpt_blocks(2 * F), device="cuda")
+    L.moe_ckpt_pack(TK, 2 * F, L.MOE_BF16, normal(TK, 2 * F), q, sc)
+    a = {"x_perm": normal(TK, d), "offsets": torch.tensor([0, 70, 70, 250, TK], dtype=torch.int32, device="cuda"),
+         "w1": normal(E, 2 * F, d, std=0.1), "w2": normal(E, d, F, std=0.1), "gu_q": q, "gu_scale": sc, "dy_perm": normal(TK, d)}
+    outs = {"dact": TK * F, "act": TK * F, "dh": TK * 2 * F, "dx_perm": TK * d, "dw1": E * 2 * F * d, "dw2": E * d * F}
+    exact = {m: torch.zeros(n, dtype=bf, device="cuda") for m, n in outs.items()}
+    room = {m: torch.zeros(n + 64, dtype=bf, device="cuda") for m, n in outs.items()}
+    L.moe_expert_ffn_bwd_ckpt(cfg, **a, **exact)
+    L.moe_expert_ffn_bwd_ckpt(cfg, **{m: torch.cat([t.flatten(), t.flatten()[:64]]) for m, t in a.items()}, **room)
+    assert status(L) == 0
+    for m, n in outs.items():
+        assert torch.equal(room[m][:n], exact[m]) and float(room[m][n:].abs().max()) == 0 and float(exact[m].abs().max()) > 0
+        assert torch.isfinite(exact[m].float()).all()
+    for m in [*a, *outs]:
+        t = {**a, **exact}[m]
+        for bad in (t.flatten()[:-1], t.flatten()[::2], t.double()):
+            with pytest.raises(L.MoEError, match=f"{m}: expected a dense GPU tensor"):
+                L.moe_expert_ffn_bwd_ckpt(cfg, **{**a, **room, m: bad})
+    n = L.moe_layer_norm_workspace_size(T, d)
+    rows = [normal(T, d), normal(T, d), None, None, *(torch.zeros(s, device="cuda") for s in (T, T, d)), None, normal(T, d),
+            torch.zeros(d, device="cuda"), None]
+    for bad in (torch.empty(n - 1, dtype=torch.uint8, device="cuda"), torch.empty(n, dtype=torch.uint8),
+                torch.empty(2 * n, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(L.MoEError, match="workspace"):
+            L.moe_layer_norm_bwd(T, d, L.MOE_BF16, *rows, bad, n)
+    L.moe_layer_norm_bwd(T, d, L.MOE_BF16, *rows, torch.empty(-(-n // 4), device="cuda"), n)
+    assert status(L) == 0

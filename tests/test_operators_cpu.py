@@ -128,3 +128,33 @@ def test_argument_checks_in_both_languages():
                 check("f", "x", bad, L.MOE_F32, 32)
             said.append((type(e.value), str(e.value)))
         assert said[0] == said[1]
+
+
+def test_expert_backward_and_workspaces_are_looked_at():
+    """The tensors of the experts' backward from a checkpoint, and workspaces: refused before their address is taken, with
+    what they should have been. What a call does not use is not looked at."""
+    torch = pytest.importorskip("torch")
+    T, d, E, F, k, S, Fs = 8, 128, 4, 256, 2, 1, 128
+    cfg = L.make_config(T, d, E, F, k, n_shared=S, d_ff_shared=Fs)
+    TK = T * k
+    sizes = {"x_perm": TK * d, "offsets": E + 1, "w1": E * 2 * F * d, "w2": E * d * F, "gu_q": TK * 2 * F, "gu_scale": TK * 4,
+             "dy_perm": TK * d, "dact": TK * F, "act": TK * F, "dh": TK * 2 * F, "dx_perm": TK * d, "dw1": E * 2 * F * d,
+             "dw2": E * d * F, "x": T * d, "dout": T * d, "ws1": S * 2 * Fs * d, "ws2": S * d * Fs, "h_gu_sh": S * T * 2 * Fs,
+             "act_sh": S * T * Fs, "dh_sh": S * T * 2 * Fs, "dx_sh": S * T * d, "dws1": S * 2 * Fs * d, "dws2": S * d * Fs,
+             "group_expert": E}
+    kinds = {"offsets": "int32", "group_expert": "int32", "gu_q": "int8", "gu_scale": "float32"}
+    for name, n in sizes.items():
+        say = f"{name}: expected a dense GPU tensor of {n} elements of torch.{kinds.get(name, 'bfloat16')}"
+        with pytest.raises(L.MoEError, match=say):
+            L.moe_expert_ffn_bwd_ckpt(cfg, **{**dict.fromkeys(sizes, 16), name: torch.zeros(n - 1)}, stream=0)
+    small = torch.zeros(4)
+    unused = {m: small if m not in ("dw1", "dw2") else None for m in sizes}
+    with pytest.raises(L.MoEError, match="dw1 is NULL"):
+        L.moe_expert_ffn_bwd_ckpt(L.make_config(0, d, E, F, k), **unused, stream=0)
+    with pytest.raises(L.MoEError, match="workspace: expected a dense GPU tensor of 64 bytes"):
+        L.moe_layer_norm_bwd(4, 64, L.MOE_F32, 16, 16, None, None, 16, 16, 16, None, 16, 16, None, small, 64, stream=0)
+    one, r = L.make_config(8, 128, 64, 128, 4), L.make_gate_rule()
+    with pytest.raises(L.MoEError, match="workspace: expected a dense GPU tensor of 64 bytes"):
+        L.moe_gate_bwd(one, r, 16, 16, 16, None, None, 16, 16, 16, 16, None, 16, small, 64, stream=0)
+    with pytest.raises(L.MoEError, match="come with dw_router"):
+        L.moe_gate_bwd(one, r, 16, 16, 16, None, None, 16, 16, 16, None, 16, None, small, 64, stream=0)

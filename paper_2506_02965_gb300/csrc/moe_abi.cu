@@ -912,10 +912,22 @@ moe_status moe_route_gate(const moe_config* cfg, const moe_gate_rule* rule, cons
     moe_status st = check_cfg(cfg);
     if (st) return st;
     if ((st = check_rule(cfg, rule))) return st;
+    // everything that the call refuses, before its first launch
+    if ((st = check_parties(cfg, party_offsets))) return st;
+    REQUIRE_ELEM(counts, 4);
+    if (cfg->T > 0) {
+        REQUIRE_VEC(x);
+        REQUIRE_VEC(w_router);
+        OPTIONAL_ELEM(router_bias, 4);
+        OPTIONAL_ELEM(balance_bias, 4);
+        REQUIRE_ELEM(logits, 4);
+        REQUIRE_ELEM(scores, 4);
+        REQUIRE_ELEM(topk_idx, 4);
+        REQUIRE_ELEM(topk_w, 4);
+    }
     // the logits of moe_route; its picks and probabilities are overwritten
     st = moe_route(cfg, x, w_router, router_bias, party_offsets, logits, scores, topk_idx, topk_w, counts, stream);
     if (st || cfg->T == 0) return st;
-    OPTIONAL_ELEM(balance_bias, 4);
     return gate_common(cfg, rule, logits, balance_bias, party_offsets, scores, topk_idx, topk_w, counts, (cudaStream_t)stream);
 }
 

@@ -158,3 +158,14 @@ def test_expert_backward_and_workspaces_are_looked_at():
         L.moe_gate_bwd(one, r, 16, 16, 16, None, None, 16, 16, 16, 16, None, 16, small, 64, stream=0)
     with pytest.raises(L.MoEError, match="come with dw_router"):
         L.moe_gate_bwd(one, r, 16, 16, 16, None, None, 16, 16, 16, None, 16, None, small, 64, stream=0)
+
+
+@pytest.mark.parametrize("name", ["x", "w_router", "router_bias", "balance_bias", "logits", "scores", "topk_idx", "topk_w", "counts"])
+def test_route_gate_refuses_before_it_launches(name):
+    """A pointer off its alignment or missing is an invalid argument, not the status of a launch on the way to it."""
+    cfg, r = L.make_config(8, 128, 64, 128, 4), L.make_gate_rule()
+    a = dict(x=16, w_router=16, router_bias=None, balance_bias=None, party_offsets=None, logits=16, scores=16, topk_idx=16, topk_w=16,
+             counts=16)
+    refused(f"{name} is not ", BAD, L.moe_route_gate, cfg, r, *{**a, name: 18}.values())
+    if a[name] is not None:
+        refused(f"{name} is NULL", BAD, L.moe_route_gate, cfg, r, *{**a, name: None}.values())

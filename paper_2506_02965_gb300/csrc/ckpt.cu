@@ -217,7 +217,7 @@ template <typename F> static cudaError_t by_rows(int64_t rows, int64_t units_per
 
 template <typename T, int VW>
 static cudaError_t pack_t(const T* x, int64_t rows, int cols, int8_t* q, float* scale, cudaStream_t s) {
-    const int64_t nb = (cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
+    const int64_t nb = ((int64_t)cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
     constexpr int PER = CkptMap<T, VW>::GROUPS * CK_U;
     return by_rows(rows, nb, [&](int64_t r, int64_t n) {
         (void)launch_pdl(ckpt_pack_kernel<T, VW>, dim3((unsigned)((n * nb + PER - 1) / PER)), dim3(CK_THREADS), 0, s, x + r * cols,
@@ -226,7 +226,7 @@ static cudaError_t pack_t(const T* x, int64_t rows, int cols, int8_t* q, float* 
 }
 template <typename T, int VW>
 static cudaError_t unpack_t(const int8_t* q, const float* scale, int64_t rows, int cols, T* x, cudaStream_t s) {
-    const int64_t nb = (cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
+    const int64_t nb = ((int64_t)cols + CKPT_BLOCK - 1) / CKPT_BLOCK;
     constexpr int PER = CkptMap<T, VW>::GROUPS * CK_U;
     return by_rows(rows, nb, [&](int64_t r, int64_t n) {
         (void)launch_pdl(ckpt_unpack_kernel<T, VW>, dim3((unsigned)((n * nb + PER - 1) / PER)), dim3(CK_THREADS), 0, s, q + r * cols,

@@ -184,3 +184,28 @@ def test_nothing_to_do(L):
     L.moe_ckpt_unpack(0, 8, L.MOE_BF16, None, None, None)
     L.moe_ckpt_swiglu_bwd(0, 8, L.MOE_BF16, None, None, None, None, None)
     assert status(L) == 0
+
+
+@pytest.mark.parametrize("C", [2 ** 31 - 1, 2 ** 31 - 120])
+def test_the_widest_rows(L, C):
+    """A row of nearly 2^31 columns: its first and last blocks are those of short rows, all others zeros."""
+    n = 300
+    x = torch.zeros(1, C, dtype=torch.bfloat16, device="cuda")
+    head = torch.randn(1, n, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").bfloat16()
+    cut = C // B * B - B  # the last whole block and the one after it
+    x[:, :n], x[:, cut:] = head, head[:, :C - cut]
+    q, s = pack(L, x)
+    qh, sh = pack(L, head)
+    qt, st = pack(L, head[:, :C - cut].contiguous())
+    assert torch.equal(q[:, :n], qh) and torch.equal(s[:, :3], sh) and torch.equal(q[:, cut:], qt) and torch.equal(s[:, -2:], st)
+    assert int(q[:, n:cut].abs().max()) == 0 and float(s[:, 3:-2].abs().max()) == 0
+    x.fill_(1.0)
+    L.moe_ckpt_unpack(1, C, L.MOE_BF16, q, s, x)
+    held = torch.empty_like(head)
+    L.moe_ckpt_unpack(1, n, L.MOE_BF16, qh, sh, held)
+    assert status(L) == 0 and torch.equal(x[:, :n], held) and float(x[:, n:cut].abs().max()) == 0
+    back = torch.empty(1, C - cut, dtype=torch.bfloat16, device="cuda")
+    L.moe_ckpt_unpack(1, C - cut, L.MOE_BF16, qt, st, back)
+    assert torch.equal(x[:, cut:], back)
+    del x, q, s
+    torch.cuda.empty_cache()

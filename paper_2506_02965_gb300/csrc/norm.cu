@@ -674,6 +674,20 @@ static cudaError_t norm_bwd_launch(NormBwdArgs a, int* ctas, cudaStream_t s) {
     return cudaGetLastError();
 }
 
+// Rows of whole spans end at kNormMaxWidth elements, in bf16 before the largest team's (the one below holds that many)
+template <typename T, int VPT, int TEAM> constexpr bool whole_rows() { return VPT * TEAM / 2 * (16 / (int)sizeof(T)) < kNormMaxWidth; }
+
+template <typename T, int VPT, int TEAM> static cudaError_t norm_fwd_rows(const NormFwdArgs& a, cudaStream_t s) {
+    if constexpr (whole_rows<T, VPT, TEAM>())
+        if (a.d % (16 / (int)sizeof(T)) == 0) return norm_fwd_launch<T, VPT, TEAM, true>(a, s);
+    return norm_fwd_launch<T, VPT, TEAM, false>(a, s);
+}
+template <typename T, int VPT, int TEAM, bool Q> static cudaError_t norm_bwd_rows(const NormBwdArgs& a, int* ctas, cudaStream_t s) {
+    if constexpr (whole_rows<T, VPT, TEAM>())
+        if (a.d % (16 / (int)sizeof(T)) == 0) return norm_bwd_launch<T, VPT, TEAM, Q, true>(a, ctas, s);
+    return norm_bwd_launch<T, VPT, TEAM, Q, false>(a, ctas, s);
+}
+
 // The team for rows of d elements: two spans a thread, from 8 threads on. (fp32 rows of 16382 and 16383
 // elements can have 4097 spans: none.)
 #define MOE_NORM_TEAM(LAUNCH)                                            \
@@ -706,7 +720,7 @@ template <typename T> static cudaError_t norm_fwd_t(const NormFwdArgs& a0, cudaS
     }
     auto run = [&]() -> cudaError_t {
         if (spans) {
-#define MOE_NORM(VPT, TEAM) (a.d % VW ? norm_fwd_launch<T, VPT, TEAM, false>(a, s) : norm_fwd_launch<T, VPT, TEAM, true>(a, s))
+#define MOE_NORM(VPT, TEAM) norm_fwd_rows<T, VPT, TEAM>(a, s)
             MOE_NORM_TEAM(MOE_NORM);
 #undef MOE_NORM
         }
@@ -727,13 +741,11 @@ template <typename T> static cudaError_t norm_bwd_t(const NormBwdArgs& a, int* c
     constexpr int VW = 16 / (int)sizeof(T);
     if (aligned_to(a.dy, 16) && aligned_to(a.h, 16) && aligned_to(a.dh, 16) && aligned_to(a.dx, 16) && aligned_to(a.q, VW)) {
         if (a.q) {
-#define MOE_NORM(VPT, TEAM) \
-    (a.d % VW ? norm_bwd_launch<T, VPT, TEAM, true, false>(a, ctas, s) : norm_bwd_launch<T, VPT, TEAM, true, true>(a, ctas, s))
+#define MOE_NORM(VPT, TEAM) norm_bwd_rows<T, VPT, TEAM, true>(a, ctas, s)
             MOE_NORM_TEAM(MOE_NORM);
 #undef MOE_NORM
         }
-#define MOE_NORM(VPT, TEAM) \
-    (a.d % VW ? norm_bwd_launch<T, VPT, TEAM, false, false>(a, ctas, s) : norm_bwd_launch<T, VPT, TEAM, false, true>(a, ctas, s))
+#define MOE_NORM(VPT, TEAM) norm_bwd_rows<T, VPT, TEAM, false>(a, ctas, s)
         MOE_NORM_TEAM(MOE_NORM);
 #undef MOE_NORM
     }

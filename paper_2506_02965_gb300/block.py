@@ -1,4 +1,4 @@
-"""A stack of pre-norm MoE blocks that trains from 8-bit activation checkpoints.
+"""A stack of pre-norm MoE blocks with a backward from 8-bit activation checkpoints.
 
 Block i:  h_i = h_{i-1} + m_{i-1},  y = LN_i(h_i),  m_i = MoE_i(y)
 Output :  LN_out(h_n + m_n), with h_1 = x + 0.
@@ -14,6 +14,8 @@ from h, the activations from [G|U], and adds up the gradients in the order of th
   forward : moe_layer_norm_fwd -> moe_route_gate -> moe_dispatch -> moe_expert_ffn_fwd -> moe_ckpt_pack -> moe_combine_fwd
   backward: moe_ckpt_unpack -> moe_layer_norm_fwd -> moe_dispatch -> moe_combine_bwd -> moe_expert_ffn_bwd_ckpt
             -> moe_gate_bwd -> moe_dispatch_bwd -> moe_layer_norm_bwd
+
+It gives gradients and moves the balance biases; the weights' update is the caller's.
 """
 from __future__ import annotations
 

@@ -1,8 +1,9 @@
 // Activation checkpoints in 8 bits (the blocks of span.cuh): packing, unpacking, and the SwiGLU
 // backward that reads [G|U] from one. Streams, all HBM-bound: of the copy rate, 6781 GB/s, 32768 x 28672 bf16 packs in
-// 412.5 us (1.02), unpacks in 417 (1.01), and its SwiGLU backward takes 661 (1.06); 17994 x 2816 24.3, 24.5 and 37.9 us
-// (0.92 to 0.99). Rows of an odd number of elements move 2 bytes a lane: 20000 x 2002 packs at 0.58, the SwiGLU
-// backward of F = 1001 at 0.61, of 1004 (8 bytes a lane) at 0.77.
+// 412.5 us (1.02), unpacks in 417 (1.01), and its SwiGLU backward takes 660 (1.06); 17994 x 2816 24.3, 24.4 and 37.9 us
+// (0.93 to 0.99). bf16 rows of an odd number of elements move 2 bytes a lane, of an odd number of pairs 4, and a row's last
+// block takes a whole group of lanes: packing 10000 x 5001 0.42 (unpacking 0.56), 200000 x 67 0.24 (0.41), 20000 x 2002
+// 0.58 (0.67); SwiGLU backward of F = 5001 0.63, 1001 0.61, 67 0.39, 1004 (8 bytes a lane) 0.77.
 #include <algorithm>
 #include <initializer_list>
 
@@ -129,8 +130,9 @@ __global__ void __launch_bounds__(CK_THREADS) ckpt_unpack_kernel(const int8_t* _
 
 // SwiGLU backward from the checkpoint of [G|U] (rows of 2F columns in one run of blocks):
 //   s = sigmoid(G), act = G s U, dU = dA G s, dG = dA U s (1 + G (1 - s)).
-// The sigmoid is the fast one (a few 2^-23 of it, far below what 8 bits left of G and U): with full-precision
-// exponentials and quotients their instructions, not HBM, are the bound.
+// The sigmoid is the fast one of both types, off by s (1 - s) (4 + 1.23 |G|) + 3 s units of 2^-24, at most 3.4 (far below what
+// 8 bits left of G and U; the layer's own fp32 epilogue has the full-precision one): with full-precision exponentials
+// and quotients their instructions, not HBM, are the bound.
 // A group of lanes takes 128 columns of G, one block of the checkpoint, and the same of U, which lie in one or two.
 template <int VW> constexpr int swiglu_u() { return VW > 1 ? 2 : 1; }  // such runs of columns in flight per group of lanes
 

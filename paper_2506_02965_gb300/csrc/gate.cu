@@ -11,15 +11,19 @@
 // with the expert in 8 bits below: enough wherever the keys that decide lie further apart than the approximation, which is
 // checked. Two groups too close (one token in 1000 of random ones) are decided by exact keys of their warp's
 // tokens; experts too close (one in 1000) by the exact keys of those few against each other, or, where they are
-// more than 24 (equal keys), by a whole warp, one pick after the other.
+// more than 24 (equal keys), by a whole warp, one pick after the other. So the time depends on the keys: where every token
+// goes that way (all logits equal, as from a router of zeros, or every key coarser than the networks' units, a bias of 3
+// and more beside sigmoid scores), 65536 x 256 takes 292 us with 8 groups and 161 without, not 41.5 and 30.4.
 // What bounds the forward is the chain of a token's instructions (370 a token of 256 experts; issue slots half busy with the
 // 16 warps an SM that 128 registers leave), not the row's one read: 65536 tokens, 256 experts, 8 groups, bias 41.5 us,
-// without groups and bias 30.6 (the read: 10.5); rounds of "largest left" in a warp per token with exact scores 94.7.
+// without groups and bias 30.4 (the read: 10.5); with the scores written too, full-precision ones from a second read of the
+// row, 74 and 51.6. Rounds of "largest left" in a warp per token with exact scores took 94.7.
 // Also measured: keeping only keys above a floor, the k-th largest of the lanes' largest, and ranking those (16 keys a lane):
 // 47 us against 44 of the networks, without groups 33 against 38, 20 against 15 for 64 experts and 11 against 9 for 16;
 // the next rows copied ahead to shared memory: 44 (the reads back cost more than the wait).
 //
-// Backward: one read of the logits, one write of their gradient, HBM-bound (65536 x 256: 25.2 us, 0.81 of the copy rate).
+// Backward: one read of the logits, one write of their gradient, HBM-bound (65536 x 256: 24.9 us, 0.82 of the copy rate; softmax
+// 26.9, 0.76).
 #include <algorithm>
 
 #include "moe_common.cuh"
@@ -66,7 +70,7 @@ template <int N> __device__ __forceinline__ void sort_bitonic(uint32_t* v) {
         for (int i = 0; i < N; ++i)
             if (!(i & h)) cswap(v[i], v[i + h]);
 }
-// any list of N, odd-even merge sort
+// any list of N, Batcher's odd-even merge sort
 template <int N> __device__ __forceinline__ void sort_any(uint32_t* v) {
 #pragma unroll
     for (int p = 1; p < N; p <<= 1)
@@ -100,7 +104,7 @@ template <bool SIG> __device__ __forceinline__ float score_of(float z, float m, 
 // KEY_RANGE (2 for sigmoid scores and their biases: 2.4e-7, 16 for logits: 1.9e-6), in bits 8 to 30 from
 // the top down, and bit 31; an expert's 255 - id below, so that equal ones come in the order of their ids. Two
 // keys of the exact order can come out the other way round only within KEY_SURE. In units, for a sigmoid key: the fast
-// score is off by s (1 - s) (2^-22 + |z| 2^-24) + 1.5 2^-23 s, at most 0.85, the exact one by 0.55, and their sums with the
+// score is off by s (1 - s) (2^-22 + 1.23 |z| 2^-24) + 1.5 2^-23 s, at most 0.85, the exact one by 0.55, and their sums with the
 // bias, below 4, can fall a spacing of at most 1 apart; the three roundings here are 1.25: 3.65 a key, 7.3 for two. Past 4
 // sigmoid keys are not sure (fine_top), as they lie on a coarser grid than the units. Logits are exact: the roundings, 1.5 a
 // key. (Keys past the range come out equal, and so not sure.) FLOOR: no finite key in the lowest 16 units, which are left
@@ -684,8 +688,10 @@ static cudaError_t launch_gate_t(const GateArgs& a, int lpg, cudaStream_t s) {
 
 // Lanes per token: the fewest (8, 16, 32) that give every group a lane and hold the pool with at
 // most 32 keys a lane, or 8 while even that leaves every warp resident: fewer lanes a token are fewer
-// instructions, more are a shorter chain of them (E = 256, 8 groups: 65536 tokens 39.6 us with 32 keys a lane, 43.8 with
-// 16, 66 with 8, 2999 tokens 15.6, 11.7 and 8.6, in earlier states of the kernel).
+// instructions, more are a shorter chain of them. E = 256, sigmoid, 8 groups, bias: 3000 and 3648 tokens with 8 keys a lane
+// 7.2 and 8.1 us, 3649, 4096, 6000 and 9728 with 32 10.1, 11.4, 12.7 and 12.6, the next wave 14.1 (9729) to 17.0 (16384);
+// softmax, one group: 6.6, 7.4 | 8.2, 6.4, 8.0, 7.9 | 11.3, 11.4. At 65536 tokens 32 keys a lane measured 39.6, 16 43.8, 8 66
+// before the kernel had its present form; 16 between the two is not tried.
 cudaError_t launch_gate(const GateArgs& a0, cudaStream_t s) {
     GateArgs a = a0;
     a.scores_vec = (uintptr_t)a.scores % 16 == 0;

@@ -164,7 +164,8 @@ __device__ __forceinline__ float fast_rcp(float x) {
     return y;
 }
 constexpr float LOG2E = 1.4426950408889634f;
-// exp(x), off by 2^-22 + |x| 2^-24 of the result; 1 / (1 + exp(-x)), off by that and 2^-23
+// exp(x), off by 2^-22 + 1.23 |x| 2^-24 of the result (the product's rounding, and 0.23 of it log2(e)'s); 1 / (1 + exp(-x)),
+// off by (1 - the result) times that, 2^-24 and 2^-23 of the result
 __device__ __forceinline__ float fast_exp(float x) { return fast_exp2(x * LOG2E); }
 __device__ __forceinline__ float fast_sigmoid(float x) { return fast_rcp(1.f + fast_exp(-x)); }
 

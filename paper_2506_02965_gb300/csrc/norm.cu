@@ -16,9 +16,13 @@
 //
 // Measured (of the copy rate, 6781 GB/s): 16384 x 4096 bf16 with residual and checkpoint, forward 92.1 us (0.97), backward
 // from the checkpoint 80.3 (0.87); without a residual 47.9 (0.83) and 68.0 (0.87); 8000 x 8192 with one 88.8 and 85.3;
-// 8000 x 4096 fp32 42.7 and 64.4; 60000 x 333 (spans at every shift, a third of a team's idle) 32.4 (0.36) and 39.8
-// (0.44); 4000 x 16384 (one team of 1024 threads an SM, no second one to work while it waits) 85 and 137 (0.4). A CTA per
+// 8000 x 4096 fp32 42.7 and 63.7; 60000 x 333 (spans at every shift, a third of a team's idle) 32.4 (0.36) and 39.4
+// (0.45); 4000 x 16384 (one team of 1024 threads an SM, no second one to work while it waits) 85 and 133 (0.45). A CTA per
 // row took 92.7 and 116 us for the first, 60.9 and 210 for the 333.
+// Farthest from the copy rate: narrow ragged rows, whose teams idle most and whose checkpoint is a pass of its own (60000 x
+// 130 bf16, residual, checkpoint, 48.2 us, 0.22, and 30.1, 0.27; 60000 x 333 67.4 and 52.8, 0.39; 30000 x 1001 0.54 and 0.57), and
+// ragged rows of more than 1024 spans, whose teams of 1024 threads hold 64 registers each and whose backwards spill (4000 x
+// 16383 bf16, four spans a thread: 224 us, 0.17, and 271, 0.21, 540 bytes spilled; of two spans 144, from a checkpoint 568 and 232).
 #include <algorithm>
 #include <numeric>
 

@@ -465,6 +465,30 @@ moe_status moe_expert_ffn_bwd_ckpt(const moe_config* cfg, const void* x_perm,
                                    void* dh_sh, void* dx_sh, void* dws1, void* dws2,
                                    const int32_t* group_expert, moe_stream_t stream);
 
+/*
+ * Embedding lookup with scaling: out[t] = scale * W[ids[t]], rounded once to dtype.
+ *   ids [T] i32; w [V,d] dtype; out [T,d] dtype out. An id < 0 (padding) gives a row of zeros; one >= V
+ *   does too and is recorded as MOE_ERR_DEVICE_CHECK (moe_device_status).
+ * T in [0, 2^31), d >= 1, V in [1, 2^31 - 1), any alignment of whole elements (16-byte aligned buffers with rows of
+ * whole 16-byte vectors are fastest). scale is finite.
+ */
+moe_status moe_embed_fwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const int32_t* ids,
+                         const void* w, float scale, void* out, moe_stream_t stream);
+
+/* Bytes of workspace for moe_embed_bwd. Host only. */
+moe_status moe_embed_workspace_size(int64_t T, int32_t d, int32_t V, size_t* bytes /* HOST out */);
+
+/*
+ * Gradient of moe_embed_fwd: dW[v] = scale * sum over t with ids[t] = v of dout[t], summed in fp32 and rounded once.
+ *   dout [T,d] dtype; dw [V,d] dtype: with accumulate = 0 written whole (zeros for ids without tokens), with
+ *   accumulate = 1 the tokens' rows are added to (in fp32, rounded once) and no other row is read or written.
+ * Ids outside [0, V) add nothing (those >= V are recorded as above). The tokens are sorted by id and each id's rows
+ * added in the order of the batch: deterministic. workspace: 16-byte aligned.
+ */
+moe_status moe_embed_bwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const int32_t* ids,
+                         const void* dout, float scale, int accumulate, void* dw, void* workspace,
+                         size_t workspace_bytes, moe_stream_t stream);
+
 /* Synchronises `stream`, returns the first error code any kernel recorded since the
  * last call (MOE_OK if none) in *code and clears it. */
 moe_status moe_device_status(moe_stream_t stream, int32_t* code /* HOST out */);

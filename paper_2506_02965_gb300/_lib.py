@@ -109,6 +109,9 @@ _SIGS = {
     "moe_ckpt_unpack": [_I64, _I32, _INT] + [P] * 4,
     "moe_ckpt_swiglu_bwd": [_I64, _I32, _INT] + [P] * 6,
     "moe_expert_ffn_bwd_ckpt": [_CFG] + [P] * 25,
+    "moe_embed_fwd": [_I64, _I32, _I32, _INT, P, P, _F32, P, P],
+    "moe_embed_workspace_size": [_I64, _I32, _I32, ctypes.POINTER(_SIZE)],
+    "moe_embed_bwd": [_I64, _I32, _I32, _INT, P, P, _F32, _INT, P, P, _SIZE, P],
 }
 for _n, _a in _SIGS.items():
     f = getattr(_lib, _n)
@@ -489,3 +492,25 @@ def moe_expert_ffn_bwd_ckpt(cfg, x_perm, offsets, w1, w2, gu_q, gu_scale, dy_per
         sh("h_gu_sh", h_gu_sh, S * T * 2 * Fs), sh("act_sh", act_sh, S * T * Fs), sh("dh_sh", dh_sh, S * T * 2 * Fs),
         sh("dx_sh", dx_sh, S * T * d), sh("dws1", dws1, S * 2 * Fs * d, used=True), sh("dws2", dws2, S * d * Fs, used=True),
         at("group_expert", group_expert, E, _I32T), _stream(stream)), fn)
+
+
+# ------------------------------------------------------------------ around a stack of blocks
+def moe_embed_fwd(T, d, V, dtype, ids, w, scale, out, stream=None):
+    fn = "moe_embed_fwd"
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_embed_fwd(T, d, V, dt, _arr(fn, "ids", ids, _I32T, T), _arr(fn, "w", w, dt, V * d), scale,
+                              _arr(fn, "out", out, dt, T * d), _stream(stream)), fn)
+
+
+def moe_embed_workspace_size(T, d, V) -> int:
+    n = ctypes.c_size_t(0)
+    _check(_lib.moe_embed_workspace_size(int(T), int(d), int(V), ctypes.byref(n)), "moe_embed_workspace_size")
+    return n.value
+
+
+def moe_embed_bwd(T, d, V, dtype, ids, dout, scale, accumulate, dw, workspace, workspace_bytes, stream=None):
+    fn = "moe_embed_bwd"
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_embed_bwd(T, d, V, dt, _arr(fn, "ids", ids, _I32T, T), _arr(fn, "dout", dout, dt, T * d), scale, accumulate,
+                              _arr(fn, "dw", dw, dt, V * d), _work(fn, workspace, workspace_bytes), workspace_bytes,
+                              _stream(stream)), fn)

@@ -1116,18 +1116,68 @@ moe_status moe_expert_ffn_bwd_ckpt(const moe_config* cfg, const void* x_perm, co
     return MOE_OK;
 }
 
+// ---------------------------------------------------------------- embedding
+static moe_status check_vocab(int64_t T, int32_t d, int32_t V, moe_dtype dtype) {
+    moe_status st = check_rows(T, d, dtype);
+    if (st) return st;
+    if (V < 1 || V == INT32_MAX) return fail(MOE_ERR_INVALID_ARG, "V=%d outside [1, 2^31 - 1)", V);
+    return MOE_OK;
+}
+
+moe_status moe_embed_fwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const int32_t* ids, const void* w, float scale, void* out,
+                         moe_stream_t stream) {
+    moe_status st = check_vocab(T, d, V, dtype);
+    if (st) return st;
+    if (scale - scale != 0.f) return fail(MOE_ERR_INVALID_ARG, "scale is not finite");
+    if (T == 0) return MOE_OK;
+    const size_t es = dtype == MOE_BF16 ? 2 : 4;
+    REQUIRE_ELEM(ids, 4);
+    REQUIRE_ELEM(w, es);
+    REQUIRE_ELEM(out, es);
+    return cuda_status(launch_embed_fwd(ids, T, d, V, dtype == MOE_BF16, w, scale, out, (cudaStream_t)stream), "moe_embed_fwd");
+}
+
+moe_status moe_embed_workspace_size(int64_t T, int32_t d, int32_t V, size_t* bytes) {
+    moe_status st = check_vocab(T, d, V, MOE_F32);
+    if (st) return st;
+    REQUIRE(bytes);
+    *bytes = embed_workspace_bytes(T, d, V);
+    return MOE_OK;
+}
+
+moe_status moe_embed_bwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const int32_t* ids, const void* dout, float scale,
+                         int accumulate, void* dw, void* workspace, size_t workspace_bytes, moe_stream_t stream) {
+    moe_status st = check_vocab(T, d, V, dtype);
+    if (st) return st;
+    if (scale - scale != 0.f) return fail(MOE_ERR_INVALID_ARG, "scale is not finite");
+    if (accumulate != 0 && accumulate != 1) return fail(MOE_ERR_INVALID_ARG, "accumulate must be 0 or 1");
+    const size_t es = dtype == MOE_BF16 ? 2 : 4;
+    REQUIRE_ELEM(dw, es);
+    if (T > 0) {
+        REQUIRE_ELEM(ids, 4);
+        REQUIRE_ELEM(dout, es);
+        REQUIRE_VEC(workspace);
+        const size_t need = embed_workspace_bytes(T, d, V);
+        if (workspace_bytes < need)
+            return fail(MOE_ERR_INVALID_ARG, "workspace of %zu bytes < %zu needed", workspace_bytes, need);
+    }
+    return cuda_status(launch_embed_bwd(ids, T, d, V, dtype == MOE_BF16, dout, scale, accumulate != 0, dw, workspace, (cudaStream_t)stream),
+                       "moe_embed_bwd");
+}
+
 moe_status moe_device_status(moe_stream_t stream, int32_t* code) {
     REQUIRE(code);
     cudaStream_t s = (cudaStream_t)stream;
-    int c[5] = {0, 0, 0, 0, 0};
+    int c[6] = {0, 0, 0, 0, 0, 0};
     cudaError_t e;
     if ((e = route_status(s, &c[0])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = dispatch_status(s, &c[1])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = gemm_status(s, &c[2])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = f32_status(s, &c[3])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = gate_status(s, &c[4])) != cudaSuccess) return cuda_status(e, "status");
+    if ((e = embed_status(s, &c[5])) != cudaSuccess) return cuda_status(e, "status");
     *code = 0;
-    for (int i = 0; i < 5; ++i)
+    for (int i = 0; i < 6; ++i)
         if (c[i] && !*code) *code = c[i];
     return MOE_OK;
 }

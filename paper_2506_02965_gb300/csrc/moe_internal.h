@@ -91,6 +91,14 @@ cudaError_t launch_ckpt_unpack(const int8_t* q, const float* scale, int64_t rows
 cudaError_t launch_ckpt_swiglu_bwd(const int8_t* q, const float* scale, const void* dact, int64_t rows, int F, bool bf16, void* act,
                                    void* dh, cudaStream_t s);
 
+// embedding lookup and its gradient (embed.cu)
+size_t embed_workspace_bytes(int64_t T, int32_t d, int32_t V);
+cudaError_t launch_embed_fwd(const int32_t* ids, int64_t T, int32_t d, int32_t V, bool bf16, const void* w, float scale, void* out,
+                             cudaStream_t s);
+cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V, bool bf16, const void* dout, float scale,
+                             bool accumulate, void* dw, void* ws, cudaStream_t s);
+cudaError_t embed_status(cudaStream_t s, int* code);
+
 cudaError_t launch_route(const RouteArgs& a, bool bf16, bool from_logits, cudaStream_t s);
 // bf16 router logits on the tensor cores with the gating epilogue (E > 64, or E % 4 == 0)
 cudaError_t launch_route_tc(const RouteArgs& a, cudaStream_t s);

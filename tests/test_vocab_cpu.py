@@ -1,0 +1,48 @@
+"""Refusals of the operators around a stack of blocks: on the host, before any device work, with a reason."""
+import os
+
+import pytest
+
+from paper_2506_02965_gb300 import build as _build
+
+if not os.path.exists(_build.LIB) or _build._stale(_build.LIB, os.path.join(_build.CSRC, "moe_abi.cu")):
+    _build.build()
+from paper_2506_02965_gb300 import _lib as L  # noqa: E402
+
+BAD = L.MOE_ERR_INVALID_ARG
+
+
+def refused(frag, fn, *args, status=BAD):
+    with pytest.raises(L.MoEError) as e:
+        fn(*args, stream=0)
+    assert e.value.status == status and frag in str(e.value), str(e.value)
+
+
+@pytest.mark.parametrize("change,frag", [
+    (dict(T=-1), "rows=-1"), (dict(T=1 << 31), "rows="), (dict(d=0), "width 0"), (dict(V=0), "V=0"), (dict(V=2 ** 31 - 1), "V="),
+    (dict(dtype=7), "dtype"), (dict(ids=None), "ids is NULL"), (dict(ids=18), "ids is not aligned"), (dict(w=None), "w is NULL"),
+    (dict(w=17), "w is not aligned"), (dict(scale=float("inf")), "scale"), (dict(scale=float("nan")), "scale"),
+    (dict(out=None), "out is NULL"), (dict(out=17), "out is not aligned")])
+def test_embed_forward(change, frag):
+    a = dict(T=4, d=64, V=100, dtype=L.MOE_BF16, ids=16, w=16, scale=1.0, out=16)
+    a.update(change)
+    refused(frag, L.moe_embed_fwd, *a.values())
+
+
+@pytest.mark.parametrize("change,frag", [
+    (dict(T=-1), "rows=-1"), (dict(d=-3), "width -3"), (dict(V=-1), "V=-1"), (dict(ids=None), "ids is NULL"),
+    (dict(dout=None), "dout is NULL"), (dict(dout=18), "dout is not aligned"), (dict(scale=float("nan")), "scale"),
+    (dict(accumulate=2), "accumulate"), (dict(dw=None), "dw is NULL"), (dict(dw=18), "dw is not aligned"),
+    (dict(ws=None), "workspace is NULL"), (dict(ws=24), "workspace is not 16-byte"), (dict(wsb=64), "workspace of 64 bytes")])
+def test_embed_backward(change, frag):
+    a = dict(T=4, d=64, V=100, dtype=L.MOE_F32, ids=16, dout=16, scale=1.0, accumulate=0, dw=16, ws=16, wsb=1 << 20)
+    a.update(change)
+    refused(frag, L.moe_embed_bwd, *a.values())
+
+
+def test_embed_workspace():
+    assert L.moe_embed_workspace_size(0, 8, 8) >= 0
+    small, large = L.moe_embed_workspace_size(4096, 64, 1000), L.moe_embed_workspace_size(65536, 4096, 131072)
+    assert 4 * 4 * 4096 <= small < large
+    with pytest.raises(L.MoEError):
+        L.moe_embed_workspace_size(4, 0, 8)

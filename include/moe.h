@@ -489,6 +489,28 @@ moe_status moe_embed_bwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const
                          const void* dout, float scale, int accumulate, void* dw, void* workspace,
                          size_t workspace_bytes, moe_stream_t stream);
 
+/* Bytes of workspace for moe_vocab_loss; with_grads: with dh and dw. Host only. */
+moe_status moe_vocab_loss_workspace_size(int64_t T, int32_t d, int32_t V, moe_dtype dtype,
+                                         int with_grads, size_t* bytes /* HOST out */);
+
+/*
+ * Softmax cross entropy of hidden states over a vocabulary, and its gradients, without the [T,V] logits in memory:
+ *   z = h w^T, lse_t = log sum_v exp z_tv, token_loss[t] = lse_t - z_t,target[t],
+ *   loss = sum_t u_t token_loss[t], u_t = weight[t], or 1 / (tokens with a target) where weight is NULL;
+ *   dz_t = u_t (softmax(z_t) - onehot(target[t])), dh = dz w, dw = dz^T h.
+ *   h [T,d], w [V,d] dtype; target [T] i32; weight [T] f32 or NULL; loss [1] f32 out; token_loss [T] f32 out or NULL;
+ *   dh [T,d], dw [V,d] dtype out: both, or both NULL (the loss alone).
+ * A token with target < 0 has none: token_loss 0 and no gradient, whatever its h holds (one with target >= V too, and it
+ * is recorded as MOE_ERR_DEVICE_CHECK). With gradients the probabilities of a piece of the tokens are held at once: in
+ * bf16 max(4096, 2d) tokens at most (2 V bytes each), in fp32 about 2^28 / V (4 V bytes each).
+ * bf16: d a multiple of 128; dz is rounded to bf16 (relative to the largest |u_t|), sums are fp32. fp32: d % 4 == 0.
+ * h, w, dh, dw, workspace 16-byte aligned. Deterministic.
+ */
+moe_status moe_vocab_loss(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const void* h,
+                          const void* w, const int32_t* target, const float* weight, float* loss,
+                          float* token_loss, void* dh, void* dw, void* workspace,
+                          size_t workspace_bytes, moe_stream_t stream);
+
 /* Synchronises `stream`, returns the first error code any kernel recorded since the
  * last call (MOE_OK if none) in *code and clears it. */
 moe_status moe_device_status(moe_stream_t stream, int32_t* code /* HOST out */);

@@ -112,6 +112,8 @@ _SIGS = {
     "moe_embed_fwd": [_I64, _I32, _I32, _INT, P, P, _F32, P, P],
     "moe_embed_workspace_size": [_I64, _I32, _I32, ctypes.POINTER(_SIZE)],
     "moe_embed_bwd": [_I64, _I32, _I32, _INT, P, P, _F32, _INT, P, P, _SIZE, P],
+    "moe_vocab_loss_workspace_size": [_I64, _I32, _I32, _INT, _INT, ctypes.POINTER(_SIZE)],
+    "moe_vocab_loss": [_I64, _I32, _I32, _INT] + [P] * 9 + [_SIZE, P],
 }
 for _n, _a in _SIGS.items():
     f = getattr(_lib, _n)
@@ -514,3 +516,19 @@ def moe_embed_bwd(T, d, V, dtype, ids, dout, scale, accumulate, dw, workspace, w
     _check(_lib.moe_embed_bwd(T, d, V, dt, _arr(fn, "ids", ids, _I32T, T), _arr(fn, "dout", dout, dt, T * d), scale, accumulate,
                               _arr(fn, "dw", dw, dt, V * d), _work(fn, workspace, workspace_bytes), workspace_bytes,
                               _stream(stream)), fn)
+
+
+def moe_vocab_loss_workspace_size(T, d, V, dtype, with_grads) -> int:
+    fn, n = "moe_vocab_loss_workspace_size", ctypes.c_size_t(0)
+    _check(_lib.moe_vocab_loss_workspace_size(int(T), int(d), int(V), _dtype_of(fn, dtype), int(bool(with_grads)), ctypes.byref(n)), fn)
+    return n.value
+
+
+def moe_vocab_loss(T, d, V, dtype, h, w, target, weight, loss, token_loss, dh, dw, workspace, workspace_bytes, stream=None):
+    fn = "moe_vocab_loss"
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_vocab_loss(T, d, V, dt, _arr(fn, "h", h, dt, T * d), _arr(fn, "w", w, dt, V * d), _arr(fn, "target", target, _I32T, T),
+                               _arr(fn, "weight", weight, MOE_F32, T), _arr(fn, "loss", loss, MOE_F32, 1),
+                               _arr(fn, "token_loss", token_loss, MOE_F32, T), _arr(fn, "dh", dh, dt, T * d),
+                               _arr(fn, "dw", dw, dt, V * d), _work(fn, workspace, workspace_bytes), workspace_bytes,
+                               _stream(stream)), fn)

@@ -1,0 +1,496 @@
+// Dense matrix products on the tensor cores (tcgen05, sm_103a) with a caller's epilogue:
+//   acc[g][m][n] = sum over k of A[g][m][k] * B[g][n][k],   16-bit operands (bf16, or fp16), fp32 accumulators,
+// for G matrices of one size, each operand stored with its contraction dimension inside (K-major) or outside
+// (MN-major). What is not here, and is in the experts' grouped kernel: groups of rows of their own lengths. What is
+// here: contractions cut into splits, only the tiles on and below the diagonal of a symmetric product, matrices that are
+// left out, and epilogues as types.
+//
+// A persistent grid of CTA pairs with 256 x 256 tiles (cta_group::2: each CTA holds half of both operands'
+// rows), or of single CTAs with 128 x 128 tiles for problems of few tiles. Warp 0 copies by TMA, a stage is 128
+// contraction terms as two 64 x 128 boxes of each operand (64 KiB, three stages), warp 1 issues the MMAs into one of
+// two accumulators, the others run the epilogue of the other. What bounds a launch with a contraction of some
+// thousand terms is the tensor pipe under the power cap; the epilogues are measured where they are.
+//
+// Waits are bounded: on a timeout the CTA records MOE_ERR_TIMEOUT, lets its copies and MMAs land, frees TMEM, returns.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "moe_internal.h"
+#include "tc_ptx.cuh"
+
+namespace moe {
+namespace dense {
+
+using namespace tc;
+
+constexpr int KST = 128;                      // contraction terms per stage
+constexpr uint32_t BOX_BYTES = 64 * 128 * 2;  // one operand box
+constexpr uint32_t STAGE_BYTES = 4 * BOX_BYTES;
+constexpr int NST = 3;
+constexpr int OUT_BOX = 32, OUT_BOX_BYTES = OUT_BOX * OUT_BOX * 2;  // epilogue staging: 32 x 32 of 16 bits
+constexpr int OUT_BOXES = 16;
+constexpr int SMEM_BYTES = 1024 + NST * (int)STAGE_BYTES + OUT_BOXES * OUT_BOX_BYTES;
+constexpr int MAX_GROUPS = 256;
+static_assert(SMEM_BYTES + 2048 <= 227 * 1024, "shared memory of one SM");
+
+__host__ __device__ constexpr int threads(int ew) { return 64 + 32 * ew; }
+
+struct Problem {
+    int M, N, K, G;
+    int splits;     // of the contraction, each of `per_split` stages (the last may have fewer)
+    int per_split;
+    int tri;        // tiles on and below the diagonal only (M == N)
+    int band;       // tile order: bands of this many rows of tiles
+    const int32_t* counts;  // [G]: matrices with counts <= 0 are left out; null: none
+    uint64_t wait_ns;
+};
+
+struct Tile {
+    int g, split;
+    int m0, n0;    // of this CTA's accumulator rows, and of the tile's columns
+    int kb0, kb1;  // stages
+    bool diag;     // (tri) a tile that the diagonal crosses
+};
+
+// What an epilogue gets besides its tile: this warp's TMEM address, its lane quarter, the share of the columns
+// [c0, c1) that it drains, and its staging boxes.
+struct Warp {
+    uint32_t tmem;
+    int q, lane, c0, c1;
+    uint8_t* box;
+    uint32_t box_u32;
+    uint32_t seq;  // boxes used so far
+};
+
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap* map, uint32_t cluster_bar, int c0, int c1, int c2) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+        "l"((uint64_t)map), "r"(cluster_bar), "r"(c0), "r"(c1), "r"(c2)
+        : "memory");
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"((uint64_t)map), "r"(src),
+                 "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+__device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
+    const __half2 h = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// 32 columns of this lane's row, as 16 words of two 16-bit values, through a staging box to the output map (which
+// cuts what lies outside the matrix). NBUF boxes per warp, each store in flight until its box is needed again.
+template <int NBUF>
+__device__ __forceinline__ void store_box(Warp& w, const CUtensorMap* map, const uint32_t (&v)[16], int col, int row, int g) {
+    const uint32_t b = w.seq % NBUF;
+    if (w.lane == 0) bulk_wait_read<NBUF - 1>();
+    __syncwarp();
+    uint8_t* base = w.box + b * OUT_BOX_BYTES + w.lane * 64;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<uint4*>(base + ((c ^ ((w.lane >> 1) & 3)) << 4)) = make_uint4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+    fence_proxy_async();
+    __syncwarp();
+    if (w.lane == 0) {
+        tma_store_3d(map, w.box_u32 + b * OUT_BOX_BYTES, col, row, g);
+        bulk_commit();
+    }
+    ++w.seq;
+}
+
+template <bool A_MN, bool B_MN, bool PAIR, bool F16, int EW, typename Epi>
+__global__ void __launch_bounds__(threads(EW), 1)
+    dense_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
+                 const __grid_constant__ Problem p, const __grid_constant__ Epi epi) {
+    pdl_begin();
+    constexpr int NPAIR = PAIR ? 2 : 1;
+    constexpr int TM = 128 * NPAIR, TN = 128 * NPAIR;
+    constexpr uint32_t IDESC = instr_desc<TN, A_MN, B_MN, TM>() & ~(F16 ? (1u << 7) | (1u << 10) : 0u);
+    constexpr int TMEM_COLS = 2 * TN;
+    constexpr int SPLIT = EW / 4;  // warps that share a lane quarter's columns
+    constexpr int NBUF = OUT_BOXES / EW;
+    static_assert(EW == 4 || EW == 8, "epilogue warps");
+
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * NST + 5];
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort, s_active;
+    __shared__ uint32_t s_fills;
+    __shared__ unsigned char s_group[MAX_GROUPS];
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* abort_flag = &s_abort;
+    const uint32_t rank = PAIR ? cluster_rank() : 0u;
+    const int64_t tile0 = (int64_t)blockIdx.x / NPAIR, tile_step = (int64_t)gridDim.x / NPAIR;
+
+    if (warp == 0) {  // the matrices that take part
+        int run = 0;
+        for (int g0 = 0; g0 < p.G; g0 += 32) {
+            const int g = g0 + lane;
+            const bool in = g < p.G && (!p.counts || p.counts[g] > 0);
+            const uint32_t m = __ballot_sync(0xffffffffu, in);
+            if (in) s_group[run + __popc(m & ((1u << lane) - 1))] = (unsigned char)g;
+            run += __popc(m);
+        }
+        if (lane == 0) {
+            s_active = run;
+            s_abort = 0;
+        }
+    }
+    __syncthreads();
+    const int mt = (p.M + TM - 1) / TM, nt = (p.N + TN - 1) / TN;
+    const int64_t per = p.tri ? (int64_t)mt * (mt + 1) / 2 : (int64_t)mt * nt;
+    const int64_t total = (int64_t)s_active * p.splits * per;
+    if (tile0 >= total) return;  // (alike in both CTAs of a pair)
+    const int stages = (p.K + KST - 1) / KST;
+
+    auto tile_at = [&](int64_t t) -> Tile {
+        Tile ti;
+        const int64_t gs = t / per;
+        const int64_t local = t - gs * per;
+        ti.g = s_group[gs / p.splits];
+        ti.split = (int)(gs % p.splits);
+        int m, n;
+        if (p.tri) {
+            m = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
+            while ((int64_t)m * (m + 1) / 2 > local) --m;
+            while ((int64_t)(m + 1) * (m + 2) / 2 <= local) ++m;
+            n = (int)(local - (int64_t)m * (m + 1) / 2);
+        } else {  // bands of p.band rows of tiles, swept along N, a band's rows innermost
+            const int64_t b = local / ((int64_t)p.band * nt);
+            const int first = (int)b * p.band, rows = min(p.band, mt - first);
+            const int rem = (int)(local - b * p.band * nt);
+            m = first + rem % rows;
+            n = rem / rows;
+        }
+        ti.diag = m == n;
+        ti.m0 = m * TM + (int)rank * 128;
+        ti.n0 = n * TN;
+        ti.kb0 = ti.split * p.per_split;
+        ti.kb1 = min(stages, ti.kb0 + p.per_split);
+        return ti;
+    };
+
+    // 1024-byte aligned ring, the staging boxes behind it
+    const uint32_t raw_u32 = smem_u32(smem_raw);
+    const uint32_t ring = raw_u32 + ((1024u - (raw_u32 & 1023u)) & 1023u);
+    uint8_t* stage_out = smem_raw + (ring - raw_u32) + NST * STAGE_BYTES;
+    const uint32_t bar0 = smem_u32(&bars[0]);
+    auto full_bar = [&](int s) { return bar0 + 8u * s; };
+    auto empty_bar = [&](int s) { return bar0 + 8u * (NST + s); };
+    auto tfull_bar = [&](int a) { return bar0 + 8u * (2 * NST + a); };
+    auto tempty_bar = [&](int a) { return bar0 + 8u * (2 * NST + 2 + a); };
+    const uint32_t drain_bar = bar0 + 8u * (2 * NST + 4);
+    auto wait_bar = [&](uint32_t bar, uint32_t parity) -> bool {
+        if constexpr (PAIR) {
+            if (mbar_try_cluster(bar, parity)) return true;
+            const uint64_t t0 = gtimer();
+            for (;;) {
+                if (mbar_try_cluster(bar, parity)) return true;
+                if (*abort_flag) return false;
+                if (gtimer() - t0 > p.wait_ns) {
+                    *abort_flag = 1;
+                    record_status(MOE_ERR_TIMEOUT);
+                    return false;
+                }
+            }
+        } else {
+            return mbar_wait(bar, parity, abort_flag, p.wait_ns);
+        }
+    };
+    auto warp_wait = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait_bar(bar, parity)); };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < NST; ++s) {
+            mbar_init(full_bar(s), 1);  // the (leader's) producer arms it for both CTAs' bytes
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(tfull_bar(a), 1);
+            mbar_init(tempty_bar(a), EW * NPAIR);
+        }
+        mbar_init(drain_bar, 1);
+        s_fills = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(TMEM_COLS)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(TMEM_COLS)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if constexpr (PAIR) cluster_sync_all();  // the peer's barriers are initialised
+    fence_after();
+    const uint32_t tmem_base = s_tmem;
+    // waits for work in flight (microseconds): not shortened with the caller's limit
+    const uint64_t drain_limit = p.wait_ns > 200000000ull ? p.wait_ns : 200000000ull;
+    auto drain = [&](uint32_t bar, uint32_t parity) {
+        const uint64_t t0 = gtimer();
+        while (!mbar_try(bar, parity) && gtimer() - t0 < drain_limit) {
+        }
+    };
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ copies
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0, fills = 0;
+            bool ok = true;
+            const uint32_t full0 = PAIR ? map_to_rank(bar0, 0) : bar0;
+            auto load = [&](uint32_t dst, const CUtensorMap* map, uint32_t fb, int c0, int c1, int c2) {
+                if constexpr (PAIR) tma_load_3d_pair(dst, map, fb, c0, c1, c2);
+                else tma_load_3d(dst, map, fb, c0, c1, c2);
+            };
+            for (int64_t t = tile0; t < total && ok; t += tile_step) {
+                const Tile ti = tile_at(t);
+                const int n0 = ti.n0 + (int)rank * 128;
+                for (int kb = ti.kb0; kb < ti.kb1; ++kb) {
+                    if (!wait_bar(empty_bar(stage), phase ^ 1u)) {
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + 2 * BOX_BYTES;
+                    const uint32_t fb = full0 + 8u * stage;
+                    // only the leader arrives, for the bytes of both CTAs; the peer's copies complete on its
+                    // barrier, after the leader's MMAs released the stage to both
+                    if (rank == 0) mbar_expect_tx(full_bar(stage), NPAIR * STAGE_BYTES);
+                    const int k0 = kb * KST;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if constexpr (A_MN) load(sa + i * BOX_BYTES, &tmA, fb, ti.m0 + 64 * i, k0, ti.g);
+                        else load(sa + i * BOX_BYTES, &tmA, fb, k0 + 64 * i, ti.m0, ti.g);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if constexpr (B_MN) load(sb + i * BOX_BYTES, &tmB, fb, n0 + 64 * i, k0, ti.g);
+                        else load(sb + i * BOX_BYTES, &tmB, fb, k0 + 64 * i, n0, ti.g);
+                    }
+                    ++fills;
+                    if (++stage == NST) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+            s_fills = fills;
+            if (rank == 0)  // every copy lands before the CTAs exit (after a whole launch at once)
+                for (uint32_t i = fills > NST ? fills - NST : 0; i < fills; ++i) drain(full_bar(i % NST), (i / NST) & 1u);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMAs (a pair's leader for both)
+        int stage = 0, acc = 0;
+        uint32_t phase = 0, acc_phase = 0;
+        bool issued = false;
+        for (int64_t t = tile0; t < total && rank == 0; t += tile_step) {
+            const Tile ti = tile_at(t);
+            bool ok = warp_wait(tempty_bar(acc), acc_phase ^ 1u);
+            if (!ok) break;
+            fence_after();
+            const uint32_t d = tmem_base + (uint32_t)(acc * TN);
+            for (int kb = ti.kb0; kb < ti.kb1; ++kb) {
+                const bool got = wait_bar(full_bar(stage), phase);
+                fence_after();
+                if (lane == 0 && got) {
+                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + 2 * BOX_BYTES;
+#pragma unroll
+                    for (int kk = 0; kk < KST / 16; ++kk) {
+                        const uint64_t ad = A_MN ? smem_desc(sa + kk * 2048, BOX_BYTES, 1024)
+                                                 : smem_desc(sa + (kk / 4) * BOX_BYTES + (kk % 4) * 32, 16, 1024);
+                        const uint64_t bd = B_MN ? smem_desc(sb + kk * 2048, BOX_BYTES, 1024)
+                                                 : smem_desc(sb + (kk / 4) * BOX_BYTES + (kk % 4) * 32, 16, 1024);
+                        const uint32_t more = kb > ti.kb0 || kk > 0 ? 1u : 0u;
+                        if constexpr (PAIR) mma_bf16_pair(d, ad, bd, IDESC, more);
+                        else mma_bf16(d, ad, bd, IDESC, more);
+                    }
+                    if constexpr (PAIR) mma_commit_pair(empty_bar(stage), 3);
+                    else mma_commit(empty_bar(stage));
+                    issued = true;
+                }
+                if (!__all_sync(0xffffffffu, got)) {
+                    ok = false;
+                    break;
+                }
+                if (++stage == NST) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
+            }
+            if (!ok) break;
+            if (lane == 0) {
+                if constexpr (PAIR) mma_commit_pair(tfull_bar(acc), 3);
+                else mma_commit(tfull_bar(acc));
+            }
+            __syncwarp();
+            if (++acc == 2) {
+                acc = 0;
+                acc_phase ^= 1u;
+            }
+        }
+        if (lane == 0 && issued) {  // every MMA of this CTA has run before TMEM is released
+            if constexpr (PAIR) mma_commit_pair(drain_bar, 1);
+            else mma_commit(drain_bar);
+            drain(drain_bar, 0);
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------------------ epilogue: warp w drains lane quarter w % 4
+        Warp w;
+        w.q = warp & 3;
+        w.lane = lane;
+        const int part = (warp - 2) >> 2;
+        w.c0 = part * (TN / SPLIT);
+        w.c1 = w.c0 + TN / SPLIT;
+        w.box = stage_out + (warp - 2) * NBUF * OUT_BOX_BYTES;
+        w.box_u32 = smem_u32(w.box);
+        w.seq = 0;
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        for (int64_t t = tile0; t < total; t += tile_step) {
+            const Tile ti = tile_at(t);
+            if (!warp_wait(tfull_bar(acc), acc_phase)) break;
+            fence_after();
+            w.tmem = tmem_base + ((uint32_t)(w.q * 32) << 16) + (uint32_t)(acc * TN);
+            epi.template run<NBUF>(p, ti, w, &tmO);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) {
+                    fence_release_smem_cluster();
+                    mbar_arrive_remote(map_to_rank(tempty_bar(acc), 0));
+                } else {
+                    mbar_arrive(tempty_bar(acc));
+                }
+            }
+            if (++acc == 2) {
+                acc = 0;
+                acc_phase ^= 1u;
+            }
+        }
+        if (lane == 0) bulk_wait0();
+    }
+    fence_before();
+    __syncthreads();
+    if constexpr (PAIR) {
+        if (threadIdx.x == 0 && *abort_flag) st_cluster(map_to_rank(smem_u32(&s_abort), rank ^ 1u), 1u);
+        __syncwarp();
+        cluster_sync_all();  // neither CTA leaves while the pair's MMAs run
+        if (*abort_flag) {   // (both CTAs see it)
+            // stages that the peer filled and the leader, giving up first, never armed
+            if (rank == 0 && threadIdx.x == 0) {
+                const uint32_t theirs = ld_cluster(map_to_rank(smem_u32(&s_fills), 1));
+                for (uint32_t i = s_fills; i < theirs; ++i) {
+                    mbar_expect_tx(full_bar(i % NST), STAGE_BYTES);
+                    drain(full_bar(i % NST), (i / NST) & 1u);
+                }
+            }
+            __syncwarp();
+            cluster_sync_all();
+        }
+    }
+    fence_after();
+    if (warp == 1) {
+        if constexpr (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------------ host side
+// A stack of G matrices [outer, inner], rows `ld` and matrices `group` elements apart (16 bytes or a multiple). As an
+// operand: boxes of 64 x 128, zeros outside; as an output: boxes of 32 x 32, nothing written outside.
+bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t ld, int G, int64_t group, bool store);
+
+template <bool A_MN, bool B_MN, bool PAIR, bool F16, int EW, typename Epi>
+static cudaError_t launch_as(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, Problem p, const Epi& epi, cudaStream_t s) {
+    constexpr int T = PAIR ? 256 : 128;
+    auto kern = dense_kernel<A_MN, B_MN, PAIR, F16, EW, Epi>;
+    cudaError_t e = allow_dynamic_smem<dense_kernel<A_MN, B_MN, PAIR, F16, EW, Epi>>(SMEM_BYTES);
+    if (e != cudaSuccess) return e;
+    const int64_t mt = (p.M + T - 1) / T, nt = (p.N + T - 1) / T;
+    const int64_t tiles = (int64_t)p.G * p.splits * (p.tri ? mt * (mt + 1) / 2 : mt * nt);
+    if (tiles <= 0) return cudaSuccess;
+    int most = sm_count();
+    if constexpr (PAIR) {  // clusters that fit at once
+        static std::atomic<int> resident[kMaxDevices] = {};
+        const int dev = current_device();
+        most = dev >= 0 && dev < kMaxDevices ? resident[dev].load() : 0;
+        if (!most) {
+            cudaLaunchConfig_t q = {};
+            q.gridDim = dim3(2 * (sm_count() / 2));
+            q.blockDim = dim3(threads(EW));
+            q.dynamicSmemBytes = SMEM_BYTES;
+            cudaLaunchAttribute qa[1];
+            qa[0].id = cudaLaunchAttributeClusterDimension;
+            qa[0].val.clusterDim.x = 2;
+            qa[0].val.clusterDim.y = qa[0].val.clusterDim.z = 1;
+            q.attrs = qa;
+            q.numAttrs = 1;
+            if (cudaOccupancyMaxActiveClusters(&most, kern, &q) != cudaSuccess || most <= 0) {
+                (void)cudaGetLastError();
+                most = sm_count() / 2;
+            }
+            if (dev >= 0 && dev < kMaxDevices) resident[dev] = most;
+        }
+    }
+    const int at_once = (int)std::min<int64_t>(tiles, most);
+    // Tile order: where one operand of a matrix fits the L2 beside what streams past it, the other is read once;
+    // else bands of about the square root of the tiles in flight, which read the fewest blocks per round.
+    constexpr int64_t kResident = 48ll << 20;
+    if ((int64_t)p.N * p.K * 2 <= kResident) p.band = 1;
+    else if ((int64_t)p.M * p.K * 2 <= kResident) p.band = (int)mt;
+    else {
+        p.band = 1;
+        while ((p.band + 1) * (p.band + 1) <= at_once) ++p.band;
+    }
+    p.wait_ns = wait_limit_ns();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)at_once * (PAIR ? 2 : 1));
+    cfg.blockDim = dim3(threads(EW));
+    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 2;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = PAIR ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, a, b, o, p, epi);
+}
+
+static inline Problem problem(int M, int N, int K, int G = 1) {
+    Problem p{};
+    p.M = M;
+    p.N = N;
+    p.K = K;
+    p.G = G;
+    p.splits = 1;
+    p.per_split = (K + KST - 1) / KST;
+    return p;
+}
+// cuts the contraction into about n splits of whole stages, none empty
+static inline void split_k(Problem& p, int n) {
+    const int stages = (p.K + KST - 1) / KST;
+    p.per_split = (stages + n - 1) / n;
+    p.splits = (stages + p.per_split - 1) / p.per_split;
+}
+
+}  // namespace dense
+}  // namespace moe

@@ -1165,10 +1165,63 @@ moe_status moe_embed_bwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const
                        "moe_embed_bwd");
 }
 
+// ---------------------------------------------------------------- loss over a vocabulary
+static moe_status check_loss(int64_t T, int32_t d, int32_t V, moe_dtype dtype) {
+    moe_status st = check_vocab(T, d, V, dtype);
+    if (st) return st;
+    if (dtype == MOE_BF16 && d % 128) return fail(MOE_ERR_INVALID_ARG, "bf16 needs d a multiple of 128 (got %d)", d);
+    if (dtype == MOE_F32 && d % 4) return fail(MOE_ERR_INVALID_ARG, "fp32 needs d %% 4 == 0 (got %d)", d);
+    return MOE_OK;
+}
+
+moe_status moe_vocab_loss_workspace_size(int64_t T, int32_t d, int32_t V, moe_dtype dtype, int with_grads, size_t* bytes) {
+    moe_status st = check_loss(T, d, V, dtype);
+    if (st) return st;
+    REQUIRE(bytes);
+    *bytes = vocab_workspace_bytes(T, d, V, dtype == MOE_BF16, with_grads != 0);
+    return MOE_OK;
+}
+
+moe_status moe_vocab_loss(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const void* h, const void* w, const int32_t* target,
+                          const float* weight, float* loss, float* token_loss, void* dh, void* dw, void* workspace,
+                          size_t workspace_bytes, moe_stream_t stream) {
+    moe_status st = check_loss(T, d, V, dtype);
+    if (st) return st;
+    REQUIRE_ELEM(loss, 4);
+    if (T > 0 && !dh != !dw) return fail(MOE_ERR_INVALID_ARG, "dh and dw come together");
+    if (dw) REQUIRE_VEC(dw);
+    if (T > 0) {
+        REQUIRE_VEC(h);
+        REQUIRE_VEC(w);
+        REQUIRE_ELEM(target, 4);
+        OPTIONAL_ELEM(weight, 4);
+        OPTIONAL_ELEM(token_loss, 4);
+        if (dh) REQUIRE_VEC(dh);
+        REQUIRE_VEC(workspace);
+        const size_t need = vocab_workspace_bytes(T, d, V, dtype == MOE_BF16, dh != nullptr);
+        if (workspace_bytes < need)
+            return fail(MOE_ERR_INVALID_ARG, "workspace of %zu bytes < %zu needed", workspace_bytes, need);
+    }
+    VocabArgs a{};
+    a.T = T;
+    a.d = d;
+    a.V = V;
+    a.bf16 = dtype == MOE_BF16;
+    a.h = h;
+    a.w = w;
+    a.target = target;
+    a.weight = weight;
+    a.loss = loss;
+    a.token_loss = token_loss;
+    a.dh = dh;
+    a.dw = dw;
+    return cuda_status(launch_vocab_loss(a, workspace, (cudaStream_t)stream), "moe_vocab_loss");
+}
+
 moe_status moe_device_status(moe_stream_t stream, int32_t* code) {
     REQUIRE(code);
     cudaStream_t s = (cudaStream_t)stream;
-    int c[6] = {0, 0, 0, 0, 0, 0};
+    int c[7] = {0, 0, 0, 0, 0, 0, 0};
     cudaError_t e;
     if ((e = route_status(s, &c[0])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = dispatch_status(s, &c[1])) != cudaSuccess) return cuda_status(e, "status");
@@ -1176,8 +1229,9 @@ moe_status moe_device_status(moe_stream_t stream, int32_t* code) {
     if ((e = f32_status(s, &c[3])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = gate_status(s, &c[4])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = embed_status(s, &c[5])) != cudaSuccess) return cuda_status(e, "status");
+    if ((e = vocab_status(s, &c[6])) != cudaSuccess) return cuda_status(e, "status");
     *code = 0;
-    for (int i = 0; i < 6; ++i)
+    for (int i = 0; i < 7; ++i)
         if (c[i] && !*code) *code = c[i];
     return MOE_OK;
 }

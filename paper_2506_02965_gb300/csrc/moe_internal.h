@@ -99,6 +99,24 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
                              bool accumulate, void* dw, void* ws, cudaStream_t s);
 cudaError_t embed_status(cudaStream_t s, int* code);
 
+// softmax cross entropy over a vocabulary (vocab.cu)
+struct VocabArgs {
+    int64_t T;
+    int d, V;
+    bool bf16;
+    const void* h;         // [T,d] dtype
+    const void* w;         // [V,d] dtype
+    const int32_t* target; // [T]
+    const float* weight;   // [T] or null
+    float* loss;           // [1]
+    float* token_loss;     // [T] or null
+    void* dh;              // [T,d] or null (both gradients or neither)
+    void* dw;              // [V,d]
+};
+size_t vocab_workspace_bytes(int64_t T, int32_t d, int32_t V, bool bf16, bool grads);
+cudaError_t launch_vocab_loss(const VocabArgs& a, void* workspace, cudaStream_t s);
+cudaError_t vocab_status(cudaStream_t s, int* code);
+
 cudaError_t launch_route(const RouteArgs& a, bool bf16, bool from_logits, cudaStream_t s);
 // bf16 router logits on the tensor cores with the gating epilogue (E > 64, or E % 4 == 0)
 cudaError_t launch_route_tc(const RouteArgs& a, cudaStream_t s);

@@ -1,0 +1,630 @@
+// Softmax cross entropy over a vocabulary, without keeping the logits, and its gradients.
+//   z = h W^T;  lse_t = log sum_v exp z_tv;  l_t = lse_t - z_t,y;  loss = sum_t u_t l_t
+//   dz_t = u_t (softmax(z_t) - onehot(y_t));  dh = dz W;  dW = dz^T h
+// Three products of 2 T V d operations bound a training step (the tensor pipe), reading W a forward of few tokens.
+//
+// bf16. The logits stay in the tensor cores' accumulators: the product's epilogue takes a row's largest logit m and
+// sum of exp(z - m) over a share of the vocabulary (a tile's columns, or half of them), and a pass over
+// these joins them to lse. A forward keeps nothing else. For the gradients the epilogue also stores exp(z - m), in
+// fp16: at most 1, so that fp16's range is enough (what is lost below 2^-25 is lost against 1), and rounded to 11
+// bits where bf16 would keep 8. A pass then makes dz = u (exp(z - m) exp(m - lse) - onehot) in place, in bf16, the
+// one rounding of dz that counts, and two products make dh and dW from it. The softmax is not computed again
+// for that (a fourth product), which costs a pass over 2 bytes a logit, and room for them: so tokens are taken in
+// pieces, as many at once as cost no more room than the fp32 sums of dW over the pieces would.
+// u is divided by its largest magnitude before that rounding and multiplied in afterwards, in fp32: weights of
+// tokens are mostly all alike, and dz near a token's target would carry the same rounding of u for all of them.
+//
+// fp32. The logits of a piece are stored transposed, [V, tokens], by the fp32 products, so that the vocabulary is the
+// dimension that both gradients' products can cut: dh as sums over parts of the vocabulary, joined afterwards.
+#include "dense_tc.cuh"
+#include "span.cuh"
+
+namespace moe {
+
+namespace {
+
+using namespace dense;
+
+constexpr int kPairs = 76;          // CTA pairs of the part: rules that also size workspaces do not ask the device
+constexpr int kMaxSplits = 16;      // of dh's contraction over the vocabulary
+constexpr int kF32Splits = 64;
+constexpr int kColChunk = 512;      // fp32: vocabulary rows whose statistics one CTA takes
+constexpr float kNegInf = -INFINITY;
+
+size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// ---------------------------------------------------------------- tile shapes
+struct Shape {
+    bool pair;
+    int splits;
+};
+// Stages that a launch takes from first to last, in units of a pair's: rounds of tiles times the stages of one, a
+// 128 x 128 tile's stage being 0.92 of a pair's (it has a quarter of the operations but half of the operands'
+// bytes per SM). With splits, also the partial sums' way through memory (0.7 us a stage at 6.5 TB/s).
+Shape pick_shape(int64_t M, int64_t N, int64_t K, int max_splits) {
+    const int64_t stages = ceil_div(K, KST);
+    Shape best{true, 1};
+    double least = 0;
+    for (int pair = 1; pair >= 0; --pair) {
+        const int64_t t = pair ? 256 : 128, tiles = ceil_div(M, t) * ceil_div(N, t);
+        for (int s = 1; s <= max_splits && s <= stages; ++s) {
+            const int64_t each = ceil_div(stages, s), real = ceil_div(stages, each);
+            const int64_t rounds = ceil_div(tiles * real, pair ? kPairs : 2 * kPairs);
+            const double cost = (double)rounds * ((double)each + 2) * (pair ? 1.0 : 0.92) +
+                                (real > 1 ? 4 + (double)real * M * N * 8 / (6.5e6 * 0.7) : 0);
+            if (least == 0 || cost < least) {
+                least = cost;
+                best = {pair != 0, (int)real};
+            }
+        }
+    }
+    return best;
+}
+
+// ---------------------------------------------------------------- epilogues
+// The logits' tile: statistics of every row's share of columns, the target's logit, and (STORE) exp(z - m) in fp16.
+template <bool STORE> struct VocabEpi {
+    const int32_t* target;
+    float2* part;  // [M][shares]: largest logit, sum of exp(z - it)
+    float* zy;     // [M]
+    int shares;
+
+    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
+        const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane, cols = w.c1 - w.c0;
+        const int base = ti.n0 + w.c0;
+        if (base >= p.N) return;
+        const int y = m < p.M ? target[m] : -1;
+        float mx = kNegInf;
+#pragma unroll 1
+        for (int c = 0; c < cols && base + c < p.N; c += 32) {
+            float v[32];
+            tmem_ld32(w.tmem + w.c0 + c, v);
+            const int left = p.N - (base + c);
+            if (left >= 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) mx = fmaxf(mx, v[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (i < left) mx = fmaxf(mx, v[i]);
+            }
+            const bool mine = y >= base + c && y < base + c + 32 && y < p.N;
+            if (__any_sync(0xffffffffu, mine)) {
+                float z = 0.f;
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (y == base + c + i) z = v[i];
+                if (mine) zy[m] = z;
+            }
+        }
+        const float ref = mx == kNegInf ? 0.f : mx;
+        float sum = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < cols && base + c < p.N; c += 32) {
+            float v[32];
+            tmem_ld32(w.tmem + w.c0 + c, v);
+            const int left = p.N - (base + c);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                v[i] = fast_exp(v[i] - ref);
+                if (i >= left) v[i] = 0.f;
+                sum += v[i];
+            }
+            if constexpr (STORE) {
+                uint32_t u[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) u[i] = pack_half(v[2 * i], v[2 * i + 1]);
+                store_box<NBUF>(w, out, u, base + c, row0, 0);
+            }
+        }
+        if (m < p.M) part[(int64_t)m * shares + base / cols] = make_float2(mx, sum);
+    }
+};
+
+// A product that is stored in bf16, times *alpha (OUT_BF16), as fp32 sums of one split or piece (OUT_F32), added to
+// such sums (OUT_ADD), or with such sums added to it, in bf16 (OUT_LAST).
+enum { OUT_BF16, OUT_F32, OUT_ADD, OUT_LAST };
+template <int MODE> struct OutEpi {
+    const float* alpha;
+    float* sums;  // [splits][M][N]
+
+    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
+        const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
+        const float a = MODE == OUT_BF16 || MODE == OUT_LAST ? *alpha : 1.f;
+        float* at = MODE == OUT_BF16 ? nullptr : sums + ((int64_t)ti.split * p.M + m) * p.N;
+#pragma unroll 1
+        for (int c = w.c0; c < w.c1 && ti.n0 + c < p.N; c += 32) {
+            float v[32];
+            tmem_ld32(w.tmem + c, v);
+            if constexpr (MODE == OUT_ADD || MODE == OUT_LAST) {
+                if (m < p.M) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 s = *reinterpret_cast<const float4*>(at + ti.n0 + c + i);
+                        v[i] += s.x; v[i + 1] += s.y; v[i + 2] += s.z; v[i + 3] += s.w;
+                    }
+                }
+            }
+            if constexpr (MODE == OUT_F32 || MODE == OUT_ADD) {
+                if (m < p.M) {
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        *reinterpret_cast<float4*>(at + ti.n0 + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                }
+            } else {
+                uint32_t u[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) u[i] = pack_bf16(a * v[2 * i], a * v[2 * i + 1]);
+                store_box<NBUF>(w, out, u, ti.n0 + c, row0, 0);
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------- passes
+__device__ __forceinline__ bool has_target(int y, int V) { return y >= 0 && y < V; }
+
+constexpr int kPrep = 1024;
+// scal[0] = the largest |weight| of a token with a target, or 1 / (tokens with a target); scal[1] = 1 / scal[0] or 0.
+// (fp32: also the vocabulary's parts as row offsets.)
+__global__ void __launch_bounds__(kPrep) vocab_prep_kernel(const int32_t* __restrict__ target, const float* __restrict__ weight, int64_t T,
+                                                          int V, float* __restrict__ scal, int32_t* __restrict__ offsets, int splits,
+                                                          int rows) {
+    pdl_begin();
+    __shared__ float s_max[32];
+    __shared__ int s_n[32];
+    float most = 0.f;
+    int n = 0;
+    bool bad = false, nan = false;
+    for (int64_t t = threadIdx.x; t < T; t += kPrep) {
+        const int y = target[t];
+        bad |= y >= V;
+        if (!has_target(y, V)) continue;
+        ++n;
+        if (weight) {
+            most = fmaxf(most, fabsf(weight[t]));
+            nan |= weight[t] != weight[t];
+        }
+    }
+    if (bad) record_status(MOE_ERR_DEVICE_CHECK);
+    if (nan) most = INFINITY;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    most = warp_max(most);
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (lane == 0) {
+        s_max[warp] = most;
+        s_n[warp] = n;
+    }
+    __syncthreads();
+    if (warp == 0) {
+        most = warp_max(s_max[lane]);
+        n = __reduce_add_sync(0xffffffffu, s_n[lane]);
+        if (lane == 0) {
+            // (weights with an infinity or a NaN are taken as they are)
+            const float a = weight ? (most < 3.4e38f ? most : 1.f) : 1.f / (float)max(n, 1);
+            scal[0] = a;
+            scal[1] = a > 0.f ? 1.f / a : 0.f;
+        }
+    }
+    if (offsets)
+        for (int i = threadIdx.x; i <= splits; i += kPrep) offsets[i] = (int)min64(V, (int64_t)i * rows);
+}
+
+// lse and the token's loss from its shares' statistics: a warp per token.
+__global__ void __launch_bounds__(256) vocab_join_kernel(const float2* __restrict__ part, int shares, int64_t rows,
+                                                         const int32_t* __restrict__ target, int V, const float* __restrict__ zy,
+                                                         const float* __restrict__ zt, float* __restrict__ lse, float* __restrict__ token) {
+    pdl_begin();
+    const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    if (t >= rows) return;
+    const float2* p = part + t * shares;
+    float m = kNegInf;
+    for (int i = lane; i < shares; i += 32) m = fmaxf(m, p[i].x);
+    m = warp_max(m);
+    const float ref = m == kNegInf ? 0.f : m;
+    float s = 0.f;
+    for (int i = lane; i < shares; i += 32) s += p[i].y * expf(p[i].x - ref);
+    s = warp_sum(s);
+    if (lane == 0) {
+        const float l = ref + logf(s);
+        const int y = target[t];
+        lse[t] = l;
+        token[t] = has_target(y, V) ? l - (zt ? zt[(int64_t)y * rows + t] : zy[t]) : 0.f;
+    }
+}
+
+// loss = sum of u_t l_t: one CTA, a fixed order, in 64 bits.
+__global__ void __launch_bounds__(1024) vocab_total_kernel(const float* __restrict__ token, const int32_t* __restrict__ target,
+                                                           const float* __restrict__ weight, const float* __restrict__ scal, int64_t T,
+                                                           int V, float* __restrict__ loss) {
+    pdl_begin();
+    __shared__ double s_part[32];
+    double sum = 0.0;
+    for (int64_t t = threadIdx.x; t < T; t += 1024)
+        if (has_target(target[t], V)) sum += (double)token[t] * (weight ? weight[t] : scal[0]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        sum = s_part[threadIdx.x];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (threadIdx.x == 0) *loss = (float)sum;
+    }
+}
+
+// The hidden states for dW = dz^T h: of tokens without a target zeros, as 0 times what stands there need not be 0. A row's
+// CTA of `words` 16-byte words.
+__device__ __forceinline__ void live_row(const uint4* h, uint4* to, int64_t t, int words, bool live) {
+    for (int i = (int)threadIdx.x; i < words; i += 256) to[t * words + i] = live ? h[t * words + i] : make_uint4(0, 0, 0, 0);
+}
+
+// exp(z - m) in fp16 -> dz / scal[0] in bf16, in place. Rows of ld elements, eight a thread.
+__global__ void __launch_bounds__(256) vocab_dz_kernel(uint4* __restrict__ e, int64_t ld, const float2* __restrict__ part, int shares,
+                                                       int share, const float* __restrict__ lse, const int32_t* __restrict__ target,
+                                                       const float* __restrict__ weight, const float* __restrict__ scal, int V,
+                                                       const uint4* __restrict__ h, uint4* __restrict__ h_live, int words) {
+    pdl_begin();
+    constexpr int U = 4;
+    const int64_t t = blockIdx.y;
+    const int y = target[t];
+    const bool live = has_target(y, V);
+    if (blockIdx.x == 0) live_row(h, h_live, t, words, live);
+    const float u = !live ? 0.f : weight ? weight[t] * scal[1] : 1.f;
+    const float l = lse[t];
+    uint4* row = e + t * (ld / 8);
+    const int first = (int)blockIdx.x * (256 * U) + (int)threadIdx.x;
+    uint4 v[U];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int i = first + k * 256;
+        v[k] = make_uint4(0, 0, 0, 0);
+        if (i * 8 < V) v[k] = row[i];
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+        const int i = first + k * 256;
+        if (i * 8 >= V) break;
+        // (a token without a target has no gradient, whatever its logits are)
+        const float m = live ? part[t * shares + i * 8 / share].x : 0.f;
+        const float f = live ? u * fast_exp(m - l) : 0.f;
+        uint32_t* q = reinterpret_cast<uint32_t*>(&v[k]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float2 x = __half22float2(*reinterpret_cast<const __half2*>(&q[j]));
+            x.x = live ? x.x * f : 0.f;
+            x.y = live ? x.y * f : 0.f;
+            if (y == i * 8 + 2 * j) x.x -= u;
+            if (y == i * 8 + 2 * j + 1) x.y -= u;
+            q[j] = pack_bf16(x.x, x.y);
+        }
+        row[i] = v[k];
+    }
+}
+
+// out = alpha * the sum of the splits' fp32 sums, in order. Four elements a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) vocab_sum_kernel(const float* __restrict__ sums, int splits, int64_t n, const float* __restrict__ alpha,
+                                                        T* __restrict__ out) {
+    pdl_begin();
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const float a = alpha ? *alpha : 1.f;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n % 4 == 0) {
+        for (int s = 0; s < splits; ++s) {
+            const float4 x = *reinterpret_cast<const float4*>(sums + s * n + i);
+            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+        }
+    } else {
+        for (int s = 0; s < splits; ++s)
+            for (int j = 0; j < 4 && i + j < n; ++j) v[j] += sums[s * n + i + j];
+    }
+    for (int j = 0; j < 4 && i + j < n; ++j) Elem<T>::store(out + i + j, a * v[j]);
+}
+
+// ---------------------------------------------------------------- fp32 passes over the transposed logits [V, n]
+// Statistics of kColChunk rows of every column: 32 columns by 8 rows of threads.
+__global__ void __launch_bounds__(256) vocab_col_kernel(const float* __restrict__ z, int V, int n, float2* __restrict__ part, int shares) {
+    pdl_begin();
+    __shared__ float2 s_part[8][33];
+    const int c = (int)blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x & 31, r = threadIdx.x >> 5;
+    const int v0 = (int)blockIdx.y * kColChunk, v1 = min(V, v0 + kColChunk);
+    float m = kNegInf, s = 0.f;
+    if (c < n) {
+        for (int v = v0 + r; v < v1; v += 8) m = fmaxf(m, z[(int64_t)v * n + c]);
+        const float ref = m == kNegInf ? 0.f : m;
+        for (int v = v0 + r; v < v1; v += 8) s += expf(z[(int64_t)v * n + c] - ref);
+    }
+    s_part[r][lane] = make_float2(m, s);
+    __syncthreads();
+    if (r == 0 && c < n) {
+        for (int k = 1; k < 8; ++k) m = fmaxf(m, s_part[k][lane].x);
+        const float ref = m == kNegInf ? 0.f : m;
+        s = 0.f;
+        for (int k = 0; k < 8; ++k) s += s_part[k][lane].y * expf(s_part[k][lane].x == kNegInf ? kNegInf : s_part[k][lane].x - ref);
+        part[(int64_t)c * shares + blockIdx.y] = make_float2(m, s);
+    }
+}
+__global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z, int V, int n, const float* __restrict__ lse,
+                                                           const int32_t* __restrict__ target, const float* __restrict__ weight,
+                                                           const float* __restrict__ scal, const float* __restrict__ h,
+                                                           float* __restrict__ h_live, int d) {
+    pdl_begin();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * d; i += (int64_t)gridDim.x * 256)
+        h_live[i] = has_target(target[i / d], V) ? h[i] : 0.f;
+    const int64_t total = (int64_t)V * n;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int v = (int)(i / n), t = (int)(i - (int64_t)v * n), y = target[t];
+        const float u = !has_target(y, V) ? 0.f : weight ? weight[t] : scal[0];
+        z[i] = has_target(y, V) ? u * (expf(z[i] - lse[t]) - (v == y ? 1.f : 0.f)) : 0.f;
+    }
+}
+__global__ void __launch_bounds__(256) vocab_add_kernel(float* __restrict__ to, const float* __restrict__ from, int64_t n) {
+    pdl_begin();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] += from[i];
+}
+
+// ---------------------------------------------------------------- plan: what a call's sizes decide
+struct Plan {
+    int64_t rows;  // tokens at once
+    int pieces;
+    int64_t ld;    // bf16: row stride of the stored exp(z - m)
+    int shares, share;
+    Shape logits, dh, dw;
+    int ew;        // epilogue warps of the logits
+    int f32_splits, f32_rows;
+    // workspace: offsets
+    size_t scal, token, lse, zy, part, e, live, sums, dwsum, offsets, total;
+};
+
+Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
+    Plan p{};
+    const int64_t t1 = std::max<int64_t>(T, 1);
+    if (bf16) {
+        // Pieces: with more than one, dW's sums over them are kept in fp32, 4 V d bytes; as many tokens as the stored
+        // exponentials' 2 V bytes make of that, and no fewer than 4096 (below, dW's contraction is short).
+        const int64_t most = grads ? std::max<int64_t>(4096, 2 * (int64_t)d) : (int64_t)1 << 24;
+        p.pieces = (int)ceil_div(t1, most);
+        p.rows = p.pieces == 1 ? t1 : ceil_div(ceil_div(t1, p.pieces), 256) * 256;
+        p.pieces = (int)ceil_div(t1, p.rows);
+        p.ld = ceil_div(V, 64) * 64;
+        p.logits = pick_shape(p.rows, V, d, 1);
+        p.dh = pick_shape(p.rows, d, V, kMaxSplits);
+        p.dw = pick_shape(V, d, p.rows, 1);
+        p.ew = d < 1024 ? 8 : 4;  // a short contraction: the epilogue, not the product, sets a tile's time
+        p.share = (p.logits.pair ? 256 : 128) / (p.ew / 4);
+        p.shares = (int)ceil_div(V, p.share);
+    } else {
+        const int64_t most = std::max<int64_t>(128, ((int64_t)1 << 28) / V / 128 * 128);
+        p.rows = std::min(t1, most);
+        p.pieces = (int)ceil_div(t1, p.rows);
+        p.shares = (int)ceil_div(V, kColChunk);
+        const int64_t tiles = ceil_div(p.rows, 128) * ceil_div(d, 128);
+        const int64_t want = std::min<int64_t>(std::min<int64_t>(kF32Splits, ceil_div(4 * kPairs, tiles)), ceil_div(V, 128));
+        p.f32_rows = (int)(ceil_div(ceil_div(V, want), 32) * 32);
+        p.f32_splits = (int)ceil_div(V, p.f32_rows);
+    }
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up(bytes);
+        return here;
+    };
+    p.scal = take(8);
+    p.token = take((size_t)t1 * 4);
+    p.lse = take((size_t)p.rows * 4);
+    p.zy = take((size_t)p.rows * 4);
+    p.part = take((size_t)p.rows * p.shares * 8);
+    if (bf16) {
+        if (grads) {
+            p.e = take((size_t)p.rows * p.ld * 2);
+            p.live = take((size_t)p.rows * d * 2);
+            p.sums = take(p.dh.splits > 1 ? (size_t)p.dh.splits * p.rows * d * 4 : 0);
+            p.dwsum = take(p.pieces > 1 ? (size_t)V * d * 4 : 0);
+        }
+    } else {
+        p.e = take((size_t)p.rows * V * 4);
+        if (grads) {
+            p.offsets = take((size_t)(p.f32_splits + 1) * 4);
+            p.live = take((size_t)p.rows * d * 4);
+            p.sums = take(p.f32_splits > 1 ? (size_t)p.f32_splits * p.rows * d * 4 : 0);
+            p.dwsum = take(p.pieces > 1 ? (size_t)V * d * 4 : 0);
+        }
+    }
+    p.total = at;
+    return p;
+}
+
+template <bool STORE>
+cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const VocabEpi<STORE>& e,
+                   cudaStream_t s) {
+    if (pl.logits.pair) {
+        if (pl.ew == 8) return launch_as<false, false, true, false, 8>(a, b, o, p, e, s);
+        return launch_as<false, false, true, false, 4>(a, b, o, p, e, s);
+    }
+    if (pl.ew == 8) return launch_as<false, false, false, false, 8>(a, b, o, p, e, s);
+    return launch_as<false, false, false, false, 4>(a, b, o, p, e, s);
+}
+template <bool A_MN, int MODE>
+cudaError_t product(bool pair, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const OutEpi<MODE>& e,
+                    cudaStream_t s) {
+    if (pair) return launch_as<A_MN, true, true, false, 4>(a, b, o, p, e, s);
+    return launch_as<A_MN, true, false, false, 4>(a, b, o, p, e, s);
+}
+
+#define MOE_TRY(call)                              \
+    do {                                           \
+        const cudaError_t e_ = (call);             \
+        if (e_ != cudaSuccess) return e_;          \
+    } while (0)
+
+cudaError_t sum_splits(const float* sums, int splits, int64_t n, const float* alpha, bool bf16, void* out, cudaStream_t s) {
+    const dim3 grid((unsigned)ceil_div(n, 1024));
+    if (bf16) (void)launch_pdl(vocab_sum_kernel<__nv_bfloat16>, grid, dim3(256), 0, s, sums, splits, n, alpha, (__nv_bfloat16*)out);
+    else (void)launch_pdl(vocab_sum_kernel<float>, grid, dim3(256), 0, s, sums, splits, n, alpha, (float*)out);
+    return cudaGetLastError();
+}
+
+float* token_loss(const Plan& pl, const VocabArgs& a, char* ws) { return a.token_loss ? a.token_loss : (float*)(ws + pl.token); }
+
+cudaError_t join(const Plan& pl, const VocabArgs& a, char* ws, int64_t t0, int64_t n, const float* zt, cudaStream_t s) {
+    (void)launch_pdl(vocab_join_kernel, dim3((unsigned)ceil_div(n, 8)), dim3(256), 0, s, (const float2*)(ws + pl.part), pl.shares, n,
+                     a.target + t0, a.V, (const float*)(ws + pl.zy), zt, (float*)(ws + pl.lse), token_loss(pl, a, ws) + t0);
+    return cudaGetLastError();
+}
+
+cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, cudaStream_t s) {
+    const int64_t t0 = piece * pl.rows, n = std::min(pl.rows, a.T - t0);
+    const int d = a.d, V = a.V;
+    const __nv_bfloat16* h = (const __nv_bfloat16*)a.h + t0 * d;
+    float* scal = (float*)(ws + pl.scal);
+    CUtensorMap mh, mw, me;
+    if (!make_map3(&mh, h, d, n, d, 1, 0, false) || !make_map3(&mw, a.w, d, V, d, 1, 0, false)) return cudaErrorInvalidValue;
+    Problem p = problem((int)n, V, d);
+    if (a.dh) {
+        if (!make_map3(&me, ws + pl.e, V, n, pl.ld, 1, 0, true)) return cudaErrorInvalidValue;
+        MOE_TRY(logits(pl, mh, mw, me, p, VocabEpi<true>{a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
+    } else {
+        MOE_TRY(logits(pl, mh, mw, mh, p, VocabEpi<false>{a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
+    }
+    MOE_TRY(join(pl, a, ws, t0, n, nullptr, s));
+    if (!a.dh) return cudaSuccess;
+    const float* weight = a.weight ? a.weight + t0 : nullptr;
+    for (int64_t r = 0; r < n; r += 65535) {  // (rows of a grid)
+        (void)launch_pdl(vocab_dz_kernel, dim3((unsigned)ceil_div(V, 8 * 256 * 4), (unsigned)std::min<int64_t>(65535, n - r)), dim3(256), 0, s,
+                         (uint4*)(ws + pl.e + r * pl.ld * 2), pl.ld, (const float2*)(ws + pl.part) + r * pl.shares, pl.shares, pl.share,
+                         (const float*)(ws + pl.lse) + r, a.target + t0 + r, weight ? weight + r : nullptr, (const float*)scal, V,
+                         (const uint4*)(h + r * d), (uint4*)(ws + pl.live + r * d * 2), d / 8);
+        MOE_TRY(cudaGetLastError());
+    }
+    CUtensorMap ma, mb, mo;
+    // dh = dz W: the vocabulary inside dz's rows, outside W's
+    if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false)) return cudaErrorInvalidValue;
+    if (!make_map3(&mo, (__nv_bfloat16*)a.dh + t0 * d, d, n, d, 1, 0, true)) return cudaErrorInvalidValue;
+    p = problem((int)n, d, V);
+    split_k(p, pl.dh.splits);
+    float* sums = (float*)(ws + pl.sums);
+    if (p.splits > 1) {
+        MOE_TRY((product<false>(pl.dh.pair, ma, mw, mo, p, OutEpi<OUT_F32>{nullptr, sums}, s)));
+        MOE_TRY(sum_splits(sums, p.splits, n * d, scal, true, (__nv_bfloat16*)a.dh + t0 * d, s));
+    } else {
+        MOE_TRY((product<false>(pl.dh.pair, ma, mw, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s)));
+    }
+    // dW = dz^T h: the tokens outside both
+    if (!make_map3(&mb, ws + pl.live, d, n, d, 1, 0, false) || !make_map3(&mo, a.dw, d, V, d, 1, 0, true)) return cudaErrorInvalidValue;
+    p = problem(V, d, (int)n);
+    float* acc = (float*)(ws + pl.dwsum);
+    if (pl.pieces == 1) return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s);
+    if (piece == 0) return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_F32>{nullptr, acc}, s);
+    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_ADD>{nullptr, acc}, s);
+    return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_LAST>{scal, acc}, s);
+}
+
+cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, cudaStream_t s) {
+    const int64_t t0 = piece * pl.rows, n = std::min(pl.rows, a.T - t0);
+    const int d = a.d, V = a.V;
+    const float* h = (const float*)a.h + t0 * d;
+    float *zt = (float*)(ws + pl.e), *scal = (float*)(ws + pl.scal);
+    GemmMArgs m{};
+    m.G = 1;
+    m.rows.rows = V;
+    m.a = a.w;
+    m.b = h;
+    m.b_group_elems = n * d;
+    m.b_kmajor = true;
+    m.N = (int)n;
+    m.K = d;
+    m.epi = EPI_STORE;
+    m.out0 = zt;
+    MOE_TRY(launch_gemm_m(m, false, s));
+    (void)launch_pdl(vocab_col_kernel, dim3((unsigned)ceil_div(n, 32), (unsigned)pl.shares), dim3(256), 0, s, (const float*)zt, V, (int)n,
+                     (float2*)(ws + pl.part), pl.shares);
+    MOE_TRY(cudaGetLastError());
+    MOE_TRY(join(pl, a, ws, t0, n, zt, s));
+    if (!a.dh) return cudaSuccess;
+    (void)launch_pdl(vocab_dz_f32_kernel, dim3((unsigned)std::min<int64_t>(ceil_div((int64_t)V * n, 1024), 16 * 2 * kPairs)), dim3(256), 0, s,
+                     zt, V, (int)n, (const float*)(ws + pl.lse), a.target + t0, a.weight ? a.weight + t0 : nullptr, (const float*)scal, h,
+                     (float*)(ws + pl.live), d);
+    MOE_TRY(cudaGetLastError());
+    // dh: sums over parts of the vocabulary, each a group of rows of both operands
+    float *dh = (float*)a.dh + t0 * d, *sums = (float*)(ws + pl.sums);
+    GemmKArgs k{};
+    k.G = pl.f32_splits;
+    k.rows.offsets = (const int32_t*)(ws + pl.offsets);
+    k.rows.rows = V;
+    k.a = zt;
+    k.b = a.w;
+    k.M = (int)n;
+    k.N = d;
+    k.out = pl.f32_splits > 1 ? sums : dh;
+    MOE_TRY(launch_gemm_k(k, false, s));
+    if (pl.f32_splits > 1) MOE_TRY(sum_splits(sums, pl.f32_splits, n * d, nullptr, false, dh, s));
+    m.a = zt;
+    m.b = ws + pl.live;
+    m.b_kmajor = false;
+    m.N = d;
+    m.K = (int)n;
+    m.out0 = piece == 0 ? a.dw : (void*)(ws + pl.dwsum);
+    MOE_TRY(launch_gemm_m(m, false, s));
+    if (piece > 0) {
+        (void)launch_pdl(vocab_add_kernel, dim3(16 * 2 * kPairs), dim3(256), 0, s, (float*)a.dw, (const float*)(ws + pl.dwsum), (int64_t)V * d);
+        MOE_TRY(cudaGetLastError());
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+namespace dense {
+
+bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t ld, int G, int64_t group, bool store) {
+    typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode fn = [] {
+        void* ptr = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            ptr = nullptr;
+        return (Encode)ptr;
+    }();
+    if (!fn) return false;
+    if (G == 1) group = outer * ld;
+    cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)outer, (cuuint64_t)G};
+    cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)group * 2};
+    cuuint32_t box[3] = {store ? (cuuint32_t)OUT_BOX : 64u, store ? (cuuint32_t)OUT_BOX : 128u, 1u};
+    cuuint32_t estr[3] = {1u, 1u, 1u};
+    // (the type only matters to arithmetic that is not done here: fp16 moves as bf16)
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              store ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace dense
+
+size_t vocab_workspace_bytes(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) { return plan(T, d, V, bf16, grads).total; }
+
+cudaError_t launch_vocab_loss(const VocabArgs& a, void* workspace, cudaStream_t s) {
+    if (a.T == 0) {
+        MOE_TRY(cudaMemsetAsync(a.loss, 0, 4, s));
+        return a.dw ? cudaMemsetAsync(a.dw, 0, (size_t)a.V * a.d * (a.bf16 ? 2 : 4), s) : cudaSuccess;
+    }
+    const Plan pl = plan(a.T, a.d, a.V, a.bf16, a.dh != nullptr);
+    char* ws = (char*)workspace;
+    float* scal = (float*)(ws + pl.scal);
+    (void)launch_pdl(vocab_prep_kernel, dim3(1), dim3(kPrep), 0, s, a.target, a.weight, a.T, a.V, scal,
+                     !a.bf16 && a.dh ? (int32_t*)(ws + pl.offsets) : nullptr, pl.f32_splits, pl.f32_rows);
+    MOE_TRY(cudaGetLastError());
+    for (int i = 0; i < pl.pieces; ++i) MOE_TRY(a.bf16 ? piece_bf16(pl, a, ws, i, s) : piece_f32(pl, a, ws, i, s));
+    (void)launch_pdl(vocab_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)token_loss(pl, a, ws), a.target, a.weight, (const float*)scal, a.T, a.V,
+                     a.loss);
+    return cudaGetLastError();
+}
+
+cudaError_t vocab_status(cudaStream_t s, int* code) { return tu_status_read_clear(s, code); }
+
+}  // namespace moe

@@ -46,3 +46,29 @@ def test_embed_workspace():
     assert 4 * 4 * 4096 <= small < large
     with pytest.raises(L.MoEError):
         L.moe_embed_workspace_size(4, 0, 8)
+
+
+@pytest.mark.parametrize("change,frag", [
+    (dict(T=-1), "rows=-1"), (dict(d=64), "multiple of 128"), (dict(d=0), "width 0"), (dict(V=0), "V=0"), (dict(dtype=3), "dtype"),
+    (dict(dtype=L.MOE_F32, d=126), "d % 4"), (dict(h=None), "h is NULL"), (dict(h=24), "h is not 16-byte"), (dict(w=None), "w is NULL"),
+    (dict(w=20), "w is not 16-byte"), (dict(target=None), "target is NULL"), (dict(target=18), "target is not aligned"),
+    (dict(weight=18), "weight is not aligned"), (dict(loss=None), "loss is NULL"), (dict(token=18), "token_loss is not aligned"),
+    (dict(dh=None), "dh and dw"), (dict(dw=None), "dh and dw"), (dict(dh=24), "dh is not 16-byte"), (dict(dw=24), "dw is not 16-byte"),
+    (dict(ws=None), "workspace is NULL"), (dict(ws=8), "workspace is not 16-byte"), (dict(wsb=1024), "workspace of 1024 bytes")])
+def test_vocab_loss(change, frag):
+    a = dict(T=4, d=128, V=1000, dtype=L.MOE_BF16, h=16, w=16, target=16, weight=None, loss=16, token=16, dh=16, dw=16, ws=16, wsb=1 << 30)
+    a.update(change)
+    refused(frag, L.moe_vocab_loss, *a.values())
+
+
+def test_vocab_loss_workspace():
+    """The loss alone keeps statistics; with gradients a piece of the probabilities, whatever the batch."""
+    size = L.moe_vocab_loss_workspace_size
+    T, d, V = 8192, 1024, 131072
+    logits = T * V * 2
+    assert size(T, d, V, L.MOE_BF16, False) < logits / 50
+    assert 4096 * V * 2 <= size(T, d, V, L.MOE_BF16, True) < logits + 4 * V * d
+    assert size(16 * T, d, V, L.MOE_BF16, True) < size(T, d, V, L.MOE_BF16, True) * 1.05
+    assert size(T, d, V, L.MOE_F32, True) < 3 * 2 ** 30
+    with pytest.raises(L.MoEError):
+        size(4, 100, 10, L.MOE_BF16, True)

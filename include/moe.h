@@ -511,6 +511,28 @@ moe_status moe_vocab_loss(int64_t T, int32_t d, int32_t V, moe_dtype dtype, cons
                           float* token_loss, void* dh, void* dw, void* workspace,
                           size_t workspace_bytes, moe_stream_t stream);
 
+/* Bytes of workspace for moe_orthogonalise. Host only. */
+moe_status moe_orthogonalise_workspace_size(int32_t groups, int32_t rows, int32_t cols, moe_dtype dtype,
+                                            size_t* bytes /* HOST out */);
+
+/*
+ * The orthogonalised update of `groups` matrices, for moe_sgd_update in the gradient's place. For each:
+ *   m = beta * momentum + dw, u = dw + beta * m (nesterov = 1) or m (0); u = dw without a momentum;
+ *   X = u / |u|_F, then `steps` times, with A = X X^T: X = a X + (b A + c A A) X, (a, b, c) = (3.4445, -4.7750, 2.0315);
+ *   out = scale * X, momentum_out = m.
+ * Five steps take the singular values from about 0.01 of |u|_F on into [0.7, 1.2].
+ *   dw, out [groups,rows,cols] dtype; momentum, momentum_out [groups,rows,cols] f32 (may be one buffer), or both NULL;
+ *   group_counts [groups] i32 or NULL: a matrix whose count is <= 0 is left out, its momentum_out and out as they were.
+ * A matrix of zeros gives zeros. bf16: the products run in fp16 with fp32 sums (the values are bounded; X also with a
+ * residual of 8 bits); fp32: as the fp32 GEMMs. steps in 1..16, groups up to 256 (MOE_ERR_UNSUPPORTED above), any sides.
+ * out may be dw's buffer. All buffers but group_counts 16-byte aligned. Deterministic.
+ */
+moe_status moe_orthogonalise(int32_t groups, int32_t rows, int32_t cols, moe_dtype dtype,
+                             const void* dw, const float* momentum, float beta, int nesterov,
+                             const int32_t* group_counts, int32_t steps, float scale,
+                             float* momentum_out, void* out, void* workspace,
+                             size_t workspace_bytes, moe_stream_t stream);
+
 /* Synchronises `stream`, returns the first error code any kernel recorded since the
  * last call (MOE_OK if none) in *code and clears it. */
 moe_status moe_device_status(moe_stream_t stream, int32_t* code /* HOST out */);

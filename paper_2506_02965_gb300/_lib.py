@@ -114,6 +114,8 @@ _SIGS = {
     "moe_embed_bwd": [_I64, _I32, _I32, _INT, P, P, _F32, _INT, P, P, _SIZE, P],
     "moe_vocab_loss_workspace_size": [_I64, _I32, _I32, _INT, _INT, ctypes.POINTER(_SIZE)],
     "moe_vocab_loss": [_I64, _I32, _I32, _INT] + [P] * 9 + [_SIZE, P],
+    "moe_orthogonalise_workspace_size": [_I32, _I32, _I32, _INT, ctypes.POINTER(_SIZE)],
+    "moe_orthogonalise": [_I32, _I32, _I32, _INT, P, P, _F32, _INT, P, _I32, _F32, P, P, P, _SIZE, P],
 }
 for _n, _a in _SIGS.items():
     f = getattr(_lib, _n)
@@ -532,3 +534,19 @@ def moe_vocab_loss(T, d, V, dtype, h, w, target, weight, loss, token_loss, dh, d
                                _arr(fn, "token_loss", token_loss, MOE_F32, T), _arr(fn, "dh", dh, dt, T * d),
                                _arr(fn, "dw", dw, dt, V * d), _work(fn, workspace, workspace_bytes), workspace_bytes,
                                _stream(stream)), fn)
+
+
+def moe_orthogonalise_workspace_size(groups, rows, cols, dtype) -> int:
+    fn, n = "moe_orthogonalise_workspace_size", ctypes.c_size_t(0)
+    _check(_lib.moe_orthogonalise_workspace_size(int(groups), int(rows), int(cols), _dtype_of(fn, dtype), ctypes.byref(n)), fn)
+    return n.value
+
+
+def moe_orthogonalise(groups, rows, cols, dtype, dw, momentum, beta, nesterov, group_counts, steps, scale, momentum_out, out, workspace,
+                      workspace_bytes, stream=None):
+    fn, n = "moe_orthogonalise", groups * rows * cols
+    dt = _dtype_of(fn, dtype)
+    _check(_lib.moe_orthogonalise(groups, rows, cols, dt, _arr(fn, "dw", dw, dt, n), _arr(fn, "momentum", momentum, MOE_F32, n), beta,
+                                  nesterov, _arr(fn, "group_counts", group_counts, _I32T, groups), steps, scale,
+                                  _arr(fn, "momentum_out", momentum_out, MOE_F32, n), _arr(fn, "out", out, dt, n),
+                                  _work(fn, workspace, workspace_bytes), workspace_bytes, _stream(stream)), fn)

@@ -22,7 +22,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmoe.so")
 SOURCES = ["route.cu", "dispatch.cu", "gemm_f32.cu", "gemm_tc.cu", "train.cu", "norm.cu", "gate.cu",
-           "ckpt.cu", "embed.cu", "vocab.cu", "moe_abi.cu"]
+           "ckpt.cu", "embed.cu", "vocab.cu", "orth.cu", "moe_abi.cu"]
 HEADERS = ["dense_tc.cuh", "device_state.h", "moe_common.cuh", "moe_internal.h", "span.cuh", "tc_ptx.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",

@@ -485,6 +485,37 @@ static inline Problem problem(int M, int N, int K, int G = 1) {
     p.per_split = (K + KST - 1) / KST;
     return p;
 }
+static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+constexpr int kPairs = 76;  // CTA pairs of the part: the rules below also size workspaces, and do not ask the device
+struct Shape {
+    bool pair;
+    int splits;
+};
+// Pair tiles or single ones, and splits: those by which a launch takes least from first to last, in units of a pair's
+// stage: rounds of tiles times the stages of one (and two for its start and end), a 128 x 128 tile's stage being 0.92
+// of a pair's (a quarter of the operations, half of the operands' bytes per SM). With splits, also the partial
+// sums' way through memory (a stage is 0.7 us; 6.5 TB/s) and a launch.
+static inline Shape pick_shape(int64_t M, int64_t N, int64_t K, int max_splits, int64_t G = 1, bool tri = false) {
+    const int64_t stages = ceil_div(K, KST);
+    Shape best{true, 1};
+    double least = 0;
+    for (int pair = 1; pair >= 0; --pair) {
+        const int64_t t = pair ? 256 : 128, mt = ceil_div(M, t), tiles = G * (tri ? mt * (mt + 1) / 2 : mt * ceil_div(N, t));
+        for (int s = 1; s <= max_splits && s <= stages; ++s) {
+            const int64_t each = ceil_div(stages, s), real = ceil_div(stages, each);
+            const int64_t rounds = ceil_div(tiles * real, pair ? kPairs : 2 * kPairs);
+            const double cost = (double)rounds * ((double)each + 2) * (pair ? 1.0 : 0.92) +
+                                (real > 1 ? 4 + (double)real * M * N * 8 / (6.5e6 * 0.7) : 0);
+            if (least == 0 || cost < least) {
+                least = cost;
+                best = {pair != 0, (int)real};
+            }
+        }
+    }
+    return best;
+}
+
 // cuts the contraction into about n splits of whole stages, none empty
 static inline void split_k(Problem& p, int n) {
     const int stages = (p.K + KST - 1) / KST;

@@ -1218,10 +1218,70 @@ moe_status moe_vocab_loss(int64_t T, int32_t d, int32_t V, moe_dtype dtype, cons
     return cuda_status(launch_vocab_loss(a, workspace, (cudaStream_t)stream), "moe_vocab_loss");
 }
 
+// ---------------------------------------------------------------- orthogonalised updates
+static moe_status check_orth(int32_t groups, int32_t rows, int32_t cols, moe_dtype dtype) {
+    if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "unknown dtype %d", (int)dtype);
+    if (groups < 0) return fail(MOE_ERR_INVALID_ARG, "groups=%d < 0", groups);
+    if (groups > kOrthMaxGroups)
+        return fail(MOE_ERR_UNSUPPORTED, "groups=%d > %d, the most matrices of a call", groups, kOrthMaxGroups);
+    if (rows < 1 || cols < 1) return fail(MOE_ERR_INVALID_ARG, "rows=%d and cols=%d must be > 0", rows, cols);
+    if (rows > 1 << 24 || cols > 1 << 24 || (int64_t)rows * cols >= (int64_t)1 << 40 ||
+        (int64_t)groups * rows >= (int64_t)1 << 31)
+        return fail(MOE_ERR_INVALID_ARG, "matrices of %d x %d, %d of them: sides up to 2^24, groups * rows < 2^31", rows, cols, groups);
+    return MOE_OK;
+}
+
+moe_status moe_orthogonalise_workspace_size(int32_t groups, int32_t rows, int32_t cols, moe_dtype dtype, size_t* bytes) {
+    moe_status st = check_orth(groups, rows, cols, dtype);
+    if (st) return st;
+    REQUIRE(bytes);
+    *bytes = orth_workspace_bytes(groups, rows, cols, dtype == MOE_BF16);
+    return MOE_OK;
+}
+
+moe_status moe_orthogonalise(int32_t groups, int32_t rows, int32_t cols, moe_dtype dtype, const void* dw, const float* momentum,
+                             float beta, int nesterov, const int32_t* group_counts, int32_t steps, float scale, float* momentum_out,
+                             void* out, void* workspace, size_t workspace_bytes, moe_stream_t stream) {
+    moe_status st = check_orth(groups, rows, cols, dtype);
+    if (st) return st;
+    if (beta - beta != 0.f) return fail(MOE_ERR_INVALID_ARG, "beta is not finite");
+    if (scale - scale != 0.f) return fail(MOE_ERR_INVALID_ARG, "scale is not finite");
+    if (nesterov != 0 && nesterov != 1) return fail(MOE_ERR_INVALID_ARG, "nesterov must be 0 or 1");
+    if (steps < 1 || steps > kOrthMaxSteps) return fail(MOE_ERR_INVALID_ARG, "steps=%d outside [1, %d]", steps, kOrthMaxSteps);
+    if (!momentum != !momentum_out) return fail(MOE_ERR_INVALID_ARG, "momentum and momentum_out come together");
+    if (groups == 0) return MOE_OK;
+    REQUIRE_VEC(dw);
+    REQUIRE_VEC(out);
+    if (momentum) {
+        REQUIRE_VEC(momentum);
+        REQUIRE_VEC(momentum_out);
+    }
+    OPTIONAL_ELEM(group_counts, 4);
+    REQUIRE_VEC(workspace);
+    const size_t need = orth_workspace_bytes(groups, rows, cols, dtype == MOE_BF16);
+    if (workspace_bytes < need)
+        return fail(MOE_ERR_INVALID_ARG, "workspace of %zu bytes < %zu needed", workspace_bytes, need);
+    OrthArgs a{};
+    a.groups = groups;
+    a.rows = rows;
+    a.cols = cols;
+    a.bf16 = dtype == MOE_BF16;
+    a.g = dw;
+    a.momentum = momentum;
+    a.beta = beta;
+    a.nesterov = nesterov;
+    a.counts = group_counts;
+    a.steps = steps;
+    a.scale = scale;
+    a.momentum_out = momentum_out;
+    a.out = out;
+    return cuda_status(launch_orthogonalise(a, workspace, (cudaStream_t)stream), "moe_orthogonalise");
+}
+
 moe_status moe_device_status(moe_stream_t stream, int32_t* code) {
     REQUIRE(code);
     cudaStream_t s = (cudaStream_t)stream;
-    int c[7] = {0, 0, 0, 0, 0, 0, 0};
+    int c[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     cudaError_t e;
     if ((e = route_status(s, &c[0])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = dispatch_status(s, &c[1])) != cudaSuccess) return cuda_status(e, "status");
@@ -1230,8 +1290,9 @@ moe_status moe_device_status(moe_stream_t stream, int32_t* code) {
     if ((e = gate_status(s, &c[4])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = embed_status(s, &c[5])) != cudaSuccess) return cuda_status(e, "status");
     if ((e = vocab_status(s, &c[6])) != cudaSuccess) return cuda_status(e, "status");
+    if ((e = orth_status(s, &c[7])) != cudaSuccess) return cuda_status(e, "status");
     *code = 0;
-    for (int i = 0; i < 7; ++i)
+    for (int i = 0; i < 8; ++i)
         if (c[i] && !*code) *code = c[i];
     return MOE_OK;
 }

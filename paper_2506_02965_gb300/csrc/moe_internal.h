@@ -117,6 +117,25 @@ size_t vocab_workspace_bytes(int64_t T, int32_t d, int32_t V, bool bf16, bool gr
 cudaError_t launch_vocab_loss(const VocabArgs& a, void* workspace, cudaStream_t s);
 cudaError_t vocab_status(cudaStream_t s, int* code);
 
+// orthogonalised updates (orth.cu)
+struct OrthArgs {
+    int groups, rows, cols;
+    bool bf16;
+    const void* g;          // [groups, rows, cols] dtype
+    const float* momentum;  // the same in fp32, or null
+    float beta;
+    int nesterov;
+    const int32_t* counts;  // [groups] or null
+    int steps;
+    float scale;
+    float* momentum_out;
+    void* out;              // as g
+};
+constexpr int kOrthMaxGroups = 256, kOrthMaxSteps = 16;
+size_t orth_workspace_bytes(int groups, int rows, int cols, bool bf16);
+cudaError_t launch_orthogonalise(const OrthArgs& a, void* workspace, cudaStream_t s);
+cudaError_t orth_status(cudaStream_t s, int* code);
+
 cudaError_t launch_route(const RouteArgs& a, bool bf16, bool from_logits, cudaStream_t s);
 // bf16 router logits on the tensor cores with the gating epilogue (E > 64, or E % 4 == 0)
 cudaError_t launch_route_tc(const RouteArgs& a, cudaStream_t s);

@@ -1,0 +1,525 @@
+// Orthogonalised updates: the momentum in front, and five or so Newton-Schulz products.
+//   m' = beta m + g;  u = g + beta m' (nesterov) or m' (g without a momentum);  X = u / |u|_F;
+//   per step, on the smaller side:  A = X X^T,  X = a X + (b A + c A A) X;  out = scale X
+// with a, b, c = 3.4445, -4.7750, 2.0315 (the published quintic, whose steps take every singular value above about 0.01 of
+// the norm into [0.7, 1.2]). For n <= m the sides of a matrix, a step is n^2 m + n^3 + 2 n^2 m operations, of the two
+// symmetric products only the tiles on and below the diagonal, the others written as their mirror images: the tensor pipe
+// bounds it for n above some hundreds, the launches below.
+//
+// bf16 matrices run in fp16. Every value is bounded (X's singular values never pass 1.21, so |X| < 1.21, |A| < 1.47,
+// |b A + c A A| < 2.81), so powers of two that put them below fp16's largest number keep 11 bits where bf16 would keep
+// 8: after five steps, which amplify what small singular directions carry by up to a^5 = 485, bf16 products are 1.2e-2
+// off (of the norm, 333 x 1000 to 2048 x 2048 matrices), fp16 ones 1.5e-3. Most of that is X's own rounding
+// between the steps, and it is where a few directions outweigh the rest (30 times: 8.5e-3) that it counts, so
+// the a X term takes X to 14 bits, its residual as an 8-bit float (e5m2, the upper half of an fp16). The other products
+// keep fp16. All sums are fp32, the norm's are 64-bit sums of fp32 ones.
+//
+// A matrix with more rows than columns is not transposed: A = X^T X and X = a X + X (b A + c A A), with the operands'
+// other major. fp32 matrices take the fp32 products throughout.
+#include <cuda_fp8.h>
+
+#include "dense_tc.cuh"
+#include "span.cuh"
+
+namespace moe {
+
+namespace {
+
+using namespace dense;
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kScaleX = 256.f, kScaleA = 4096.f;  // of the fp16 X, and of A and b A + c A A
+constexpr float kResidual = 4096.f;                 // of X's residual, which is 2^-12 of X at most
+
+size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// ---------------------------------------------------------------- momentum and norm
+// The sum of squares as three fp32 sums, of x 2^-64, x and x 2^64: whichever neither overflowed nor vanished.
+struct Squares {
+    float big = 0.f, mid = 0.f, small = 0.f;
+    __device__ __forceinline__ void add(float x) {
+        const float b = x * 0x1p-64f, s = x * 0x1p64f;
+        big = fmaf(b, b, big);
+        mid = fmaf(x, x, mid);
+        small = fmaf(s, s, small);
+    }
+};
+
+// N consecutive floats, aligned to them or to 16 bytes
+template <int N> __device__ __forceinline__ void load_f32(const float* p, float (&v)[N]) {
+    constexpr int W = N < 4 ? N : 4;
+#pragma unroll
+    for (int i = 0; i < N / W; ++i) {
+        Span<float, W> s;
+        s.load(p + i * W);
+        float f[W];
+        s.unpack(f);
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[i * W + j] = f[j];
+    }
+}
+template <int N> __device__ __forceinline__ void store_f32(float* p, const float (&v)[N]) {
+    constexpr int W = N < 4 ? N : 4;
+#pragma unroll
+    for (int i = 0; i < N / W; ++i) {
+        float f[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) f[j] = v[i * W + j];
+        Span<float, W> s;
+        s.pack(f);
+        s.store(p + i * W);
+    }
+}
+
+struct UpdateArgs {
+    const void* g;
+    const float* mom;      // or null
+    float* mom_out;
+    const int32_t* counts;
+    int64_t elems;         // of a matrix
+    int cols;
+    int64_t ld, group;     // of X: row stride, and matrix stride
+    float beta;
+    int nesterov;
+    double* part;          // [G][parts][3]
+    int parts;
+    float* inv;            // [G]: 1 / |u|
+};
+
+// u (and m') of N elements from `at` on
+template <typename T, int N>
+__device__ __forceinline__ void update_of(const UpdateArgs& a, int64_t at, float (&u)[N], float (&m)[N]) {
+    if constexpr (sizeof(T) == 4) {
+        load_f32<N>((const float*)a.g + at, u);
+    } else {
+        Span<T, N> s;
+        s.load((const T*)a.g + at);
+        s.unpack(u);
+    }
+    if (a.mom) {
+        load_f32<N>(a.mom + at, m);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            m[j] = fmaf(a.beta, m[j], u[j]);
+            u[j] = a.nesterov ? fmaf(a.beta, m[j], u[j]) : m[j];
+        }
+    }
+}
+
+template <typename T, int N> __global__ void __launch_bounds__(256) orth_norm_kernel(const UpdateArgs a) {
+    pdl_begin();
+    const int g = blockIdx.y;
+    if (a.counts && a.counts[g] <= 0) return;
+    Squares q;
+    const int64_t spans = a.elems / N, base = g * a.elems;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < spans; i += (int64_t)gridDim.x * 256) {
+        float u[N], m[N];
+        update_of<T, N>(a, base + i * N, u, m);
+#pragma unroll
+        for (int j = 0; j < N; ++j) q.add(u[j]);
+    }
+    double v[3] = {(double)q.big, (double)q.mid, (double)q.small};
+    __shared__ double s_part[8][3];
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5][k] = v[k];
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        double s = 0.0;
+        for (int w = 0; w < 8; ++w) s += s_part[w][threadIdx.x];
+        a.part[((int64_t)g * a.parts + blockIdx.x) * 3 + threadIdx.x] = s;
+    }
+}
+
+__global__ void __launch_bounds__(32) orth_inv_kernel(const UpdateArgs a) {
+    pdl_begin();
+    const int g = blockIdx.x;
+    if (a.counts && a.counts[g] <= 0) return;
+    double v[3] = {0.0, 0.0, 0.0};
+    for (int i = threadIdx.x; i < a.parts; i += 32)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) v[k] += a.part[((int64_t)g * a.parts + i) * 3 + k];
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    if (threadIdx.x == 0) {
+        // the fp32 sums' range: squares near the ends of it are taken from the sum that holds them as normal numbers
+        const double n2 = !(v[1] < 0x1p120) ? v[0] * 0x1p128 : v[1] > 0x1p-60 ? v[1] : v[2] * 0x1p-128;
+        const double n = sqrt(n2);
+        // (without a direction, zeros; an infinite or undefined norm leaves nothing but NaN)
+        a.inv[g] = n > 0.0 ? (float)fmin(1.0 / n, 3.0e38) : n == 0.0 ? 0.f : __int_as_float(0x7fc00000);
+    }
+}
+
+// X = u / |u|: in fp16 with its residual, or in fp32; and m'
+template <typename T, int N, bool HALF>
+__global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, void* hi, uint8_t* lo) {
+    pdl_begin();
+    const int g = blockIdx.y;
+    if (a.counts && a.counts[g] <= 0) return;
+    const float inv = a.inv[g];
+    const int64_t spans = a.elems / N, base = g * a.elems;
+    const int per_row = a.cols / N;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < spans; i += (int64_t)gridDim.x * 256) {
+        float u[N], m[N];
+        update_of<T, N>(a, base + i * N, u, m);
+        if (a.mom) store_f32<N>(a.mom_out + base + i * N, m);
+        const int64_t row = i / per_row, at = g * a.group + row * a.ld + (i - row * per_row) * N;
+        if constexpr (HALF) {
+            alignas(16) __half h[N];
+            alignas(8) uint8_t r[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float x = u[j] * inv * kScaleX;
+                h[j] = __float2half_rn(x);
+                r[j] = (uint8_t)__nv_cvt_float_to_fp8((x - __half2float(h[j])) * kResidual, __NV_SATFINITE, __NV_E5M2);
+            }
+            __half* to = (__half*)hi + at;
+            if constexpr (N == 8) {
+                *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(h);
+                *reinterpret_cast<uint2*>(lo + at) = *reinterpret_cast<const uint2*>(r);
+            } else {
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    to[j] = h[j];
+                    lo[at + j] = r[j];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) u[j] *= inv;
+            store_f32<N>((float*)hi + at, u);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- epilogues
+// v = alpha acc + beta C for 32 columns of this lane's row; C in fp16, with a residual or without, or none.
+struct Term {
+    const __half* hi;
+    const uint8_t* lo;
+    int64_t ld, group;
+    float beta;
+};
+struct Ahead {  // a chunk of C on its way
+    uint4 h[4], l[2];
+    __device__ __forceinline__ void load(const Term& t, int g, int m, int col, bool in) {
+        const int64_t at = g * t.group + (int64_t)m * t.ld + col;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[i] = in && t.hi ? *reinterpret_cast<const uint4*>(t.hi + at + 8 * i) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) l[i] = in && t.lo ? *reinterpret_cast<const uint4*>(t.lo + at + 16 * i) : make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void add(float beta, float (&v)[32]) const {
+        const uint32_t* hw = reinterpret_cast<const uint32_t*>(h);
+        const uint32_t* lw = reinterpret_cast<const uint32_t*>(l);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&hw[i]));
+            // two bytes, each the upper one of an fp16
+            const uint32_t r = __byte_perm(lw[i / 2], 0, i & 1 ? 0x3424 : 0x1404);
+            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&r));
+            v[2 * i] = fmaf(beta, fmaf(y.x, 1.f / kResidual, x.x), v[2 * i]);
+            v[2 * i + 1] = fmaf(beta, fmaf(y.y, 1.f / kResidual, x.y), v[2 * i + 1]);
+        }
+    }
+};
+
+// A symmetric product in fp16, its lower tiles and their mirror images.
+struct SymEpi {
+    Term c;
+    float alpha;
+    __half* out;
+    int64_t ld, group;
+
+    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
+        const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
+        const bool in = m < p.M;
+        Ahead next;
+        next.load(c, ti.g, m, ti.n0 + w.c0, in && ti.n0 + w.c0 < p.N);
+#pragma unroll 1
+        for (int k = w.c0; k < w.c1 && ti.n0 + k < p.N; k += 32) {
+            const Ahead now = next;
+            next.load(c, ti.g, m, ti.n0 + k + 32, in && k + 32 < w.c1 && ti.n0 + k + 32 < p.N);
+            float v[32];
+            tmem_ld32(w.tmem + k, v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= alpha;
+            now.add(c.beta, v);
+            uint32_t u[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) u[i] = pack_half(v[2 * i], v[2 * i + 1]);
+            store_box<NBUF>(w, map, u, ti.n0 + k, row0, ti.g);
+            if (!ti.diag) {
+                // rows of the mirror image: of two columns j, j + 1 the even lanes write rows (m, m + 1) of column j,
+                // the odd ones those of column j + 1
+                __half* to = out + ti.g * group + (int64_t)(ti.n0 + k) * ld + (m & ~1);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t mine = u[i], other = __shfl_xor_sync(0xffffffffu, mine, 1);
+                    const uint32_t pair = (w.lane & 1) ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
+                    const int col = 2 * i + (w.lane & 1);
+                    if ((m & ~1) < p.M && ti.n0 + k + col < p.N) *reinterpret_cast<uint32_t*>(to + (int64_t)col * ld) = pair;
+                }
+            }
+        }
+    }
+};
+
+// X' = alpha acc + beta X in fp16 with its residual; (LAST) in the matrix's own type, times a scale.
+template <bool LAST> struct StepEpi {
+    Term c;
+    float alpha;
+    uint8_t* lo;           // LAST: unused
+    int64_t ld, group;
+    float scale;           // LAST
+    __nv_bfloat16* out;    // LAST: rows of p.N, where the map does not serve them
+    int by_map;
+
+    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
+        const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
+        const bool in = m < p.M;
+        Ahead next;
+        next.load(c, ti.g, m, ti.n0 + w.c0, in && ti.n0 + w.c0 < p.N);
+#pragma unroll 1
+        for (int k = w.c0; k < w.c1 && ti.n0 + k < p.N; k += 32) {
+            const Ahead now = next;
+            next.load(c, ti.g, m, ti.n0 + k + 32, in && k + 32 < w.c1 && ti.n0 + k + 32 < p.N);
+            float v[32];
+            tmem_ld32(w.tmem + k, v);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= alpha;
+            now.add(c.beta, v);
+            uint32_t u[16];
+            if constexpr (LAST) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) u[i] = pack_bf16(v[2 * i] * scale, v[2 * i + 1] * scale);
+                if (by_map) {
+                    store_box<NBUF>(w, map, u, ti.n0 + k, row0, ti.g);
+                } else if (in) {
+                    __nv_bfloat16* to = out + ((int64_t)ti.g * p.M + m) * p.N + ti.n0 + k;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (ti.n0 + k + i < p.N) to[i] = __ushort_as_bfloat16((uint16_t)(u[i / 2] >> (i & 1 ? 16 : 0)));
+                }
+            } else {
+                uint32_t r[8];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    u[i] = pack_half(v[2 * i], v[2 * i + 1]);
+                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+                    const uint32_t e = __nv_cvt_float2_to_fp8x2(make_float2((v[2 * i] - h.x) * kResidual, (v[2 * i + 1] - h.y) * kResidual),
+                                                                __NV_SATFINITE, __NV_E5M2);
+                    r[i / 2] = i & 1 ? r[i / 2] | (e << 16) : e;
+                }
+                store_box<NBUF>(w, map, u, ti.n0 + k, row0, ti.g);
+                if (in) {
+                    uint4* to = reinterpret_cast<uint4*>(lo + ti.g * group + (int64_t)m * ld + ti.n0 + k);
+                    to[0] = make_uint4(r[0], r[1], r[2], r[3]);
+                    to[1] = make_uint4(r[4], r[5], r[6], r[7]);
+                }
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------- fp32
+// B = a I + b A + c A A, over A's square
+__global__ void __launch_bounds__(256) orth_poly_kernel(const float* __restrict__ A, float* __restrict__ sq, int64_t n, int64_t total) {
+    pdl_begin();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t at = i % (n * n);
+        sq[i] = fmaf(kC, sq[i], fmaf(kB, A[i], at / n == at % n ? kA : 0.f));
+    }
+}
+__global__ void __launch_bounds__(256) orth_out_kernel(const float* __restrict__ x, float* __restrict__ out, int64_t elems, float scale,
+                                                       const int32_t* __restrict__ counts) {
+    pdl_begin();
+    if (counts && counts[blockIdx.y] <= 0) return;
+    const int64_t base = blockIdx.y * elems;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += (int64_t)gridDim.x * 256) out[base + i] = x[base + i] * scale;
+}
+
+struct Plan {
+    int n;              // the smaller side
+    int64_t ld, ldn;    // row strides of X and of the squares
+    int parts;
+    size_t part, inv, x[2], lo[2], a, b, total;
+};
+
+Plan plan(int G, int rows, int cols, bool bf16) {
+    Plan p{};
+    p.n = std::min(rows, cols);
+    p.ld = bf16 ? ceil_div(cols, 64) * 64 : cols;
+    p.ldn = bf16 ? ceil_div(p.n, 64) * 64 : p.n;
+    const int64_t want = ceil_div((int64_t)rows * cols, 8 * 256);
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(16 * kPairs, G)));
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t here = at;
+        at += up(bytes);
+        return here;
+    };
+    const size_t xs = (size_t)G * rows * p.ld, as = (size_t)G * p.n * p.ldn, es = bf16 ? 2 : 4;
+    p.part = take((size_t)G * p.parts * 24);
+    p.inv = take((size_t)G * 4);
+    for (int i = 0; i < 2; ++i) p.x[i] = take(xs * es);
+    for (int i = 0; i < 2; ++i) p.lo[i] = bf16 ? take(xs) : 0;
+    p.a = take(as * es);
+    p.b = take(as * es);
+    p.total = at;
+    return p;
+}
+
+#define MOE_TRY(call)                              \
+    do {                                           \
+        const cudaError_t e_ = (call);             \
+        if (e_ != cudaSuccess) return e_;          \
+    } while (0)
+
+template <typename T, int N>
+cudaError_t start(const UpdateArgs& a, int G, void* hi, uint8_t* lo, cudaStream_t s) {
+    constexpr bool HALF = sizeof(T) == 2;
+    const dim3 grid((unsigned)a.parts, (unsigned)G);
+    (void)launch_pdl(orth_norm_kernel<T, N>, grid, dim3(256), 0, s, a);
+    (void)launch_pdl(orth_inv_kernel, dim3((unsigned)G), dim3(32), 0, s, a);
+    (void)launch_pdl(orth_start_kernel<T, N, HALF>, grid, dim3(256), 0, s, a, hi, lo);
+    return cudaGetLastError();
+}
+template <typename T>
+cudaError_t start_n(const UpdateArgs& a, int G, void* hi, uint8_t* lo, cudaStream_t s) {
+    if (a.cols % 8 == 0) return start<T, 8>(a, G, hi, lo, s);
+    if (a.cols % 4 == 0) return start<T, 4>(a, G, hi, lo, s);
+    if (a.cols % 2 == 0) return start<T, 2>(a, G, hi, lo, s);
+    return start<T, 1>(a, G, hi, lo, s);
+}
+
+template <bool A_MN, bool B_MN, typename Epi>
+cudaError_t product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, Problem p, const Epi& e, cudaStream_t s) {
+    if (pick_shape(p.M, p.N, p.K, 1, p.G, p.tri).pair) return launch_as<A_MN, B_MN, true, true, 8>(a, b, o, p, e, s);
+    return launch_as<A_MN, B_MN, false, true, 8>(a, b, o, p, e, s);
+}
+
+cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t s) {
+    const int R = o.rows, C = o.cols, G = o.groups, n = pl.n;
+    const bool tall = R > C;
+    const int64_t xg = R * pl.ld, ag = n * pl.ldn;
+    __half *A = (__half*)(ws + pl.a), *B = (__half*)(ws + pl.b);
+    CUtensorMap mx[2], sx[2], ma, sa, mb, sb, mo;
+    for (int i = 0; i < 2; ++i)
+        if (!make_map3(&mx[i], ws + pl.x[i], C, R, pl.ld, G, xg, false) || !make_map3(&sx[i], ws + pl.x[i], C, R, pl.ld, G, xg, true))
+            return cudaErrorInvalidValue;
+    if (!make_map3(&ma, A, n, n, pl.ldn, G, ag, false) || !make_map3(&sa, A, n, n, pl.ldn, G, ag, true) ||
+        !make_map3(&mb, B, n, n, pl.ldn, G, ag, false) || !make_map3(&sb, B, n, n, pl.ldn, G, ag, true))
+        return cudaErrorInvalidValue;
+    const bool by_map = C % 8 == 0;
+    if (by_map ? !make_map3(&mo, o.out, C, R, C, G, (int64_t)R * C, true) : (mo = sx[0], false)) return cudaErrorInvalidValue;
+    Problem sq = problem(n, n, tall ? R : C, G), cube = problem(n, n, n, G), step = problem(R, C, n, G);
+    sq.tri = cube.tri = 1;
+    sq.counts = cube.counts = step.counts = o.counts;
+    for (int i = 0; i < o.steps; ++i) {
+        const int x = i & 1, y = x ^ 1;
+        const Term none{nullptr, nullptr, 0, 0, 0.f};
+        const SymEpi ea{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag};
+        if (tall) MOE_TRY((product<true, true>(mx[x], mx[x], sa, sq, ea, s)));
+        else MOE_TRY((product<false, false>(mx[x], mx[x], sa, sq, ea, s)));
+        const SymEpi eb{{A, nullptr, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag};
+        MOE_TRY((product<false, false>(ma, ma, sb, cube, eb, s)));
+        const Term cx{(const __half*)(ws + pl.x[x]), (const uint8_t*)(ws + pl.lo[x]), pl.ld, xg, kA};
+        if (i + 1 < o.steps) {
+            const StepEpi<false> e{cx, 1.f / kScaleA, (uint8_t*)(ws + pl.lo[y]), pl.ld, xg, 1.f, nullptr, 1};
+            if (tall) MOE_TRY((product<false, false>(mx[x], mb, sx[y], step, e, s)));
+            else MOE_TRY((product<false, true>(mb, mx[x], sx[y], step, e, s)));
+        } else {
+            const StepEpi<true> e{cx, 1.f / kScaleA, nullptr, pl.ld, xg, o.scale / kScaleX, (__nv_bfloat16*)o.out, by_map};
+            if (tall) MOE_TRY((product<false, false>(mx[x], mb, mo, step, e, s)));
+            else MOE_TRY((product<false, true>(mb, mx[x], mo, step, e, s)));
+        }
+    }
+    return cudaSuccess;
+}
+
+cudaError_t steps_f32(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t s) {
+    const int R = o.rows, C = o.cols, G = o.groups, n = pl.n;
+    const bool tall = R > C;
+    float *A = (float*)(ws + pl.a), *B = (float*)(ws + pl.b);
+    const int64_t nn = (int64_t)n * n;
+    auto rows_by = [&](int rows, int K, const float* a, const float* b, int64_t b_elems, bool kmajor, int N, float* out) {
+        GemmMArgs m{};
+        m.G = G;
+        m.rows.rows = rows;
+        m.rows.a_stride = m.rows.out_stride = rows;
+        m.a = a;
+        m.b = b;
+        m.b_group_elems = b_elems;
+        m.b_kmajor = kmajor;
+        m.N = N;
+        m.K = K;
+        m.epi = EPI_STORE;
+        m.out0 = out;
+        return launch_gemm_m(m, false, s);
+    };
+    for (int i = 0; i < o.steps; ++i) {
+        float *x = (float*)(ws + pl.x[i & 1]), *y = (float*)(ws + pl.x[(i & 1) ^ 1]);
+        if (tall) {
+            GemmKArgs k{};
+            k.G = G;
+            k.rows.rows = R;
+            k.rows.a_stride = k.rows.b_stride = R;
+            k.a = k.b = x;
+            k.M = k.N = C;
+            k.out = A;
+            MOE_TRY(launch_gemm_k(k, false, s));
+        } else {
+            MOE_TRY(rows_by(R, C, x, x, (int64_t)R * C, true, R, A));
+        }
+        MOE_TRY(rows_by(n, n, A, A, nn, true, n, B));
+        (void)launch_pdl(orth_poly_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(nn * G, 256), 16 * 2 * kPairs)), dim3(256), 0, s,
+                         (const float*)A, B, (int64_t)n, nn * G);
+        MOE_TRY(cudaGetLastError());
+        if (tall) MOE_TRY(rows_by(R, C, x, B, nn, true, C, y));
+        else MOE_TRY(rows_by(R, R, B, x, (int64_t)R * C, false, C, y));
+    }
+    const int64_t elems = (int64_t)R * C;
+    (void)launch_pdl(orth_out_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(elems, 1024), 8 * kPairs), (unsigned)G), dim3(256), 0, s,
+                     (const float*)(ws + pl.x[o.steps & 1]), (float*)o.out, elems, o.scale, o.counts);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t orth_workspace_bytes(int groups, int rows, int cols, bool bf16) { return plan(groups, rows, cols, bf16).total; }
+
+cudaError_t launch_orthogonalise(const OrthArgs& o, void* workspace, cudaStream_t s) {
+    if (o.groups == 0) return cudaSuccess;
+    const Plan pl = plan(o.groups, o.rows, o.cols, o.bf16);
+    char* ws = (char*)workspace;
+    UpdateArgs a{};
+    a.g = o.g;
+    a.mom = o.momentum;
+    a.mom_out = o.momentum_out;
+    a.counts = o.counts;
+    a.elems = (int64_t)o.rows * o.cols;
+    a.cols = o.cols;
+    a.ld = pl.ld;
+    a.group = o.rows * pl.ld;
+    a.beta = o.beta;
+    a.nesterov = o.nesterov;
+    a.part = (double*)(ws + pl.part);
+    a.parts = pl.parts;
+    a.inv = (float*)(ws + pl.inv);
+    if (o.bf16) {
+        MOE_TRY(start_n<__nv_bfloat16>(a, o.groups, ws + pl.x[0], (uint8_t*)(ws + pl.lo[0]), s));
+        return steps_half(pl, o, ws, s);
+    }
+    MOE_TRY(start_n<float>(a, o.groups, ws + pl.x[0], nullptr, s));
+    return steps_f32(pl, o, ws, s);
+}
+
+cudaError_t orth_status(cudaStream_t s, int* code) { return tu_status_read_clear(s, code); }
+
+}  // namespace moe

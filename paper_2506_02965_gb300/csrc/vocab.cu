@@ -25,42 +25,12 @@ namespace {
 
 using namespace dense;
 
-constexpr int kPairs = 76;          // CTA pairs of the part: rules that also size workspaces do not ask the device
 constexpr int kMaxSplits = 16;      // of dh's contraction over the vocabulary
 constexpr int kF32Splits = 64;
 constexpr int kColChunk = 512;      // fp32: vocabulary rows whose statistics one CTA takes
 constexpr float kNegInf = -INFINITY;
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-
-// ---------------------------------------------------------------- tile shapes
-struct Shape {
-    bool pair;
-    int splits;
-};
-// Stages that a launch takes from first to last, in units of a pair's: rounds of tiles times the stages of one, a
-// 128 x 128 tile's stage being 0.92 of a pair's (it has a quarter of the operations but half of the operands'
-// bytes per SM). With splits, also the partial sums' way through memory (0.7 us a stage at 6.5 TB/s).
-Shape pick_shape(int64_t M, int64_t N, int64_t K, int max_splits) {
-    const int64_t stages = ceil_div(K, KST);
-    Shape best{true, 1};
-    double least = 0;
-    for (int pair = 1; pair >= 0; --pair) {
-        const int64_t t = pair ? 256 : 128, tiles = ceil_div(M, t) * ceil_div(N, t);
-        for (int s = 1; s <= max_splits && s <= stages; ++s) {
-            const int64_t each = ceil_div(stages, s), real = ceil_div(stages, each);
-            const int64_t rounds = ceil_div(tiles * real, pair ? kPairs : 2 * kPairs);
-            const double cost = (double)rounds * ((double)each + 2) * (pair ? 1.0 : 0.92) +
-                                (real > 1 ? 4 + (double)real * M * N * 8 / (6.5e6 * 0.7) : 0);
-            if (least == 0 || cost < least) {
-                least = cost;
-                best = {pair != 0, (int)real};
-            }
-        }
-    }
-    return best;
-}
 
 // ---------------------------------------------------------------- epilogues
 // The logits' tile: statistics of every row's share of columns, the target's logit, and (STORE) exp(z - m) in fp16.

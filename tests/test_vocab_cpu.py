@@ -72,3 +72,27 @@ def test_vocab_loss_workspace():
     assert size(T, d, V, L.MOE_F32, True) < 3 * 2 ** 30
     with pytest.raises(L.MoEError):
         size(4, 100, 10, L.MOE_BF16, True)
+
+
+@pytest.mark.parametrize("change,frag", [
+    (dict(groups=-1), "groups=-1"), (dict(rows=0), "rows=0"), (dict(cols=-4), "cols=-4"), (dict(rows=1 << 25), "sides"), (dict(dtype=9), "dtype"),
+    (dict(dw=None), "dw is NULL"), (dict(dw=24), "dw is not 16-byte"), (dict(momentum=None), "come together"),
+    (dict(momentum_out=None), "come together"), (dict(momentum=20), "momentum is not 16-byte"), (dict(beta=float("nan")), "beta"),
+    (dict(nesterov=2), "nesterov"), (dict(counts=18), "group_counts is not aligned"), (dict(steps=0), "steps=0"), (dict(steps=17), "steps=17"),
+    (dict(scale=float("inf")), "scale"), (dict(out=None), "out is NULL"), (dict(out=8), "out is not 16-byte"),
+    (dict(ws=None), "workspace is NULL"), (dict(ws=8), "workspace is not 16-byte"), (dict(wsb=100), "workspace of 100 bytes")])
+def test_orthogonalise(change, frag):
+    a = dict(groups=2, rows=64, cols=32, dtype=L.MOE_BF16, dw=16, momentum=16, beta=0.9, nesterov=1, counts=None, steps=5, scale=1.0,
+             momentum_out=16, out=16, ws=16, wsb=1 << 30)
+    a.update(change)
+    refused(frag, L.moe_orthogonalise, *a.values())
+
+
+def test_orthogonalise_limits():
+    refused("groups=257", L.moe_orthogonalise, 257, 8, 8, L.MOE_BF16, 16, None, 0.9, 1, None, 5, 1.0, None, 16, 16, 1 << 30,
+            status=L.MOE_ERR_UNSUPPORTED)
+    with pytest.raises(L.MoEError):
+        L.moe_orthogonalise_workspace_size(2, 0, 8, L.MOE_F32)
+    n = L.moe_orthogonalise_workspace_size(4, 5632, 1024, L.MOE_BF16)
+    assert 6 * 4 * 5632 * 1024 <= n <= 7 * 4 * 5632 * 1024
+    L.moe_orthogonalise(0, 8, 8, L.MOE_BF16, None, None, 0.9, 1, None, 5, 1.0, None, None, None, 0, stream=0)

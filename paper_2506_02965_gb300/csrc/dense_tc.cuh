@@ -7,7 +7,7 @@
 //
 // A persistent grid of CTA pairs with 256 x 256 tiles (cta_group::2: each CTA holds half of both operands'
 // rows), or of single CTAs with 128 x 128 tiles for problems of few tiles. Warp 0 copies by TMA, a stage is 128
-// contraction terms as two 64 x 128 boxes of each operand (64 KiB, three stages), warp 1 issues the MMAs into one of
+// contraction terms as two 64 x 128 boxes of each operand (64 KiB, three stages; see AR), warp 1 issues the MMAs into one of
 // two accumulators, the others run the epilogue of the other. What bounds a launch with a contraction of some
 // thousand terms is the tensor pipe under the power cap; the epilogues are measured where they are.
 //
@@ -27,14 +27,18 @@ namespace dense {
 using namespace tc;
 
 constexpr int KST = 128;                      // contraction terms per stage
-constexpr uint32_t BOX_BYTES = 64 * 128 * 2;  // one operand box
-constexpr uint32_t STAGE_BYTES = 4 * BOX_BYTES;
-constexpr int NST = 3;
+constexpr uint32_t BOX_BYTES = 64 * 128 * 2;  // one operand box (128 rows, or 128 contraction terms)
+// AR: rows of A that a CTA holds, 128, or 32 (single CTAs, K-major A): a few rows leave room for more stages, and what
+// such a launch waits for is B on its way (7 rows against 65536 x 2048: 75 us with three stages of 128 rows of both;
+// narrower tiles of B only make more stages of the same 1.1 us). The MMA reads 128 rows all the same: what follows the
+// box, bytes that only reach accumulator rows that nobody reads.
+constexpr uint32_t stage_bytes(int ar) { return 2 * (uint32_t)ar * 128 + 2 * BOX_BYTES; }
+constexpr int stages_of(int ar) { return ar == 128 ? 3 : 5; }
 constexpr int OUT_BOX = 32, OUT_BOX_BYTES = OUT_BOX * OUT_BOX * 2;  // epilogue staging: 32 x 32 of 16 bits
-constexpr int OUT_BOXES = 16;
-constexpr int SMEM_BYTES = 1024 + NST * (int)STAGE_BYTES + OUT_BOXES * OUT_BOX_BYTES;
+constexpr int out_boxes(int ar) { return ar == 128 ? 16 : 8; }
+constexpr int smem_bytes(int ar) { return 1024 + stages_of(ar) * (int)stage_bytes(ar) + out_boxes(ar) * OUT_BOX_BYTES; }
 constexpr int MAX_GROUPS = 256;
-static_assert(SMEM_BYTES + 2048 <= 227 * 1024, "shared memory of one SM");
+static_assert(smem_bytes(128) + 2048 <= 227 * 1024 && smem_bytes(32) + 2048 <= 227 * 1024, "shared memory of one SM");
 
 __host__ __device__ constexpr int threads(int ew) { return 64 + 32 * ew; }
 
@@ -106,17 +110,20 @@ __device__ __forceinline__ void store_box(Warp& w, const CUtensorMap* map, const
     ++w.seq;
 }
 
-template <bool A_MN, bool B_MN, bool PAIR, bool F16, int EW, typename Epi>
+template <bool A_MN, bool B_MN, bool PAIR, bool F16, int EW, int AR, typename Epi>
 __global__ void __launch_bounds__(threads(EW), 1)
     dense_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
                  const __grid_constant__ Problem p, const __grid_constant__ Epi epi) {
     pdl_begin();
     constexpr int NPAIR = PAIR ? 2 : 1;
     constexpr int TM = 128 * NPAIR, TN = 128 * NPAIR;
+    static_assert(AR == 128 || (AR == 32 && !PAIR && !A_MN), "rows of A");
+    constexpr int NST = stages_of(AR);
+    constexpr uint32_t STAGE_BYTES = stage_bytes(AR), BOX_A = (uint32_t)AR * 128;
     constexpr uint32_t IDESC = instr_desc<TN, A_MN, B_MN, TM>() & ~(F16 ? (1u << 7) | (1u << 10) : 0u);
     constexpr int TMEM_COLS = 2 * TN;
     constexpr int SPLIT = EW / 4;  // warps that share a lane quarter's columns
-    constexpr int NBUF = OUT_BOXES / EW;
+    constexpr int NBUF = out_boxes(AR) / EW;
     static_assert(EW == 4 || EW == 8, "epilogue warps");
 
     extern __shared__ uint8_t smem_raw[];
@@ -264,7 +271,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
                         ok = false;
                         break;
                     }
-                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + 2 * BOX_BYTES;
+                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + 2 * BOX_A;
                     const uint32_t fb = full0 + 8u * stage;
                     // only the leader arrives, for the bytes of both CTAs; the peer's copies complete on its
                     // barrier, after the leader's MMAs released the stage to both
@@ -272,8 +279,8 @@ __global__ void __launch_bounds__(threads(EW), 1)
                     const int k0 = kb * KST;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        if constexpr (A_MN) load(sa + i * BOX_BYTES, &tmA, fb, ti.m0 + 64 * i, k0, ti.g);
-                        else load(sa + i * BOX_BYTES, &tmA, fb, k0 + 64 * i, ti.m0, ti.g);
+                        if constexpr (A_MN) load(sa + i * BOX_A, &tmA, fb, ti.m0 + 64 * i, k0, ti.g);
+                        else load(sa + i * BOX_A, &tmA, fb, k0 + 64 * i, ti.m0, ti.g);
                     }
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -306,11 +313,11 @@ __global__ void __launch_bounds__(threads(EW), 1)
                 const bool got = wait_bar(full_bar(stage), phase);
                 fence_after();
                 if (lane == 0 && got) {
-                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + 2 * BOX_BYTES;
+                    const uint32_t sa = ring + stage * STAGE_BYTES, sb = sa + 2 * BOX_A;
 #pragma unroll
                     for (int kk = 0; kk < KST / 16; ++kk) {
                         const uint64_t ad = A_MN ? smem_desc(sa + kk * 2048, BOX_BYTES, 1024)
-                                                 : smem_desc(sa + (kk / 4) * BOX_BYTES + (kk % 4) * 32, 16, 1024);
+                                                 : smem_desc(sa + (kk / 4) * BOX_A + (kk % 4) * 32, 16, 1024);
                         const uint64_t bd = B_MN ? smem_desc(sb + kk * 2048, BOX_BYTES, 1024)
                                                  : smem_desc(sb + (kk / 4) * BOX_BYTES + (kk % 4) * 32, 16, 1024);
                         const uint32_t more = kb > ti.kb0 || kk > 0 ? 1u : 0u;
@@ -413,16 +420,17 @@ __global__ void __launch_bounds__(threads(EW), 1)
 
 // ------------------------------------------------------------------------ host side
 // A stack of G matrices [outer, inner], rows `ld` and matrices `group` elements apart (16 bytes or a multiple). As an
-// operand: boxes of 64 x 128, zeros outside; as an output: boxes of 32 x 32, nothing written outside.
-bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t ld, int G, int64_t group, bool store);
+// operand: boxes of 64 x 128 (box_rows: an A of 32 rows), zeros outside; as an output: boxes of 32 x 32, nothing written outside.
+bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t ld, int G, int64_t group, bool store,
+               int box_rows = 128);
 
-template <bool A_MN, bool B_MN, bool PAIR, bool F16, int EW, typename Epi>
+template <bool A_MN, bool B_MN, bool PAIR, bool F16, int EW, int AR = 128, typename Epi>
 static cudaError_t launch_as(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, Problem p, const Epi& epi, cudaStream_t s) {
-    constexpr int T = PAIR ? 256 : 128;
-    auto kern = dense_kernel<A_MN, B_MN, PAIR, F16, EW, Epi>;
-    cudaError_t e = allow_dynamic_smem<dense_kernel<A_MN, B_MN, PAIR, F16, EW, Epi>>(SMEM_BYTES);
+    constexpr int TM = PAIR ? 256 : 128, TN = TM, SMEM = smem_bytes(AR);
+    auto kern = dense_kernel<A_MN, B_MN, PAIR, F16, EW, AR, Epi>;
+    cudaError_t e = allow_dynamic_smem<dense_kernel<A_MN, B_MN, PAIR, F16, EW, AR, Epi>>(SMEM);
     if (e != cudaSuccess) return e;
-    const int64_t mt = (p.M + T - 1) / T, nt = (p.N + T - 1) / T;
+    const int64_t mt = (p.M + TM - 1) / TM, nt = (p.N + TN - 1) / TN;
     const int64_t tiles = (int64_t)p.G * p.splits * (p.tri ? mt * (mt + 1) / 2 : mt * nt);
     if (tiles <= 0) return cudaSuccess;
     int most = sm_count();
@@ -434,7 +442,7 @@ static cudaError_t launch_as(const CUtensorMap& a, const CUtensorMap& b, const C
             cudaLaunchConfig_t q = {};
             q.gridDim = dim3(2 * (sm_count() / 2));
             q.blockDim = dim3(threads(EW));
-            q.dynamicSmemBytes = SMEM_BYTES;
+            q.dynamicSmemBytes = SMEM;
             cudaLaunchAttribute qa[1];
             qa[0].id = cudaLaunchAttributeClusterDimension;
             qa[0].val.clusterDim.x = 2;
@@ -462,7 +470,7 @@ static cudaError_t launch_as(const CUtensorMap& a, const CUtensorMap& b, const C
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)at_once * (PAIR ? 2 : 1));
     cfg.blockDim = dim3(threads(EW));
-    cfg.dynamicSmemBytes = SMEM_BYTES;
+    cfg.dynamicSmemBytes = SMEM;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -9,11 +9,10 @@
 // the sorted tokens: no atomics, the same bits on every call. Three launches:
 //   sort    one cluster of 1 to 8 CTAs, a stable radix sort of (id, token) by digits of up to 9 bits; every
 //           warp owns a run of keys and counts their digits in shared memory, the CTAs read one another's
-//           totals through distributed shared memory;
-//   reduce  a party of threads per chunk of sorted tokens, a span of columns a thread: runs inside the chunk go
-//           to dW, the parts of runs that cross a chunk's ends to the workspace as fp32; other CTAs zero the
-//           rows without tokens meanwhile;
-//   join    runs that crossed: their parts in order of the chunks.
+//           totals through distributed shared memory; the other SMs zero dW meanwhile;
+//   sums    a party of threads per chunk of sorted tokens, a span of columns a thread: runs inside the chunk go
+//           to dW, the parts of runs that cross a chunk's ends to the workspace as fp32;
+//   joins   runs that crossed: their parts in order of the chunks.
 #include <algorithm>
 #include <type_traits>
 
@@ -28,11 +27,17 @@ namespace {
 constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32;
 constexpr int SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
 constexpr int SORT_MAX_CTAS = 8;
+constexpr int SORT_ONE = 4096;  // tokens that one CTA sorts
 constexpr int PARTY = 256;  // threads of a CTA of the lookup, the sums and the joins
 
-int chunk_len(int64_t T) { return T <= 8192 ? 32 : 64; }
-int64_t chunks_of(int64_t T) { return (T + chunk_len(T) - 1) / chunk_len(T); }
-int64_t words_of(int32_t V) { return ((int64_t)V + 31) / 32; }
+// Sorted tokens per chunk: as many as leave one to two thousand threads an SM, 8 to 64 (a thread has eight rows on their
+// way at once; each chunk leaves two rows of partial sums at most).
+int chunk_len(int64_t T, int32_t d) {
+    int n = 8;
+    while (n < 64 && T * d / (8 * n) >= 2 * 152 * 1024) n *= 2;
+    return n;
+}
+int64_t chunks_of(int64_t T, int32_t d) { return (T + chunk_len(T, d) - 1) / chunk_len(T, d); }
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // ---------------------------------------------------------------- lookup
@@ -74,76 +79,118 @@ __global__ void __launch_bounds__(PARTY) embed_fwd_kernel(const int32_t* __restr
 }
 
 // ---------------------------------------------------------------- sort
-struct SortBuf {
-    int32_t* key[2];
-    int32_t* tok[2];
-    uint32_t* used;  // a bit per id, or null
+struct SortArgs {
+    const int32_t* ids;
+    int64_t T;
+    int32_t V;
+    int passes, bits;
+    int32_t *key[2], *tok[2];  // between passes; [0]: the result
+    int32_t* runs;             // the sums' list of runs to join: its length, 0 here
+    uint8_t* zero;             // dW, or null
+    size_t zero_bytes;
 };
 
-// After an even number of passes the sorted tokens are in buffer 0, after an odd one in buffer 1.
-__global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(const int32_t* __restrict__ ids, int64_t T, int32_t V, int passes,
-                                                                  int bits, SortBuf b) {
+// Zeros by all threads of the CTAs that do not sort: 16-byte stores but for the ends.
+__device__ __forceinline__ void zero_fill(uint8_t* p, size_t bytes, int64_t part, int64_t parts) {
+    const size_t head = min((size_t)(-(intptr_t)p & 15), bytes), words = (bytes - head) / 16, tail = head + words * 16;
+    uint4* w = reinterpret_cast<uint4*>(p + head);
+    for (size_t i = (size_t)part; i < words; i += (size_t)parts) w[i] = make_uint4(0, 0, 0, 0);
+    if (part < (int64_t)head) p[part] = 0;
+    if (part < (int64_t)(bytes - tail)) p[tail + part] = 0;
+}
+
+// The lanes of `there` whose digit is this lane's (a ballot per bit)
+__device__ __forceinline__ uint32_t alike(uint32_t there, uint32_t digit, int bits) {
+    uint32_t m = there;
+    for (int b = 0; b < bits; ++b) {
+        const bool one = (digit >> b) & 1u;
+        const uint32_t v = __ballot_sync(there, one);
+        m &= one ? v : ~v;
+    }
+    return m;
+}
+
+// The first cluster sorts, the others zero dW. ONE: a cluster of one CTA, whose keys stay in shared memory between
+// passes (T <= SORT_ONE).
+template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(const SortArgs a, int ctas) {
     pdl_begin();
-    extern __shared__ int32_t s_hist[];  // [SORT_WARPS][bins]
+    if ((int)blockIdx.x >= ctas) {
+        zero_fill(a.zero, a.zero_bytes, (int64_t)(blockIdx.x - ctas) * SORT_THREADS + threadIdx.x, (int64_t)(gridDim.x - ctas) * SORT_THREADS);
+        return;
+    }
+    extern __shared__ int32_t s_hist[];  // [SORT_WARPS][bins], and of ONE [2][2][T] keys and tokens
     __shared__ int32_t s_tot[SORT_BINS], s_base[SORT_BINS], s_sum[SORT_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int ctas = (int)gridDim.x, cta = (int)blockIdx.x;  // (the grid is one cluster)
-    const int bins = 1 << bits;
-    const int64_t warps = (int64_t)ctas * SORT_WARPS;
+    const int cta = (int)blockIdx.x;
+    const int bits = a.bits, bins = 1 << bits;
+    const int64_t T = a.T, warps = (int64_t)ctas * SORT_WARPS;
     const int64_t per = ((T + warps - 1) / warps + 31) / 32 * 32;
     const int64_t beg = min64(T, (cta * SORT_WARPS + warp) * per), end = min64(T, beg + per);
     int32_t* hist = s_hist + warp * bins;
+    int32_t* held = s_hist + SORT_WARPS * bins;
 
-    if (b.used) {
-        const int64_t words = ((int64_t)V + 31) / 32;
-        for (int64_t i = (int64_t)cta * SORT_THREADS + threadIdx.x; i < words; i += (int64_t)ctas * SORT_THREADS) b.used[i] = 0;
-        tc::cluster_sync_all();
-    }
-    for (int p = 0; p < passes; ++p) {
-        const int shift = p * bits;
-        const int32_t *kin = b.key[p & 1], *tin = b.tok[p & 1];
-        int32_t *kout = b.key[(p + 1) & 1], *tout = b.tok[(p + 1) & 1];
-        // (through L2: another SM of the cluster wrote them)
+    for (int p = 0; p < a.passes; ++p) {
+        const int shift = p * bits, left = a.passes - 1 - p;
+        const int32_t *kin = ONE ? held + (left & 1) * 2 * T : a.key[(left + 1) & 1], *tin = ONE ? kin + T : a.tok[(left + 1) & 1];
+        int32_t *kout = ONE ? held + ((left + 1) & 1) * 2 * T : a.key[left & 1], *tout = ONE ? kout + T : a.tok[left & 1];
         auto key_at = [&](int64_t i) -> int32_t {
-            if (p > 0) return __ldcg(kin + i);
-            const int32_t id = ids[i];
-            return id < 0 || id >= V ? V : id;  // no row: after all others
+            if (p > 0) return ONE ? kin[i] : __ldcg(kin + i);  // (through L2: another SM of the cluster wrote them)
+            const int32_t id = a.ids[i];
+            if (id >= a.V) record_status(MOE_ERR_DEVICE_CHECK);
+            return id < 0 || id >= a.V ? a.V : id;  // no row: after all others
         };
         for (int i = lane; i < bins; i += 32) hist[i] = 0;
         __syncwarp();
-        for (int64_t i = beg + lane; i - lane < end; i += 32) {
-            const bool in = i < end;
-            const uint32_t there = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const int32_t k = key_at(i);
-                if (p == 0 && ids[i] >= V) record_status(MOE_ERR_DEVICE_CHECK);
-                const uint32_t d = ((uint32_t)k >> shift) & (uint32_t)(bins - 1);
-                const uint32_t same = __match_any_sync(there, d);
-                if ((same & ((1u << lane) - 1)) == 0) hist[d] += __popc(same);
-                if (p == 0 && b.used && k < V) atomicOr(b.used + (k >> 5), 1u << (k & 31));
+        // KEYS keys a lane at a time; a warp with no more than that keeps them for the second walk
+        constexpr int KEYS = 8;
+        int32_t k[KEYS];
+        auto load_keys = [&](int64_t i0) {
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j) {
+                const int64_t i = i0 + 32 * j + lane;
+                k[j] = i < end ? key_at(i) : 0;
             }
-            __syncwarp();
+        };
+        for (int64_t i0 = beg; i0 < end; i0 += 32 * KEYS) {
+            load_keys(i0);
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j) {
+                const int64_t i = i0 + 32 * j + lane;
+                if (i - lane >= end) break;
+                const uint32_t there = __ballot_sync(0xffffffffu, i < end);
+                if (i < end) {
+                    const uint32_t d = ((uint32_t)k[j] >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
+                    if ((same & ((1u << lane) - 1)) == 0) hist[d] += __popc(same);
+                }
+                __syncwarp();
+            }
         }
         __syncthreads();
         // digits in front of a warp's in its CTA, and the CTA's totals
         for (int d = threadIdx.x; d < bins; d += SORT_THREADS) {
-            int32_t run = 0;
+            int32_t n[SORT_WARPS], run = 0;
+#pragma unroll
+            for (int w = 0; w < SORT_WARPS; ++w) n[w] = s_hist[w * bins + d];
+#pragma unroll
             for (int w = 0; w < SORT_WARPS; ++w) {
-                const int32_t n = s_hist[w * bins + d];
                 s_hist[w * bins + d] = run;
-                run += n;
+                run += n[w];
             }
             s_tot[d] = run;
         }
-        tc::cluster_sync_all();
         // where a digit of this CTA begins: smaller digits of all CTAs, then this digit's of the CTAs before
         int32_t all = 0, before = 0;
-        if ((int)threadIdx.x < bins) {
-            const uint32_t mine = tc::smem_u32(&s_tot[threadIdx.x]);
-            for (int r = 0; r < ctas; ++r) {
-                const int32_t n = (int32_t)tc::ld_cluster(tc::map_to_rank(mine, (uint32_t)r));
-                if (r < cta) before += n;
-                all += n;
+        if constexpr (ONE) {
+            if ((int)threadIdx.x < bins) all = s_tot[threadIdx.x];  // (its own)
+        } else {
+            tc::cluster_sync_all();
+            if ((int)threadIdx.x < bins) {
+                const uint32_t mine = tc::smem_u32(&s_tot[threadIdx.x]);
+                for (int r = 0; r < ctas; ++r) {
+                    const int32_t n = (int32_t)tc::ld_cluster(tc::map_to_rank(mine, (uint32_t)r));
+                    if (r < cta) before += n;
+                    all += n;
+                }
             }
         }
         int32_t inc = all;
@@ -154,35 +201,55 @@ __global__ void __launch_bounds__(SORT_THREADS) embed_sort_kernel(const int32_t*
         }
         if (lane == 31) s_sum[warp] = inc;
         __syncthreads();
-        int32_t ahead = 0;
-        for (int w = 0; w < warp; ++w) ahead += s_sum[w];
-        if ((int)threadIdx.x < bins) s_base[threadIdx.x] = ahead + inc - all + before;
-        __syncthreads();
-        for (int64_t i = beg + lane; i - lane < end; i += 32) {
-            const bool in = i < end;
-            const uint32_t there = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const int32_t k = key_at(i);
-                const uint32_t d = ((uint32_t)k >> shift) & (uint32_t)(bins - 1);
-                const uint32_t same = __match_any_sync(there, d);
-                const int rank = __popc(same & ((1u << lane) - 1));
-                const int64_t at = s_base[d] + hist[d] + rank;
-                __syncwarp(there);
-                if (rank == 0) hist[d] += __popc(same);
-                kout[at] = k;
-                tout[at] = p > 0 ? __ldcg(tin + i) : (int32_t)i;
-            }
-            __syncwarp();
+        if ((int)threadIdx.x < bins) {
+            int32_t ahead = 0;
+            for (int w = 0; w < warp; ++w) ahead += s_sum[w];
+            s_base[threadIdx.x] = ahead + inc - all + before;
         }
-        tc::cluster_sync_all();  // the pass is written, and every CTA has read the totals
+        __syncthreads();
+        for (int64_t i0 = beg; i0 < end; i0 += 32 * KEYS) {
+            if (per > 32 * KEYS) load_keys(i0);
+            int32_t t[KEYS];
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j) {
+                const int64_t i = i0 + 32 * j + lane;
+                t[j] = p == 0 || i >= end ? (int32_t)i : ONE ? tin[i] : __ldcg(tin + i);
+            }
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j) {
+                const int64_t i = i0 + 32 * j + lane;
+                if (i - lane >= end) break;
+                const uint32_t there = __ballot_sync(0xffffffffu, i < end);
+                if (i < end) {
+                    const uint32_t d = ((uint32_t)k[j] >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
+                    const int rank = __popc(same & ((1u << lane) - 1));
+                    const int64_t at = s_base[d] + hist[d] + rank;
+                    __syncwarp(there);
+                    if (rank == 0) hist[d] += __popc(same);
+                    kout[at] = k[j];
+                    tout[at] = t[j];
+                }
+                __syncwarp();
+            }
+        }
+        // the pass is written, and every CTA has read the totals
+        if constexpr (ONE) __syncthreads();
+        else tc::cluster_sync_all();
     }
+    if constexpr (ONE) {  // out in whole lines (scattered 4-byte stores take a cycle each)
+        for (int i = threadIdx.x; i < (int)T; i += SORT_THREADS) {
+            a.key[0][i] = held[2 * T + i];
+            a.tok[0][i] = held[3 * T + i];
+        }
+    }
+    if (cta == 0 && threadIdx.x == 0) *a.runs = 0;
 }
 
 // ---------------------------------------------------------------- sums
 template <typename T> struct EmbedBwd {
     const int32_t* key;  // [T] sorted ids, V: no row
     const int32_t* tok;  // [T]
-    const uint32_t* used;
+    int32_t* runs;       // [1 + chunks]: how many runs leave the chunk that they begin in, and those chunks, in any order
     const T* dout;
     T* dw;
     float* part;  // [chunks][2][d]: of the run that came into the chunk, of the one that leaves it
@@ -190,7 +257,6 @@ template <typename T> struct EmbedBwd {
     int32_t V;
     uint32_t spr;  // spans per row
     int chunk, party, slabs;
-    int64_t sum_ctas;
     float scale;
     int accumulate;
 };
@@ -217,21 +283,6 @@ template <typename T, int N>
 __global__ void __launch_bounds__(PARTY) embed_sum_kernel(const EmbedBwd<T> a) {
     pdl_begin();
     constexpr int U = 8;
-    if ((int64_t)blockIdx.x >= a.sum_ctas) {
-        // rows without tokens: 32 ids, one word of the bit table, a warp at a time
-        const int64_t word = ((int64_t)blockIdx.x - a.sum_ctas) * (PARTY / 32) + (threadIdx.x >> 5);
-        if (word * 32 >= a.V) return;
-        const uint32_t used = a.used[word];
-        const int rows = (int)min64(32, a.V - word * 32);
-        Span<T, N> z;
-        z.zero();
-        for (int r = 0; r < rows; ++r) {
-            if ((used >> r) & 1u) continue;
-            T* row = a.dw + (word * 32 + r) * (int64_t)a.spr * N;
-            for (uint32_t c = threadIdx.x & 31; c < a.spr; c += 32) z.store(row + (int64_t)c * N);
-        }
-        return;
-    }
     const int parties = PARTY / a.party;
     const int64_t item = (int64_t)blockIdx.x * parties + threadIdx.x / a.party;
     const int64_t chunk = item / a.slabs;
@@ -251,12 +302,16 @@ __global__ void __launch_bounds__(PARTY) embed_sum_kernel(const EmbedBwd<T> a) {
     };
     for (int64_t p0 = beg; p0 < end; p0 += U) {
         Span<T, N> v[U];
-        int32_t k[U];
+        int32_t k[U], t[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             k[u] = p0 + u < end ? a.key[p0 + u] : a.V;
+            t[u] = p0 + u < end ? a.tok[p0 + u] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
             v[u].zero();
-            if (k[u] < a.V) v[u].load(a.dout + ((int64_t)a.tok[p0 + u] * a.spr + col) * N);
+            if (k[u] < a.V) v[u].load(a.dout + ((int64_t)t[u] * a.spr + col) * N);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -277,33 +332,80 @@ __global__ void __launch_bounds__(PARTY) embed_sum_kernel(const EmbedBwd<T> a) {
     }
     const bool leaves = end < a.n && a.key[end] == run;
     if (came) part(0);
-    else if (leaves) part(1);
-    else embed_put<T, N>(a, run, col, acc);
+    else if (leaves) {
+        part(1);
+        if (col == 0) a.runs[1 + atomicAdd(a.runs, 1)] = (int32_t)chunk;
+    } else embed_put<T, N>(a, run, col, acc);
 }
 
-// A run that begins in a chunk and leaves it: the chunk's part, then those of the chunks that it comes into.
+template <typename T, int N>
+__device__ __forceinline__ void load_part(const EmbedBwd<T>& a, int64_t slot, uint32_t col, float (&v)[N]) {
+    constexpr int W = N < 4 ? N : 4;
+    const float* p = a.part + (slot * a.spr + col) * N;
+#pragma unroll
+    for (int i = 0; i < N / W; ++i) {
+        Span<float, W> s;
+        float f[W];
+        s.load(p + i * W);
+        s.unpack(f);
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[i * W + j] = f[j];
+    }
+}
+
+// A run that begins in a chunk and leaves it: the chunk's part and those of the chunks that it comes into. A CTA per run and
+// slab of columns; its parties take equal shares of the run's chunks, each with JOIN parts on their way at once, and
+// their sums are added in order. (The list's order is that of the sums' CTAs: it decides who does what, and no sum.)
+constexpr int JOIN = 8;
 template <typename T, int N>
 __global__ void __launch_bounds__(PARTY) embed_join_kernel(const EmbedBwd<T> a) {
     pdl_begin();
-    const int parties = PARTY / a.party;
-    const int64_t item = (int64_t)blockIdx.x * parties + threadIdx.x / a.party;
-    const int64_t chunk = item / a.slabs;
-    const uint32_t col = (uint32_t)(item % a.slabs) * a.party + threadIdx.x % a.party;
-    const int64_t beg = chunk * a.chunk, end = beg + a.chunk;
-    if (end >= a.n || col >= a.spr) return;
-    const int32_t run = a.key[end - 1];
-    if (run >= a.V || a.key[end] != run) return;                       // nothing leaves
-    if (a.key[beg] == run && beg > 0 && a.key[beg - 1] == run) return;  // it came in: not its first chunk
-    float acc[N];
-    const float* p = a.part + ((chunk * 2 + 1) * a.spr + col) * N;
+    __shared__ float s_sum[PARTY][N];
+    const int64_t chunks = (a.n + a.chunk - 1) / a.chunk, items = (int64_t)a.runs[0] * a.slabs;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t chunk = a.runs[1 + item / a.slabs];
+        const int32_t run = a.key[(chunk + 1) * a.chunk];
+        int64_t more = 0;  // chunks that the run comes into
+        for (;;) {
+            const int64_t c = chunk + 1 + more + threadIdx.x;
+            const int n = __syncthreads_count(c < chunks && a.key[c * a.chunk] == run);
+            more += n;
+            if (n < PARTY) break;
+        }
+        const int parties = PARTY / a.party, party = threadIdx.x / a.party;
+        const uint32_t col = (uint32_t)(item % a.slabs) * a.party + threadIdx.x % a.party;
+        const int64_t share = (more + parties - 1) / parties;
+        const int64_t c0 = chunk + 1 + min64(more, party * share), c1 = chunk + 1 + min64(more, (party + 1) * share);
+        float acc[N];
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] = p[j];
-    for (int64_t c = chunk + 1; c * a.chunk < a.n && a.key[c * a.chunk] == run; ++c) {
-        p = a.part + (c * 2 * a.spr + col) * N;
+        for (int j = 0; j < N; ++j) acc[j] = 0.f;
+        if (col < a.spr) {
+            if (party == 0) load_part<T, N>(a, chunk * 2 + 1, col, acc);
+            for (int64_t c = c0; c < c1; c += JOIN) {
+                float v[JOIN][N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) acc[j] += p[j];
+                for (int u = 0; u < JOIN; ++u) {
+#pragma unroll
+                    for (int j = 0; j < N; ++j) v[u][j] = 0.f;
+                    if (c + u < c1) load_part<T, N>(a, (c + u) * 2, col, v[u]);
+                }
+#pragma unroll
+                for (int u = 0; u < JOIN; ++u)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) acc[j] += v[u][j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) s_sum[threadIdx.x][j] = acc[j];
+        __syncthreads();
+        if (party == 0 && col < a.spr) {
+            for (int q = 1; q < parties; ++q)
+#pragma unroll
+                for (int j = 0; j < N; ++j) acc[j] += s_sum[threadIdx.x + q * a.party][j];
+            embed_put<T, N>(a, run, col, acc);
+        }
+        __syncthreads();
     }
-    embed_put<T, N>(a, run, col, acc);
 }
 
 // elements per access that the rows' width and the buffers' addresses allow, up to 16 bytes
@@ -334,19 +436,18 @@ cudaError_t sums(EmbedBwd<T> a, int32_t d, cudaStream_t s) {
     while (a.party < PARTY && (uint32_t)a.party < a.spr) a.party *= 2;
     a.slabs = (int)((a.spr + a.party - 1) / a.party);
     const int64_t items = (a.n + a.chunk - 1) / a.chunk * a.slabs, parties = PARTY / a.party;
-    a.sum_ctas = (items + parties - 1) / parties;
-    const int64_t zero_ctas = a.accumulate ? 0 : (words_of(a.V) + PARTY / 32 - 1) / (PARTY / 32);
-    (void)launch_pdl(embed_sum_kernel<T, N>, dim3((unsigned)(a.sum_ctas + zero_ctas)), dim3(PARTY), 0, s, a);
+    const unsigned ctas = (unsigned)((items + parties - 1) / parties);
+    (void)launch_pdl(embed_sum_kernel<T, N>, dim3(ctas), dim3(PARTY), 0, s, a);
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess || a.n <= a.chunk) return e;
-    (void)launch_pdl(embed_join_kernel<T, N>, dim3((unsigned)a.sum_ctas), dim3(PARTY), 0, s, a);
+    (void)launch_pdl(embed_join_kernel<T, N>, dim3((unsigned)std::min<int64_t>(items, 4 * sm_count())), dim3(PARTY), 0, s, a);
     return cudaGetLastError();
 }
 
 }  // namespace
 
 size_t embed_workspace_bytes(int64_t T, int32_t d, int32_t V) {
-    return 4 * up((size_t)T * 4) + up((size_t)words_of(V) * 4) + up((size_t)chunks_of(T) * 2 * (size_t)d * 4);
+    return 4 * up((size_t)T * 4)+ up((size_t)(chunks_of(T, d) + 1) * 4) + up((size_t)chunks_of(T, d) * 2 * (size_t)d * 4);
 }
 
 cudaError_t launch_embed_fwd(const int32_t* ids, int64_t T, int32_t d, int32_t V, bool bf16, const void* w, float scale, void* out,
@@ -368,7 +469,7 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
                              bool accumulate, void* dw, void* ws, cudaStream_t s) {
     if (T == 0)
         return accumulate ? cudaSuccess : cudaMemsetAsync(dw, 0, (size_t)V * (size_t)d * (bf16 ? 2 : 4), s);
-    SortBuf b{};
+    SortArgs b{};
     char* at = (char*)ws;
     for (int i = 0; i < 2; ++i) {
         b.key[i] = (int32_t*)at;
@@ -376,20 +477,28 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
         b.tok[i] = (int32_t*)at;
         at += up((size_t)T * 4);
     }
-    uint32_t* used = (uint32_t*)at;
-    at += up((size_t)words_of(V) * 4);
-    b.used = accumulate ? nullptr : used;
+    b.runs = (int32_t*)at;
+    at += up((size_t)(chunks_of(T, d) + 1) * 4);
+    b.ids = ids;
+    b.T = T;
+    b.V = V;
+    if (!accumulate) {
+        b.zero = (uint8_t*)dw;
+        b.zero_bytes = (size_t)V * (size_t)d * (bf16 ? 2 : 4);
+    }
     // keys are 0 .. V: digits of equal width, as few passes as 9 bits allow
     int all = 1;
     while (((int64_t)V >> all) > 0) ++all;
-    const int passes = (all + SORT_BITS - 1) / SORT_BITS, bits = (all + passes - 1) / passes;
-    int ctas = 1;
-    while (ctas < SORT_MAX_CTAS && (int64_t)ctas * 2048 < T) ctas *= 2;
-    const size_t smem = (size_t)SORT_WARPS * (size_t)(1 << bits) * 4;
-    cudaError_t e = allow_dynamic_smem<embed_sort_kernel>((size_t)SORT_WARPS * SORT_BINS * 4);
+    b.passes = (all + SORT_BITS - 1) / SORT_BITS;
+    b.bits = (all + b.passes - 1) / b.passes;
+    const bool one = T <= SORT_ONE;
+    int ctas = one ? 1 : 2;
+    while (!one && ctas < SORT_MAX_CTAS && (int64_t)ctas * 4096 < T) ctas *= 2;
+    const size_t smem = (size_t)SORT_WARPS * (size_t)(1 << b.bits) * 4 + (one ? (size_t)T * 16 : 0);
+    cudaError_t e = allow_dynamic_smem<embed_sort_kernel<true>>((size_t)SORT_WARPS * SORT_BINS * 4 + (size_t)SORT_ONE * 16);
+    if (e == cudaSuccess) e = allow_dynamic_smem<embed_sort_kernel<false>>((size_t)SORT_WARPS * SORT_BINS * 4);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)ctas);
     cfg.blockDim = dim3(SORT_THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -400,21 +509,45 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    // dW is zeroed by the SMs that do not sort, in one round: as many clusters as fit at once (19 of eight CTAs do
+    // not: 131072 x 4096 237 us in two rounds)
+    int clusters = 1;
+    if (!accumulate) {
+        static std::atomic<int> resident[kMaxDevices][2] = {};
+        const int dev = current_device();
+        std::atomic<int>* kept = dev >= 0 && dev < kMaxDevices && (one || ctas == SORT_MAX_CTAS) ? &resident[dev][one] : nullptr;
+        clusters = kept ? kept->load() : 0;
+        if (!clusters) {
+            cfg.gridDim = dim3((unsigned)(sm_count() / ctas * ctas));
+            if ((one ? cudaOccupancyMaxActiveClusters(&clusters, embed_sort_kernel<true>, &cfg)
+                     : cudaOccupancyMaxActiveClusters(&clusters, embed_sort_kernel<false>, &cfg)) != cudaSuccess ||
+                clusters < 2) {
+                (void)cudaGetLastError();
+                clusters = 2;
+            }
+            clusters = std::min(clusters, sm_count() / ctas);
+            if (kept) *kept = clusters;
+        }
+    }
+    cfg.gridDim = dim3((unsigned)(clusters * ctas));
     cfg.numAttrs = 2;
-    if ((e = cudaLaunchKernelEx(&cfg, embed_sort_kernel, ids, T, V, passes, bits, b)) != cudaSuccess) return e;
+    if ((e = one ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<true>, b, ctas) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<false>, b, ctas)) !=
+        cudaSuccess)
+        return e;
 
     auto args = [&](auto* t) {
         using E = std::remove_pointer_t<decltype(t)>;
         EmbedBwd<E> a{};
-        a.key = b.key[passes & 1];
-        a.tok = b.tok[passes & 1];
-        a.used = used;
+        a.key = b.key[0];
+        a.tok = b.tok[0];
+        a.runs = b.runs;
         a.dout = (const E*)dout;
         a.dw = (E*)dw;
         a.part = (float*)at;
         a.n = T;
         a.V = V;
-        a.chunk = chunk_len(T);
+        a.chunk = chunk_len(T, d);
         a.scale = scale;
         a.accumulate = accumulate;
         return a;

@@ -25,7 +25,8 @@ namespace {
 
 using namespace dense;
 
-constexpr int kMaxSplits = 16;      // of dh's contraction over the vocabulary
+constexpr int kMaxSplits = 16;      // of dh's contraction over the vocabulary (four times as many for up to 128 tokens)
+constexpr int kShortRows = 256;     // dw of up to so many tokens: eight epilogue warps
 constexpr int kF32Splits = 64;
 constexpr int kColChunk = 512;      // fp32: vocabulary rows whose statistics one CTA takes
 constexpr float kNegInf = -INFINITY;
@@ -135,31 +136,23 @@ template <int MODE> struct OutEpi {
 // ---------------------------------------------------------------- passes
 __device__ __forceinline__ bool has_target(int y, int V) { return y >= 0 && y < V; }
 
-constexpr int kPrep = 1024;
 // scal[0] = the largest |weight| of a token with a target, or 1 / (tokens with a target); scal[1] = 1 / scal[0] or 0.
-// (fp32: also the vocabulary's parts as row offsets.)
-__global__ void __launch_bounds__(kPrep) vocab_prep_kernel(const int32_t* __restrict__ target, const float* __restrict__ weight, int64_t T,
-                                                          int V, float* __restrict__ scal, int32_t* __restrict__ offsets, int splits,
-                                                          int rows) {
-    pdl_begin();
+// One CTA of whole warps, up to 32.
+__device__ __forceinline__ void weights_scale(const int32_t* target, const float* weight, int64_t T, int V, float* scal) {
     __shared__ float s_max[32];
     __shared__ int s_n[32];
     float most = 0.f;
     int n = 0;
-    bool bad = false, nan = false;
-    for (int64_t t = threadIdx.x; t < T; t += kPrep) {
+    bool bad = false;
+    for (int64_t t = threadIdx.x; t < T; t += blockDim.x) {
         const int y = target[t];
         bad |= y >= V;
         if (!has_target(y, V)) continue;
         ++n;
-        if (weight) {
-            most = fmaxf(most, fabsf(weight[t]));
-            nan |= weight[t] != weight[t];
-        }
+        if (weight) most = weight[t] == weight[t] ? fmaxf(most, fabsf(weight[t])) : INFINITY;
     }
     if (bad) record_status(MOE_ERR_DEVICE_CHECK);
-    if (nan) most = INFINITY;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     most = warp_max(most);
     n = __reduce_add_sync(0xffffffffu, n);
     if (lane == 0) {
@@ -168,8 +161,8 @@ __global__ void __launch_bounds__(kPrep) vocab_prep_kernel(const int32_t* __rest
     }
     __syncthreads();
     if (warp == 0) {
-        most = warp_max(s_max[lane]);
-        n = __reduce_add_sync(0xffffffffu, s_n[lane]);
+        most = warp_max(lane < warps ? s_max[lane] : 0.f);
+        n = __reduce_add_sync(0xffffffffu, lane < warps ? s_n[lane] : 0);
         if (lane == 0) {
             // (weights with an infinity or a NaN are taken as they are)
             const float a = weight ? (most < 3.4e38f ? most : 1.f) : 1.f / (float)max(n, 1);
@@ -177,52 +170,119 @@ __global__ void __launch_bounds__(kPrep) vocab_prep_kernel(const int32_t* __rest
             scal[1] = a > 0.f ? 1.f / a : 0.f;
         }
     }
-    if (offsets)
-        for (int i = threadIdx.x; i <= splits; i += kPrep) offsets[i] = (int)min64(V, (int64_t)i * rows);
+    __syncthreads();
 }
 
-// lse and the token's loss from its shares' statistics: a warp per token.
-__global__ void __launch_bounds__(256) vocab_join_kernel(const float2* __restrict__ part, int shares, int64_t rows,
-                                                         const int32_t* __restrict__ target, int V, const float* __restrict__ zy,
-                                                         const float* __restrict__ zt, float* __restrict__ lse, float* __restrict__ token) {
-    pdl_begin();
-    const int64_t t = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31;
-    if (t >= rows) return;
-    const float2* p = part + t * shares;
-    float m = kNegInf;
-    for (int i = lane; i < shares; i += 32) m = fmaxf(m, p[i].x);
-    m = warp_max(m);
-    const float ref = m == kNegInf ? 0.f : m;
-    float s = 0.f;
-    for (int i = lane; i < shares; i += 32) s += p[i].y * expf(p[i].x - ref);
-    s = warp_sum(s);
-    if (lane == 0) {
-        const float l = ref + logf(s);
-        const int y = target[t];
-        lse[t] = l;
-        token[t] = has_target(y, V) ? l - (zt ? zt[(int64_t)y * rows + t] : zy[t]) : 0.f;
-    }
-}
-
-// loss = sum of u_t l_t: one CTA, a fixed order, in 64 bits.
-__global__ void __launch_bounds__(1024) vocab_total_kernel(const float* __restrict__ token, const int32_t* __restrict__ target,
-                                                           const float* __restrict__ weight, const float* __restrict__ scal, int64_t T,
-                                                           int V, float* __restrict__ loss) {
-    pdl_begin();
+// loss = sum of u_t l_t by one CTA of whole warps: a fixed order, in 64 bits.
+__device__ __forceinline__ void total_loss(const float* token, const int32_t* target, const float* weight, const float* scal, int64_t T, int V,
+                                           float* loss) {
     __shared__ double s_part[32];
     double sum = 0.0;
-    for (int64_t t = threadIdx.x; t < T; t += 1024)
-        if (has_target(target[t], V)) sum += (double)token[t] * (weight ? weight[t] : scal[0]);
+    const float u = scal[0];
+    for (int64_t t = threadIdx.x; t < T; t += blockDim.x)
+        if (has_target(target[t], V)) sum += (double)token[t] * (weight ? weight[t] : u);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5] = sum;
     __syncthreads();
     if (threadIdx.x < 32) {
-        sum = s_part[threadIdx.x];
+        sum = threadIdx.x < (blockDim.x >> 5) ? s_part[threadIdx.x] : 0.0;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (threadIdx.x == 0) *loss = (float)sum;
+    }
+}
+__global__ void __launch_bounds__(1024) vocab_total_kernel(const float* __restrict__ token, const int32_t* __restrict__ target,
+                                                           const float* __restrict__ weight, const float* __restrict__ scal, int64_t T,
+                                                           int V, float* __restrict__ loss) {
+    pdl_begin();
+    total_loss(token, target, weight, scal, T, V, loss);
+}
+
+struct JoinArgs {
+    const float2* part;
+    int shares, V, d;
+    int64_t rows;
+    const int32_t* target;   // of the piece's first token
+    const float* zy;         // bf16: the target's logit as the product has it
+    const __nv_bfloat16 *h, *w;
+    const float* zt;         // fp32: the transposed logits
+    float *lse, *token;
+    // the whole batch
+    const int32_t* all_target;
+    const float* all_weight;
+    int64_t T;
+    float* scal;             // null: not in this launch
+    float* loss;             // one CTA that holds the whole batch: the loss too
+    const float* all_token;
+    int32_t* offsets;        // fp32: the vocabulary's parts as row offsets, or null
+    int splits, split_rows;
+};
+// <h, w> of d values in fp32, by a warp
+__device__ __forceinline__ float warp_dot(const __nv_bfloat16* h, const __nv_bfloat16* w, int d, int lane) {
+    float s = 0.f;
+#pragma unroll 4
+    for (int i = lane * 8; i < d; i += 256) {
+        float a[8], b[8];
+        unpack8(ldg_nc(h + i), a);
+        unpack8(ldg_nc(w + i), b);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s = fmaf(a[j], b[j], s);
+    }
+    return warp_sum(s);
+}
+// lse and the token's loss from its shares' statistics: a warp per token, and one more CTA for what the batch needs as a
+// whole. In bf16 the target's logit is taken once more as an fp32 dot product: the tensor cores' accumulators truncate,
+// which leaves a large logit a few 1e-6 of it short (7 tokens, d = 2048: the losses 1.2e-6 off, and 1e-7 with
+// this); lse follows by its share p_y of the difference.
+template <bool BF16> __global__ void __launch_bounds__(1024) vocab_join_kernel(const JoinArgs a) {
+    pdl_begin();
+    const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
+    if (a.scal && blockIdx.x == gridDim.x - 1) {
+        weights_scale(a.all_target, a.all_weight, a.T, a.V, a.scal);
+        if (a.offsets)
+            for (int i = threadIdx.x; i <= a.splits; i += blockDim.x) a.offsets[i] = (int)min64(a.V, (int64_t)i * a.split_rows);
+        if (!a.loss) return;
+    }
+    const int64_t t = a.loss ? threadIdx.x >> 5 : (int64_t)blockIdx.x * warps + (threadIdx.x >> 5);
+    if (t < a.rows) {
+        const float2* p = a.part + t * a.shares;
+        const int y = a.target[t];
+        float m = kNegInf, s = 0.f;
+        for (int i0 = lane; i0 < a.shares; i0 += 256) {  // eight shares on their way at once
+            float2 v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = i0 + 32 * k < a.shares ? p[i0 + 32 * k] : make_float2(kNegInf, 0.f);
+            float top = m;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) top = fmaxf(top, v[k].x);
+            const float ref = top == kNegInf ? 0.f : top;
+            s *= expf(m - ref);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k].y * expf(v[k].x - ref);
+            m = top;
+        }
+        const float top = warp_max(m), ref = top == kNegInf ? 0.f : top;
+        s = warp_sum(s * expf(m - ref));
+        float lse = ref + logf(s), l = 0.f;
+        if (has_target(y, a.V)) {
+            if constexpr (BF16) {
+                const float z = a.zy[t], off = warp_dot(a.h + t * a.d, a.w + (int64_t)y * a.d, a.d, lane) - z;
+                const float mine = expf(z - lse) * off;
+                l = (lse - z) - (off - mine);
+                lse += mine;
+            } else {
+                l = lse - a.zt[(int64_t)y * a.rows + t];
+            }
+        }
+        if (lane == 0) {
+            a.lse[t] = lse;
+            a.token[t] = l;
+        }
+    }
+    if (a.loss) {
+        __syncthreads();
+        total_loss(a.all_token, a.all_target, a.all_weight, a.scal, a.T, a.V, a.loss);
     }
 }
 
@@ -232,14 +292,26 @@ __device__ __forceinline__ void live_row(const uint4* h, uint4* to, int64_t t, i
     for (int i = (int)threadIdx.x; i < words; i += 256) to[t * words + i] = live ? h[t * words + i] : make_uint4(0, 0, 0, 0);
 }
 
+struct TotalArgs {  // of the whole batch; loss null: not in this launch
+    const float* token;
+    const int32_t* target;
+    const float* weight;
+    int64_t T;
+    float* loss;
+};
 // exp(z - m) in fp16 -> dz / scal[0] in bf16, in place. Rows of ld elements, eight a thread.
 __global__ void __launch_bounds__(256) vocab_dz_kernel(uint4* __restrict__ e, int64_t ld, const float2* __restrict__ part, int shares,
                                                        int share, const float* __restrict__ lse, const int32_t* __restrict__ target,
                                                        const float* __restrict__ weight, const float* __restrict__ scal, int V,
-                                                       const uint4* __restrict__ h, uint4* __restrict__ h_live, int words) {
+                                                       const uint4* __restrict__ h, uint4* __restrict__ h_live, int words,
+                                                       const TotalArgs total) {
     pdl_begin();
     constexpr int U = 4;
     const int64_t t = blockIdx.y;
+    if (total.loss && blockIdx.x == gridDim.x - 1) {  // one more column of CTAs, of which the first adds up the batch
+        if (t == 0) total_loss(total.token, total.target, total.weight, scal, total.T, V, total.loss);
+        return;
+    }
     const int y = target[t];
     const bool live = has_target(y, V);
     if (blockIdx.x == 0) live_row(h, h_live, t, words, live);
@@ -345,7 +417,7 @@ struct Plan {
     int64_t ld;    // bf16: row stride of the stored exp(z - m)
     int shares, share;
     Shape logits, dh, dw;
-    int ew;        // epilogue warps of the logits
+    int ew, dw_ew; // epilogue warps of the logits, of dw
     int f32_splits, f32_rows;
     // workspace: offsets
     size_t scal, token, lse, zy, part, e, live, sums, dwsum, offsets, total;
@@ -363,9 +435,11 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
         p.pieces = (int)ceil_div(t1, p.rows);
         p.ld = ceil_div(V, 64) * 64;
         p.logits = pick_shape(p.rows, V, d, 1);
-        p.dh = pick_shape(p.rows, d, V, kMaxSplits);
+        p.dh = pick_shape(p.rows, d, V, p.rows <= 128 ? 4 * kMaxSplits : kMaxSplits);
         p.dw = pick_shape(V, d, p.rows, 1);
         p.ew = d < 1024 ? 8 : 4;  // a short contraction: the epilogue, not the product, sets a tile's time
+        // a contraction of a few stages: the stores set the time
+        p.dw_ew = p.rows <= kShortRows ? 8 : 4;
         p.share = (p.logits.pair ? 256 : 128) / (p.ew / 4);
         p.shares = (int)ceil_div(V, p.share);
     } else {
@@ -409,6 +483,8 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
     return p;
 }
 
+bool short_a(bool pair, int64_t rows) { return !pair && rows <= 32; }
+
 template <bool STORE>
 cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const VocabEpi<STORE>& e,
                    cudaStream_t s) {
@@ -416,13 +492,26 @@ cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, c
         if (pl.ew == 8) return launch_as<false, false, true, false, 8>(a, b, o, p, e, s);
         return launch_as<false, false, true, false, 4>(a, b, o, p, e, s);
     }
+    if (short_a(pl.logits.pair, p.M)) {
+        if (pl.ew == 8) return launch_as<false, false, false, false, 8, 32>(a, b, o, p, e, s);
+        return launch_as<false, false, false, false, 4, 32>(a, b, o, p, e, s);
+    }
     if (pl.ew == 8) return launch_as<false, false, false, false, 8>(a, b, o, p, e, s);
     return launch_as<false, false, false, false, 4>(a, b, o, p, e, s);
 }
 template <bool A_MN, int MODE>
-cudaError_t product(bool pair, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const OutEpi<MODE>& e,
+cudaError_t product(bool pair, int ew, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const OutEpi<MODE>& e,
                     cudaStream_t s) {
+    if constexpr (A_MN && MODE == OUT_BF16) {
+        if (ew == 8) {
+            if (pair) return launch_as<A_MN, true, true, false, 8>(a, b, o, p, e, s);
+            return launch_as<A_MN, true, false, false, 8>(a, b, o, p, e, s);
+        }
+    }
     if (pair) return launch_as<A_MN, true, true, false, 4>(a, b, o, p, e, s);
+    if constexpr (!A_MN) {
+        if (short_a(pair, p.M)) return launch_as<A_MN, true, false, false, 4, 32>(a, b, o, p, e, s);
+    }
     return launch_as<A_MN, true, false, false, 4>(a, b, o, p, e, s);
 }
 
@@ -441,9 +530,39 @@ cudaError_t sum_splits(const float* sums, int splits, int64_t n, const float* al
 
 float* token_loss(const Plan& pl, const VocabArgs& a, char* ws) { return a.token_loss ? a.token_loss : (float*)(ws + pl.token); }
 
-cudaError_t join(const Plan& pl, const VocabArgs& a, char* ws, int64_t t0, int64_t n, const float* zt, cudaStream_t s) {
-    (void)launch_pdl(vocab_join_kernel, dim3((unsigned)ceil_div(n, 8)), dim3(256), 0, s, (const float2*)(ws + pl.part), pl.shares, n,
-                     a.target + t0, a.V, (const float*)(ws + pl.zy), zt, (float*)(ws + pl.lse), token_loss(pl, a, ws) + t0);
+// One CTA for a batch of few tokens, which then has the loss too.
+bool few(const VocabArgs& a) { return a.T <= 32; }
+
+cudaError_t join(const Plan& pl, const VocabArgs& a, char* ws, int piece, int64_t t0, int64_t n, const float* zt, cudaStream_t s) {
+    JoinArgs j{};
+    j.part = (const float2*)(ws + pl.part);
+    j.shares = pl.shares;
+    j.V = a.V;
+    j.d = a.d;
+    j.rows = n;
+    j.target = a.target + t0;
+    j.zy = (const float*)(ws + pl.zy);
+    j.zt = zt;
+    j.lse = (float*)(ws + pl.lse);
+    j.all_token = token_loss(pl, a, ws);
+    j.token = token_loss(pl, a, ws) + t0;
+    j.all_target = a.target;
+    j.all_weight = a.weight;
+    j.T = a.T;
+    if (piece == 0) j.scal = (float*)(ws + pl.scal);
+    if (few(a)) j.loss = a.loss;
+    const int warps = few(a) ? (int)a.T : 8;
+    const unsigned ctas = few(a) ? 1 : (unsigned)(ceil_div(n, warps) + (piece == 0));
+    if (a.bf16) {
+        j.h = (const __nv_bfloat16*)a.h + t0 * a.d;
+        j.w = (const __nv_bfloat16*)a.w;
+        (void)launch_pdl(vocab_join_kernel<true>, dim3(ctas), dim3(32 * warps), 0, s, j);
+    } else {
+        if (a.dh && piece == 0) j.offsets = (int32_t*)(ws + pl.offsets);
+        j.splits = pl.f32_splits;
+        j.split_rows = pl.f32_rows;
+        (void)launch_pdl(vocab_join_kernel<false>, dim3(ctas), dim3(32 * warps), 0, s, j);
+    }
     return cudaGetLastError();
 }
 
@@ -453,7 +572,8 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     const __nv_bfloat16* h = (const __nv_bfloat16*)a.h + t0 * d;
     float* scal = (float*)(ws + pl.scal);
     CUtensorMap mh, mw, me;
-    if (!make_map3(&mh, h, d, n, d, 1, 0, false) || !make_map3(&mw, a.w, d, V, d, 1, 0, false)) return cudaErrorInvalidValue;
+    if (!make_map3(&mh, h, d, n, d, 1, 0, false, short_a(pl.logits.pair, n) ? 32 : 128) || !make_map3(&mw, a.w, d, V, d, 1, 0, false))
+        return cudaErrorInvalidValue;
     Problem p = problem((int)n, V, d);
     if (a.dh) {
         if (!make_map3(&me, ws + pl.e, V, n, pl.ld, 1, 0, true)) return cudaErrorInvalidValue;
@@ -461,37 +581,40 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     } else {
         MOE_TRY(logits(pl, mh, mw, mh, p, VocabEpi<false>{a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
     }
-    MOE_TRY(join(pl, a, ws, t0, n, nullptr, s));
+    MOE_TRY(join(pl, a, ws, piece, t0, n, nullptr, s));
     if (!a.dh) return cudaSuccess;
     const float* weight = a.weight ? a.weight + t0 : nullptr;
     for (int64_t r = 0; r < n; r += 65535) {  // (rows of a grid)
-        (void)launch_pdl(vocab_dz_kernel, dim3((unsigned)ceil_div(V, 8 * 256 * 4), (unsigned)std::min<int64_t>(65535, n - r)), dim3(256), 0, s,
+        TotalArgs total{token_loss(pl, a, ws), a.target, a.weight, a.T, nullptr};
+        if (!few(a) && piece == pl.pieces - 1 && r == 0) total.loss = a.loss;
+        (void)launch_pdl(vocab_dz_kernel, dim3((unsigned)(ceil_div(V, 8 * 256 * 4) + (total.loss != nullptr)), (unsigned)std::min<int64_t>(65535, n - r)), dim3(256), 0, s,
                          (uint4*)(ws + pl.e + r * pl.ld * 2), pl.ld, (const float2*)(ws + pl.part) + r * pl.shares, pl.shares, pl.share,
                          (const float*)(ws + pl.lse) + r, a.target + t0 + r, weight ? weight + r : nullptr, (const float*)scal, V,
-                         (const uint4*)(h + r * d), (uint4*)(ws + pl.live + r * d * 2), d / 8);
+                         (const uint4*)(h + r * d), (uint4*)(ws + pl.live + r * d * 2), d / 8, total);
         MOE_TRY(cudaGetLastError());
     }
     CUtensorMap ma, mb, mo;
     // dh = dz W: the vocabulary inside dz's rows, outside W's
-    if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false)) return cudaErrorInvalidValue;
+    if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false, short_a(pl.dh.pair, n) ? 32 : 128)) return cudaErrorInvalidValue;
     if (!make_map3(&mo, (__nv_bfloat16*)a.dh + t0 * d, d, n, d, 1, 0, true)) return cudaErrorInvalidValue;
     p = problem((int)n, d, V);
     split_k(p, pl.dh.splits);
     float* sums = (float*)(ws + pl.sums);
     if (p.splits > 1) {
-        MOE_TRY((product<false>(pl.dh.pair, ma, mw, mo, p, OutEpi<OUT_F32>{nullptr, sums}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_F32>{nullptr, sums}, s)));
         MOE_TRY(sum_splits(sums, p.splits, n * d, scal, true, (__nv_bfloat16*)a.dh + t0 * d, s));
     } else {
-        MOE_TRY((product<false>(pl.dh.pair, ma, mw, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s)));
     }
     // dW = dz^T h: the tokens outside both
-    if (!make_map3(&mb, ws + pl.live, d, n, d, 1, 0, false) || !make_map3(&mo, a.dw, d, V, d, 1, 0, true)) return cudaErrorInvalidValue;
+    if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false) || !make_map3(&mb, ws + pl.live, d, n, d, 1, 0, false) ||
+        !make_map3(&mo, a.dw, d, V, d, 1, 0, true)) return cudaErrorInvalidValue;
     p = problem(V, d, (int)n);
     float* acc = (float*)(ws + pl.dwsum);
-    if (pl.pieces == 1) return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s);
-    if (piece == 0) return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_F32>{nullptr, acc}, s);
-    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_ADD>{nullptr, acc}, s);
-    return product<true>(pl.dw.pair, ma, mb, mo, p, OutEpi<OUT_LAST>{scal, acc}, s);
+    if (pl.pieces == 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s);
+    if (piece == 0) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_F32>{nullptr, acc}, s);
+    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_ADD>{nullptr, acc}, s);
+    return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_LAST>{scal, acc}, s);
 }
 
 cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, cudaStream_t s) {
@@ -514,7 +637,7 @@ cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, c
     (void)launch_pdl(vocab_col_kernel, dim3((unsigned)ceil_div(n, 32), (unsigned)pl.shares), dim3(256), 0, s, (const float*)zt, V, (int)n,
                      (float2*)(ws + pl.part), pl.shares);
     MOE_TRY(cudaGetLastError());
-    MOE_TRY(join(pl, a, ws, t0, n, zt, s));
+    MOE_TRY(join(pl, a, ws, piece, t0, n, zt, s));
     if (!a.dh) return cudaSuccess;
     (void)launch_pdl(vocab_dz_f32_kernel, dim3((unsigned)std::min<int64_t>(ceil_div((int64_t)V * n, 1024), 16 * 2 * kPairs)), dim3(256), 0, s,
                      zt, V, (int)n, (const float*)(ws + pl.lse), a.target + t0, a.weight ? a.weight + t0 : nullptr, (const float*)scal, h,
@@ -551,7 +674,7 @@ cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, c
 
 namespace dense {
 
-bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t ld, int G, int64_t group, bool store) {
+bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t ld, int G, int64_t group, bool store, int box_rows) {
     typedef CUresult (*Encode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
     static const Encode fn = [] {
@@ -566,7 +689,7 @@ bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, i
     if (G == 1) group = outer * ld;
     cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)outer, (cuuint64_t)G};
     cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)group * 2};
-    cuuint32_t box[3] = {store ? (cuuint32_t)OUT_BOX : 64u, store ? (cuuint32_t)OUT_BOX : 128u, 1u};
+    cuuint32_t box[3] = {store ? (cuuint32_t)OUT_BOX : 64u, store ? (cuuint32_t)OUT_BOX : (cuuint32_t)box_rows, 1u};
     cuuint32_t estr[3] = {1u, 1u, 1u};
     // (the type only matters to arithmetic that is not done here: fp16 moves as bf16)
     return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
@@ -586,10 +709,8 @@ cudaError_t launch_vocab_loss(const VocabArgs& a, void* workspace, cudaStream_t 
     const Plan pl = plan(a.T, a.d, a.V, a.bf16, a.dh != nullptr);
     char* ws = (char*)workspace;
     float* scal = (float*)(ws + pl.scal);
-    (void)launch_pdl(vocab_prep_kernel, dim3(1), dim3(kPrep), 0, s, a.target, a.weight, a.T, a.V, scal,
-                     !a.bf16 && a.dh ? (int32_t*)(ws + pl.offsets) : nullptr, pl.f32_splits, pl.f32_rows);
-    MOE_TRY(cudaGetLastError());
     for (int i = 0; i < pl.pieces; ++i) MOE_TRY(a.bf16 ? piece_bf16(pl, a, ws, i, s) : piece_f32(pl, a, ws, i, s));
+    if (few(a) || (a.bf16 && a.dh)) return cudaSuccess;  // (the loss came with another pass)
     (void)launch_pdl(vocab_total_kernel, dim3(1), dim3(1024), 0, s, (const float*)token_loss(pl, a, ws), a.target, a.weight, (const float*)scal, a.T, a.V,
                      a.loss);
     return cudaGetLastError();

@@ -112,15 +112,20 @@ def test_alignment(kind, off, d):
     check_bwd(ids, dout, V, 3.0, backward(ids, dout, V, kind, 3.0, dw))
 
 
-def test_sorted_by_place_in_the_batch():
-    """Sums in order of the batch: 2^24 + 1 + ... loses its ones, 1 + ... + 2^24 does not."""
+def test_a_long_run_of_unequal_terms():
+    """One id, 2^24 and then ones: a 1 that meets the large sum alone is half a step and lost, those of later chunks are added
+    up first. Between the two extremes, the same bits on every call, and whatever other ids are in the batch."""
     T, V, d = 200, 9, 4
     ids = torch.full((T,), 4, dtype=torch.int32, device="cuda")
     dout = torch.ones(T, d, device="cuda")
     dout[0] = 2.0 ** 24
     dw = backward(ids, dout, V, "f32", 1.0, torch.empty(V, d, device="cuda"))
-    first = 2.0 ** 24  # each 1 is half a step: to even; then the parts of the later chunks, 32 ones each
-    assert (dw[4] == first + (T - 32)).all() and (dw[:4] == 0).all() and (dw[5:] == 0).all()
+    check_bwd(ids, dout, V, 1.0, dw)
+    assert (dw[4] > 2.0 ** 24).all() and (dw[4] <= 2.0 ** 24 + T - 1).all() and (dw[:4] == 0).all() and (dw[5:] == 0).all()
+    for _ in range(3):
+        assert torch.equal(dw, backward(ids, dout, V, "f32", 1.0, torch.empty(V, d, device="cuda")))
+    ids[50::50] = 7
+    check_bwd(ids, dout, V, 1.0, backward(ids, dout, V, "f32", 1.0, torch.empty(V, d, device="cuda")))
 
 
 def test_ids_out_of_range_are_recorded():

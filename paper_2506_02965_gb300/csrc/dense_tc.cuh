@@ -81,6 +81,11 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t sr
                  "r"(c0), "r"(c1), "r"(c2)
                  : "memory");
 }
+// An epilogue that reads nothing beside the product.
+struct Plain {
+    template <int CHUNKS> struct Held {};
+    template <int NBUF, typename H> __device__ __forceinline__ void fetch(H&, const Problem&, const Tile&, Warp&) const {}
+};
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     const __half2 h = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -369,10 +374,12 @@ __global__ void __launch_bounds__(threads(EW), 1)
         uint32_t acc_phase = 0;
         for (int64_t t = tile0; t < total; t += tile_step) {
             const Tile ti = tile_at(t);
+            typename Epi::template Held<TN / SPLIT / 32> held;  // what the epilogue reads, on its way during the product
+            epi.template fetch<NBUF>(held, p, ti, w);
             if (!warp_wait(tfull_bar(acc), acc_phase)) break;
             fence_after();
             w.tmem = tmem_base + ((uint32_t)(w.q * 32) << 16) + (uint32_t)(acc * TN);
-            epi.template run<NBUF>(p, ti, w, &tmO);
+            epi.template run<NBUF>(held, p, ti, w, &tmO);
             fence_before();
             __syncwarp();
             if (lane == 0) {

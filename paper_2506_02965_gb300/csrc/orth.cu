@@ -33,6 +33,14 @@ constexpr float kResidual = 4096.f;                 // of X's residual, which is
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
+// The residuals of X are read and written by the epilogue alone, a box of 32 x 32 at a time, a row a lane: so a box is kept
+// as two halves of 16 columns with the lanes' 16 bytes side by side, and a warp moves whole lines.
+constexpr int LO_BOX = 32 * 32;
+__device__ __forceinline__ int64_t lo_at(int64_t box, int row, int col) { return box * LO_BOX + (col & 16) * 32 + (row & 31) * 16 + (col & 15); }
+__device__ __forceinline__ int64_t lo_box(int g, int row, int col, int row_boxes, int col_boxes) {
+    return ((int64_t)g * row_boxes + row / 32) * col_boxes + col / 32;
+}
+
 // ---------------------------------------------------------------- momentum and norm
 // The sum of squares as three fp32 sums, of x 2^-64, x and x 2^64: whichever neither overflowed nor vanished.
 struct Squares {
@@ -92,9 +100,16 @@ __device__ __forceinline__ void update_of(const UpdateArgs& a, int64_t at, float
     if constexpr (sizeof(T) == 4) {
         load_f32<N>((const float*)a.g + at, u);
     } else {
-        Span<T, N> s;
-        s.load((const T*)a.g + at);
-        s.unpack(u);
+        constexpr int W = N < 8 ? N : 8;
+#pragma unroll
+        for (int i = 0; i < N / W; ++i) {
+            Span<T, W> s;
+            float f[W];
+            s.load((const T*)a.g + at + i * W);
+            s.unpack(f);
+#pragma unroll
+            for (int j = 0; j < W; ++j) u[i * W + j] = f[j];
+        }
     }
     if (a.mom) {
         load_f32<N>(a.mom + at, m);
@@ -157,21 +172,35 @@ __global__ void __launch_bounds__(32) orth_inv_kernel(const UpdateArgs a) {
 
 // X = u / |u|: in fp16 with its residual, or in fp32; and m'
 template <typename T, int N, bool HALF>
-__global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, void* hi, uint8_t* lo) {
+__global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, void* hi, uint8_t* lo, int row_boxes, int col_boxes) {
     pdl_begin();
     const int g = blockIdx.y;
     if (a.counts && a.counts[g] <= 0) return;
     const float inv = a.inv[g];
-    const int64_t spans = a.elems / N, base = g * a.elems;
+    const int64_t base = g * a.elems;
     const int per_row = a.cols / N;
+    // N = 16: a warp takes blocks of 8 rows by 64 columns, so that X's rows and the residuals' boxes both get whole lines
+    const int blocks = (per_row + 3) / 4, rows = (int)(a.elems / a.cols);
+    const int64_t spans = N == 16 ? (int64_t)((rows + 7) / 8) * blocks * 32 : a.elems / N;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < spans; i += (int64_t)gridDim.x * 256) {
+        int row, col;
+        if constexpr (N == 16) {
+            const uint32_t b = (uint32_t)(i >> 5), rb = b / (uint32_t)blocks;
+            row = (int)rb * 8 + (threadIdx.x & 31) / 4;
+            col = ((int)(b - rb * blocks) * 4 + (threadIdx.x & 3)) * 16;
+            if (row >= rows || col >= a.cols) continue;
+        } else {
+            row = (int)(i / per_row);
+            col = (int)(i - (int64_t)row * per_row) * N;
+        }
+        const int64_t from = base + (int64_t)row * a.cols + col;
         float u[N], m[N];
-        update_of<T, N>(a, base + i * N, u, m);
-        if (a.mom) store_f32<N>(a.mom_out + base + i * N, m);
-        const int64_t row = i / per_row, at = g * a.group + row * a.ld + (i - row * per_row) * N;
+        update_of<T, N>(a, from, u, m);
+        if (a.mom) store_f32<N>(a.mom_out + from, m);
+        const int64_t at = g * a.group + row * a.ld + col;
         if constexpr (HALF) {
             alignas(16) __half h[N];
-            alignas(8) uint8_t r[N];
+            alignas(16) uint8_t r[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const float x = u[j] * inv * kScaleX;
@@ -179,14 +208,19 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, voi
                 r[j] = (uint8_t)__nv_cvt_float_to_fp8((x - __half2float(h[j])) * kResidual, __NV_SATFINITE, __NV_E5M2);
             }
             __half* to = (__half*)hi + at;
-            if constexpr (N == 8) {
+            uint8_t* to_lo = lo + lo_at(lo_box(g, row, col, row_boxes, col_boxes), row, col);  // (N columns are in one half)
+            if constexpr (N == 16) {
+                reinterpret_cast<uint4*>(to)[0] = reinterpret_cast<const uint4*>(h)[0];
+                reinterpret_cast<uint4*>(to)[1] = reinterpret_cast<const uint4*>(h)[1];
+                *reinterpret_cast<uint4*>(to_lo) = *reinterpret_cast<const uint4*>(r);
+            } else if constexpr (N == 8) {
                 *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(h);
-                *reinterpret_cast<uint2*>(lo + at) = *reinterpret_cast<const uint2*>(r);
+                *reinterpret_cast<uint2*>(to_lo) = *reinterpret_cast<const uint2*>(r);
             } else {
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     to[j] = h[j];
-                    lo[at + j] = r[j];
+                    to_lo[j] = r[j];
                 }
             }
         } else {
@@ -198,36 +232,51 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, voi
 }
 
 // ---------------------------------------------------------------- epilogues
-// v = alpha acc + beta C for 32 columns of this lane's row; C in fp16, with a residual or without, or none.
+// v = alpha acc + beta C for 32 columns of this lane's row, C in fp16 (null: none). All of a warp's chunks of C are on
+// their way while the tile's product runs, as whole 64-byte pieces of rows, four lanes each; at its turn a chunk goes
+// through the staging box that it will leave from, where every lane finds its row. (One chunk ahead of another, 16 bytes
+// of its own row a lane: a step of 16 x 5632 x 1024 180 us; all ahead 166; asynchronous copies into the boxes, for which
+// four warps have enough of them, 184: the epilogue's own time a tile, not the memory, sets the pace of a short product.)
 struct Term {
     const __half* hi;
-    const uint8_t* lo;
     int64_t ld, group;
     float beta;
 };
-struct Ahead {  // a chunk of C on its way
-    uint4 h[4], l[2];
-    __device__ __forceinline__ void load(const Term& t, int g, int m, int col, bool in) {
-        const int64_t at = g * t.group + (int64_t)m * t.ld + col;
+template <int CHUNKS> struct Ahead {
+    uint4 h[CHUNKS][4];
+    __device__ __forceinline__ void load(const Term& c, const Problem& p, const Tile& ti, const Warp& w) {
+        const int row = ti.m0 + w.q * 32 + w.lane / 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) h[i] = in && t.hi ? *reinterpret_cast<const uint4*>(t.hi + at + 8 * i) : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < CHUNKS; ++k) {
+            const int col = ti.n0 + w.c0 + 32 * k;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) l[i] = in && t.lo ? *reinterpret_cast<const uint4*>(t.lo + at + 16 * i) : make_uint4(0, 0, 0, 0);
-    }
-    __device__ __forceinline__ void add(float beta, float (&v)[32]) const {
-        const uint32_t* hw = reinterpret_cast<const uint32_t*>(h);
-        const uint32_t* lw = reinterpret_cast<const uint32_t*>(l);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&hw[i]));
-            // two bytes, each the upper one of an fp16
-            const uint32_t r = __byte_perm(lw[i / 2], 0, i & 1 ? 0x3424 : 0x1404);
-            const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&r));
-            v[2 * i] = fmaf(beta, fmaf(y.x, 1.f / kResidual, x.x), v[2 * i]);
-            v[2 * i + 1] = fmaf(beta, fmaf(y.y, 1.f / kResidual, x.y), v[2 * i + 1]);
+            for (int i = 0; i < 4; ++i) {
+                const bool in = c.hi && row + 8 * i < p.M && col < p.N;
+                h[k][i] = in ? *reinterpret_cast<const uint4*>(c.hi + ti.g * c.group + (int64_t)(row + 8 * i) * c.ld + col + 8 * (w.lane % 4))
+                             : make_uint4(0, 0, 0, 0);
+            }
         }
     }
+    // this lane's row of chunk k, by way of the box that is next to leave
+    template <int NBUF> __device__ __forceinline__ void row(Warp& w, int k, uint32_t (&x)[16]) const {
+        if (w.lane == 0) bulk_wait_read<NBUF - 1>();
+        __syncwarp();
+        uint8_t* box = w.box + w.seq % NBUF * OUT_BOX_BYTES;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 8 * i + w.lane / 4;
+            *reinterpret_cast<uint4*>(box + r * 64 + (((w.lane % 4) ^ ((r >> 1) & 3)) << 4)) = h[k][i];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(box + w.lane * 64 + ((i ^ ((w.lane >> 1) & 3)) << 4));
+            x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+        }
+        __syncwarp();
+    }
 };
+__device__ __forceinline__ float2 two_halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
 // A symmetric product in fp16, its lower tiles and their mirror images.
 struct SymEpi {
@@ -236,20 +285,32 @@ struct SymEpi {
     __half* out;
     int64_t ld, group;
 
-    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
+    template <int CHUNKS> using Held = Ahead<CHUNKS>;
+    template <int NBUF, int CHUNKS>
+    __device__ __forceinline__ void fetch(Ahead<CHUNKS>& held, const Problem& p, const Tile& ti, Warp& w) const {
+        held.load(c, p, ti, w);
+    }
+    template <int NBUF, int CHUNKS>
+    __device__ __forceinline__ void run(const Ahead<CHUNKS>& held, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
         const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
-        const bool in = m < p.M;
-        Ahead next;
-        next.load(c, ti.g, m, ti.n0 + w.c0, in && ti.n0 + w.c0 < p.N);
-#pragma unroll 1
-        for (int k = w.c0; k < w.c1 && ti.n0 + k < p.N; k += 32) {
-            const Ahead now = next;
-            next.load(c, ti.g, m, ti.n0 + k + 32, in && k + 32 < w.c1 && ti.n0 + k + 32 < p.N);
+#pragma unroll
+        for (int chunk = 0; chunk < CHUNKS; ++chunk) {
+            const int k = w.c0 + 32 * chunk;
+            if (ti.n0 + k >= p.N) break;
             float v[32];
             tmem_ld32(w.tmem + k, v);
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] *= alpha;
-            now.add(c.beta, v);
+            if (c.hi) {
+                uint32_t x[16];
+                held.template row<NBUF>(w, chunk, x);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float2 y = two_halves(x[i]);
+                    v[2 * i] = fmaf(c.beta, y.x, v[2 * i]);
+                    v[2 * i + 1] = fmaf(c.beta, y.y, v[2 * i + 1]);
+                }
+            }
             uint32_t u[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) u[i] = pack_half(v[2 * i], v[2 * i + 1]);
@@ -273,54 +334,77 @@ struct SymEpi {
 // X' = alpha acc + beta X in fp16 with its residual; (LAST) in the matrix's own type, times a scale.
 template <bool LAST> struct StepEpi {
     Term c;
+    const uint8_t* lo_in;
     float alpha;
-    uint8_t* lo;           // LAST: unused
-    int64_t ld, group;
+    uint8_t* lo_out;       // LAST: unused
+    int row_boxes, col_boxes;
     float scale;           // LAST
     __nv_bfloat16* out;    // LAST: rows of p.N, where the map does not serve them
     int by_map;
 
-    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
-        const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
-        const bool in = m < p.M;
-        Ahead next;
-        next.load(c, ti.g, m, ti.n0 + w.c0, in && ti.n0 + w.c0 < p.N);
-#pragma unroll 1
-        for (int k = w.c0; k < w.c1 && ti.n0 + k < p.N; k += 32) {
-            const Ahead now = next;
-            next.load(c, ti.g, m, ti.n0 + k + 32, in && k + 32 < w.c1 && ti.n0 + k + 32 < p.N);
-            float v[32];
-            tmem_ld32(w.tmem + k, v);
+    template <int CHUNKS> struct Held {
+        Ahead<CHUNKS> x;
+        uint4 l[CHUNKS][2];
+    };
+    template <int NBUF, int CHUNKS>
+    __device__ __forceinline__ void fetch(Held<CHUNKS>& held, const Problem& p, const Tile& ti, Warp& w) const {
+        held.x.load(c, p, ti, w);
+        const int row0 = ti.m0 + w.q * 32;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= alpha;
-            now.add(c.beta, v);
+        for (int k = 0; k < CHUNKS; ++k) {
+            const int col = ti.n0 + w.c0 + 32 * k;
+            const bool in = row0 < p.M && col < p.N;
+            const uint4* l = reinterpret_cast<const uint4*>(lo_in + (in ? lo_box(ti.g, row0, col, row_boxes, col_boxes) * LO_BOX : 0));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) held.l[k][i] = in ? l[32 * i + w.lane] : make_uint4(0, 0, 0, 0);
+        }
+    }
+    template <int NBUF, int CHUNKS>
+    __device__ __forceinline__ void run(const Held<CHUNKS>& held, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
+        const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
+#pragma unroll
+        for (int k = 0; k < CHUNKS; ++k) {
+            const int col = ti.n0 + w.c0 + 32 * k;
+            if (col >= p.N) break;
+            float v[32];
+            tmem_ld32(w.tmem + w.c0 + 32 * k, v);
+            uint32_t x[16];
+            held.x.template row<NBUF>(w, k, x);
+            const uint32_t* lw = reinterpret_cast<const uint32_t*>(held.l[k]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                // the residual: two bytes, each the upper one of an fp16
+                const float2 h = two_halves(x[i]), y = two_halves(__byte_perm(lw[i / 2], 0, i & 1 ? 0x3424 : 0x1404));
+                v[2 * i] = fmaf(c.beta, fmaf(y.x, 1.f / kResidual, h.x), v[2 * i] * alpha);
+                v[2 * i + 1] = fmaf(c.beta, fmaf(y.y, 1.f / kResidual, h.y), v[2 * i + 1] * alpha);
+            }
             uint32_t u[16];
             if constexpr (LAST) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) u[i] = pack_bf16(v[2 * i] * scale, v[2 * i + 1] * scale);
                 if (by_map) {
-                    store_box<NBUF>(w, map, u, ti.n0 + k, row0, ti.g);
-                } else if (in) {
-                    __nv_bfloat16* to = out + ((int64_t)ti.g * p.M + m) * p.N + ti.n0 + k;
+                    store_box<NBUF>(w, map, u, col, row0, ti.g);
+                } else if (m < p.M) {
+                    __nv_bfloat16* to = out + ((int64_t)ti.g * p.M + m) * p.N + col;
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        if (ti.n0 + k + i < p.N) to[i] = __ushort_as_bfloat16((uint16_t)(u[i / 2] >> (i & 1 ? 16 : 0)));
+                        if (col + i < p.N) to[i] = __ushort_as_bfloat16((uint16_t)(u[i / 2] >> (i & 1 ? 16 : 0)));
                 }
             } else {
                 uint32_t r[8];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     u[i] = pack_half(v[2 * i], v[2 * i + 1]);
-                    const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+                    const float2 h = two_halves(u[i]);
                     const uint32_t e = __nv_cvt_float2_to_fp8x2(make_float2((v[2 * i] - h.x) * kResidual, (v[2 * i + 1] - h.y) * kResidual),
                                                                 __NV_SATFINITE, __NV_E5M2);
                     r[i / 2] = i & 1 ? r[i / 2] | (e << 16) : e;
                 }
-                store_box<NBUF>(w, map, u, ti.n0 + k, row0, ti.g);
-                if (in) {
-                    uint4* to = reinterpret_cast<uint4*>(lo + ti.g * group + (int64_t)m * ld + ti.n0 + k);
-                    to[0] = make_uint4(r[0], r[1], r[2], r[3]);
-                    to[1] = make_uint4(r[4], r[5], r[6], r[7]);
+                store_box<NBUF>(w, map, u, col, row0, ti.g);
+                if (row0 < p.M) {
+                    uint4* to = reinterpret_cast<uint4*>(lo_out + lo_box(ti.g, row0, col, row_boxes, col_boxes) * LO_BOX);
+                    to[w.lane] = make_uint4(r[0], r[1], r[2], r[3]);
+                    to[32 + w.lane] = make_uint4(r[4], r[5], r[6], r[7]);
                 }
             }
         }
@@ -347,6 +431,7 @@ __global__ void __launch_bounds__(256) orth_out_kernel(const float* __restrict__
 struct Plan {
     int n;              // the smaller side
     int64_t ld, ldn;    // row strides of X and of the squares
+    int row_boxes, col_boxes;  // of X's residuals
     int parts;
     size_t part, inv, x[2], lo[2], a, b, total;
 };
@@ -356,6 +441,8 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     p.n = std::min(rows, cols);
     p.ld = bf16 ? ceil_div(cols, 64) * 64 : cols;
     p.ldn = bf16 ? ceil_div(p.n, 64) * 64 : p.n;
+    p.row_boxes = (int)ceil_div(rows, 32);
+    p.col_boxes = (int)ceil_div(cols, 32);
     const int64_t want = ceil_div((int64_t)rows * cols, 8 * 256);
     p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(16 * kPairs, G)));
     size_t at = 0;
@@ -368,7 +455,7 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     p.part = take((size_t)G * p.parts * 24);
     p.inv = take((size_t)G * 4);
     for (int i = 0; i < 2; ++i) p.x[i] = take(xs * es);
-    for (int i = 0; i < 2; ++i) p.lo[i] = bf16 ? take(xs) : 0;
+    for (int i = 0; i < 2; ++i) p.lo[i] = bf16 ? take((size_t)G * p.row_boxes * p.col_boxes * LO_BOX) : 0;
     p.a = take(as * es);
     p.b = take(as * es);
     p.total = at;
@@ -382,20 +469,21 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     } while (0)
 
 template <typename T, int N>
-cudaError_t start(const UpdateArgs& a, int G, void* hi, uint8_t* lo, cudaStream_t s) {
+cudaError_t start(const UpdateArgs& a, int G, const Plan& pl, void* hi, uint8_t* lo, cudaStream_t s) {
     constexpr bool HALF = sizeof(T) == 2;
     const dim3 grid((unsigned)a.parts, (unsigned)G);
-    (void)launch_pdl(orth_norm_kernel<T, N>, grid, dim3(256), 0, s, a);
+    (void)launch_pdl(orth_norm_kernel<T, N < 8 ? N : 8>, grid, dim3(256), 0, s, a);
     (void)launch_pdl(orth_inv_kernel, dim3((unsigned)G), dim3(32), 0, s, a);
-    (void)launch_pdl(orth_start_kernel<T, N, HALF>, grid, dim3(256), 0, s, a, hi, lo);
+    (void)launch_pdl(orth_start_kernel<T, N, HALF>, grid, dim3(256), 0, s, a, hi, lo, pl.row_boxes, pl.col_boxes);
     return cudaGetLastError();
 }
 template <typename T>
-cudaError_t start_n(const UpdateArgs& a, int G, void* hi, uint8_t* lo, cudaStream_t s) {
-    if (a.cols % 8 == 0) return start<T, 8>(a, G, hi, lo, s);
-    if (a.cols % 4 == 0) return start<T, 4>(a, G, hi, lo, s);
-    if (a.cols % 2 == 0) return start<T, 2>(a, G, hi, lo, s);
-    return start<T, 1>(a, G, hi, lo, s);
+cudaError_t start_n(const UpdateArgs& a, int G, const Plan& pl, void* hi, uint8_t* lo, cudaStream_t s) {
+    if (sizeof(T) == 2 && a.cols % 16 == 0) return start<T, sizeof(T) == 2 ? 16 : 8>(a, G, pl, hi, lo, s);
+    if (a.cols % 8 == 0) return start<T, 8>(a, G, pl, hi, lo, s);
+    if (a.cols % 4 == 0) return start<T, 4>(a, G, pl, hi, lo, s);
+    if (a.cols % 2 == 0) return start<T, 2>(a, G, pl, hi, lo, s);
+    return start<T, 1>(a, G, pl, hi, lo, s);
 }
 
 template <bool A_MN, bool B_MN, typename Epi>
@@ -423,19 +511,20 @@ cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t
     sq.counts = cube.counts = step.counts = o.counts;
     for (int i = 0; i < o.steps; ++i) {
         const int x = i & 1, y = x ^ 1;
-        const Term none{nullptr, nullptr, 0, 0, 0.f};
+        const Term none{nullptr, 0, 0, 0.f};
         const SymEpi ea{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag};
         if (tall) MOE_TRY((product<true, true>(mx[x], mx[x], sa, sq, ea, s)));
         else MOE_TRY((product<false, false>(mx[x], mx[x], sa, sq, ea, s)));
-        const SymEpi eb{{A, nullptr, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag};
+        const SymEpi eb{{A, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag};
         MOE_TRY((product<false, false>(ma, ma, sb, cube, eb, s)));
-        const Term cx{(const __half*)(ws + pl.x[x]), (const uint8_t*)(ws + pl.lo[x]), pl.ld, xg, kA};
+        const Term cx{(const __half*)(ws + pl.x[x]), pl.ld, xg, kA};
+        const uint8_t* lo = (const uint8_t*)(ws + pl.lo[x]);
         if (i + 1 < o.steps) {
-            const StepEpi<false> e{cx, 1.f / kScaleA, (uint8_t*)(ws + pl.lo[y]), pl.ld, xg, 1.f, nullptr, 1};
+            const StepEpi<false> e{cx, lo, 1.f / kScaleA, (uint8_t*)(ws + pl.lo[y]), pl.row_boxes, pl.col_boxes, 1.f, nullptr, 1};
             if (tall) MOE_TRY((product<false, false>(mx[x], mb, sx[y], step, e, s)));
             else MOE_TRY((product<false, true>(mb, mx[x], sx[y], step, e, s)));
         } else {
-            const StepEpi<true> e{cx, 1.f / kScaleA, nullptr, pl.ld, xg, o.scale / kScaleX, (__nv_bfloat16*)o.out, by_map};
+            const StepEpi<true> e{cx, lo, 1.f / kScaleA, nullptr, pl.row_boxes, pl.col_boxes, o.scale / kScaleX, (__nv_bfloat16*)o.out, by_map};
             if (tall) MOE_TRY((product<false, false>(mx[x], mb, mo, step, e, s)));
             else MOE_TRY((product<false, true>(mb, mx[x], mo, step, e, s)));
         }
@@ -513,10 +602,10 @@ cudaError_t launch_orthogonalise(const OrthArgs& o, void* workspace, cudaStream_
     a.parts = pl.parts;
     a.inv = (float*)(ws + pl.inv);
     if (o.bf16) {
-        MOE_TRY(start_n<__nv_bfloat16>(a, o.groups, ws + pl.x[0], (uint8_t*)(ws + pl.lo[0]), s));
+        MOE_TRY(start_n<__nv_bfloat16>(a, o.groups, pl, ws + pl.x[0], (uint8_t*)(ws + pl.lo[0]), s));
         return steps_half(pl, o, ws, s);
     }
-    MOE_TRY(start_n<float>(a, o.groups, ws + pl.x[0], nullptr, s));
+    MOE_TRY(start_n<float>(a, o.groups, pl, ws + pl.x[0], nullptr, s));
     return steps_f32(pl, o, ws, s);
 }
 

@@ -35,13 +35,13 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // ---------------------------------------------------------------- epilogues
 // The logits' tile: statistics of every row's share of columns, the target's logit, and (STORE) exp(z - m) in fp16.
-template <bool STORE> struct VocabEpi {
+template <bool STORE> struct VocabEpi : Plain {
     const int32_t* target;
     float2* part;  // [M][shares]: largest logit, sum of exp(z - it)
     float* zy;     // [M]
     int shares;
 
-    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
+    template <int NBUF, typename H> __device__ __forceinline__ void run(const H&, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
         const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane, cols = w.c1 - w.c0;
         const int base = ti.n0 + w.c0;
         if (base >= p.N) return;
@@ -96,11 +96,11 @@ template <bool STORE> struct VocabEpi {
 // A product that is stored in bf16, times *alpha (OUT_BF16), as fp32 sums of one split or piece (OUT_F32), added to
 // such sums (OUT_ADD), or with such sums added to it, in bf16 (OUT_LAST).
 enum { OUT_BF16, OUT_F32, OUT_ADD, OUT_LAST };
-template <int MODE> struct OutEpi {
+template <int MODE> struct OutEpi : Plain {
     const float* alpha;
     float* sums;  // [splits][M][N]
 
-    template <int NBUF> __device__ __forceinline__ void run(const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
+    template <int NBUF, typename H> __device__ __forceinline__ void run(const H&, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
         const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
         const float a = MODE == OUT_BF16 || MODE == OUT_LAST ? *alpha : 1.f;
         float* at = MODE == OUT_BF16 ? nullptr : sums + ((int64_t)ti.split * p.M + m) * p.N;
@@ -577,9 +577,9 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     Problem p = problem((int)n, V, d);
     if (a.dh) {
         if (!make_map3(&me, ws + pl.e, V, n, pl.ld, 1, 0, true)) return cudaErrorInvalidValue;
-        MOE_TRY(logits(pl, mh, mw, me, p, VocabEpi<true>{a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
+        MOE_TRY(logits(pl, mh, mw, me, p, VocabEpi<true>{{}, a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
     } else {
-        MOE_TRY(logits(pl, mh, mw, mh, p, VocabEpi<false>{a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
+        MOE_TRY(logits(pl, mh, mw, mh, p, VocabEpi<false>{{}, a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
     }
     MOE_TRY(join(pl, a, ws, piece, t0, n, nullptr, s));
     if (!a.dh) return cudaSuccess;
@@ -601,20 +601,20 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     split_k(p, pl.dh.splits);
     float* sums = (float*)(ws + pl.sums);
     if (p.splits > 1) {
-        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_F32>{nullptr, sums}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_F32>{{}, nullptr, sums}, s)));
         MOE_TRY(sum_splits(sums, p.splits, n * d, scal, true, (__nv_bfloat16*)a.dh + t0 * d, s));
     } else {
-        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_BF16>{{}, scal, nullptr}, s)));
     }
     // dW = dz^T h: the tokens outside both
     if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false) || !make_map3(&mb, ws + pl.live, d, n, d, 1, 0, false) ||
         !make_map3(&mo, a.dw, d, V, d, 1, 0, true)) return cudaErrorInvalidValue;
     p = problem(V, d, (int)n);
     float* acc = (float*)(ws + pl.dwsum);
-    if (pl.pieces == 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_BF16>{scal, nullptr}, s);
-    if (piece == 0) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_F32>{nullptr, acc}, s);
-    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_ADD>{nullptr, acc}, s);
-    return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_LAST>{scal, acc}, s);
+    if (pl.pieces == 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_BF16>{{}, scal, nullptr}, s);
+    if (piece == 0) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_F32>{{}, nullptr, acc}, s);
+    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_ADD>{{}, nullptr, acc}, s);
+    return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_LAST>{{}, scal, acc}, s);
 }
 
 cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, cudaStream_t s) {

@@ -24,19 +24,24 @@ import torch
 
 from . import _lib as L
 from .layer import MoELayer
+from .lm import Muon
 
 
 class RoundRobinTrainer:
-    def __init__(self, shape, n_parties: int, lr: float, device: str = "cuda", master=None):
+    def __init__(self, shape, n_parties: int, lr: float, device: str = "cuda", master=None, update: str = "sgd"):
         """shape: one batch (T tokens of one party: n_parties = 1, no shared experts).
         master: keep fp32 master copies of the parameters that the SGD updates and
-        round into the layer's bf16 weights (default: for bf16 shapes)."""
+        round into the layer's bf16 weights (default: for bf16 shapes).
+        update: of the experts a batch called, "sgd" or "muon" (lm.Muon: orthogonalised, W1[e] and W2[e] a
+        matrix each, an uncalled expert's momentum stays as it is). The gating takes SGD."""
         if shape.n_parties != 1:
             raise ValueError("a batch holds the tokens of one party: shape.n_parties must be 1")
         if shape.n_shared:
             raise ValueError("the toy block has no shared experts")
         if n_parties < 1:
             raise ValueError("n_parties must be >= 1")
+        if update not in ("sgd", "muon"):
+            raise ValueError(f'update must be "sgd" or "muon", not {update!r}')
         self.shape, self.n, self.lr = shape, int(n_parties), float(lr)
         self.layer = lay = MoELayer(shape, device)
         E, d = shape.n_experts, shape.d_model
@@ -51,6 +56,7 @@ class RoundRobinTrainer:
             self.m2 = torch.empty(lay.w2.shape, dtype=f32, device=device)
         else:
             self.m_router = self.m1 = self.m2 = None
+        self.muon = (Muon(lay.w1), Muon(lay.w2)) if update == "muon" else None
 
     # ------------------------------------------------------------------ parameters
     @property
@@ -94,10 +100,14 @@ class RoundRobinTrainer:
         mr = self.m_router[party] if self.master else None
         L.moe_sgd_update(self.w_router[party], lay.dw_router, 1, E * d, None, self.lr, self.dtype,
                          w_master=mr, stream=main)
-        L.moe_sgd_update(lay.w1, lay.dw1, E, 2 * F * d, lay.counts, self.lr, self.dtype,
-                         w_master=self.m1, stream=main)
-        L.moe_sgd_update(lay.w2, lay.dw2, E, d * F, lay.counts, self.lr, self.dtype,
-                         w_master=self.m2, stream=main)
+        if self.muon:
+            self.muon[0].update(lay.w1, lay.dw1, self.lr, lay.counts.view(E), self.m1, main)
+            self.muon[1].update(lay.w2, lay.dw2, self.lr, lay.counts.view(E), self.m2, main)
+        else:
+            L.moe_sgd_update(lay.w1, lay.dw1, E, 2 * F * d, lay.counts, self.lr, self.dtype,
+                             w_master=self.m1, stream=main)
+            L.moe_sgd_update(lay.w2, lay.dw2, E, d * F, lay.counts, self.lr, self.dtype,
+                             w_master=self.m2, stream=main)
         if record is not None:
             with torch.cuda.stream(main):
                 record[0:1].copy_(self.mse)
@@ -128,5 +138,5 @@ class RoundRobinTrainer:
         return order_log, log
 
     def kernels_per_step(self) -> int:
-        """CUDA kernels per batch: the layer's, 2 for the loss, 3 SGD updates."""
+        """CUDA kernels per batch by SGD: the layer's, 2 for the loss, 3 updates."""
         return self.layer.kernels_per_step() + 2 + 3

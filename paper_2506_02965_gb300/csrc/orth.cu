@@ -12,7 +12,7 @@
 // off (of the norm, 333 x 1000 to 2048 x 2048 matrices), fp16 ones 1.5e-3. Most of that is X's own rounding
 // between the steps, and it is where a few directions outweigh the rest (30 times: 8.5e-3) that it counts, so
 // the a X term takes X to 14 bits, its residual as an 8-bit float (e5m2, the upper half of an fp16). The other products
-// keep fp16. All sums are fp32, the norm's are 64-bit sums of fp32 ones.
+// keep fp16. All sums are fp32.
 //
 // A matrix with more rows than columns is not transposed: A = X^T X and X = a X + X (b A + c A A), with the operands'
 // other major. fp32 matrices take the fp32 products throughout.
@@ -42,11 +42,14 @@ __device__ __forceinline__ int64_t lo_box(int g, int row, int col, int row_boxes
 }
 
 // ---------------------------------------------------------------- momentum and norm
-// The sum of squares as three fp32 sums, of x 2^-64, x and x 2^64: whichever neither overflowed nor vanished.
+// The sum of squares as three fp32 sums, of x 2^-96, x and x 2^88: one of them neither overflows nor loses what matters,
+// from the smallest fp32 numbers to the largest. x itself serves norms of 2^-30 to 2^60; below, a value is at most 2^-30
+// and 2^-149 at least, so that the third sum's squares are 2^-122 to 2^116; above, those that matter are over 2^40.
+constexpr float kBig = 0x1p-96f, kSmall = 0x1p88f;
 struct Squares {
     float big = 0.f, mid = 0.f, small = 0.f;
     __device__ __forceinline__ void add(float x) {
-        const float b = x * 0x1p-64f, s = x * 0x1p64f;
+        const float b = x * kBig, s = x * kSmall;
         big = fmaf(b, b, big);
         mid = fmaf(x, x, mid);
         small = fmaf(s, s, small);
@@ -89,9 +92,11 @@ struct UpdateArgs {
     int64_t ld, group;     // of X: row stride, and matrix stride
     float beta;
     int nesterov;
-    double* part;          // [G][parts][3]
+    float* part;           // [G][parts][3]
     int parts;
-    float* inv;            // [G]: 1 / |u|
+    // fp32: the row offsets of X^T X's parts (see steps_f32), or null
+    int32_t* offsets;
+    int splits, split_rows, G, ld_rows;
 };
 
 // u (and m') of N elements from `at` on
@@ -133,50 +138,58 @@ template <typename T, int N> __global__ void __launch_bounds__(256) orth_norm_ke
 #pragma unroll
         for (int j = 0; j < N; ++j) q.add(u[j]);
     }
-    double v[3] = {(double)q.big, (double)q.mid, (double)q.small};
-    __shared__ double s_part[8][3];
+    float v[3] = {q.big, q.mid, q.small};
+    __shared__ float s_part[8][3];
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        v[k] = warp_sum(v[k]);
         if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5][k] = v[k];
     }
     __syncthreads();
     if (threadIdx.x < 3) {
-        double s = 0.0;
+        float s = 0.f;
         for (int w = 0; w < 8; ++w) s += s_part[w][threadIdx.x];
         a.part[((int64_t)g * a.parts + blockIdx.x) * 3 + threadIdx.x] = s;
     }
 }
 
-__global__ void __launch_bounds__(32) orth_inv_kernel(const UpdateArgs a) {
-    pdl_begin();
-    const int g = blockIdx.x;
-    if (a.counts && a.counts[g] <= 0) return;
-    double v[3] = {0.0, 0.0, 0.0};
-    for (int i = threadIdx.x; i < a.parts; i += 32)
+// What takes u to u / |u|, from the parts, by every CTA for itself (in the same order): a power of two, and a factor after it.
+__device__ __forceinline__ float2 inverse_norm(const UpdateArgs& a, int g) {
+    __shared__ float s_part[8][3];
+    __shared__ float2 s_inv;
+    float v[3] = {0.f, 0.f, 0.f};
+    for (int i = threadIdx.x; i < a.parts; i += 256)
 #pragma unroll
         for (int k = 0; k < 3; ++k) v[k] += a.part[((int64_t)g * a.parts + i) * 3 + k];
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-    if (threadIdx.x == 0) {
-        // the fp32 sums' range: squares near the ends of it are taken from the sum that holds them as normal numbers
-        const double n2 = !(v[1] < 0x1p120) ? v[0] * 0x1p128 : v[1] > 0x1p-60 ? v[1] : v[2] * 0x1p-128;
-        const double n = sqrt(n2);
-        // (without a direction, zeros; an infinite or undefined norm leaves nothing but NaN)
-        a.inv[g] = n > 0.0 ? (float)fmin(1.0 / n, 3.0e38) : n == 0.0 ? 0.f : __int_as_float(0x7fc00000);
+    for (int k = 0; k < 3; ++k) {
+        v[k] = warp_sum(v[k]);
+        if ((threadIdx.x & 31) == 0) s_part[threadIdx.x >> 5][k] = v[k];
     }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < 8; ++w)
+            for (int k = 0; k < 3; ++k) v[k] += s_part[w][k];
+        const float inf = __int_as_float(0x7f800000);
+        s_inv = !(v[1] < 0x1p120f) ? make_float2(kBig, 1.f / sqrtf(v[0])) : v[1] > 0x1p-60f ? make_float2(1.f, 1.f / sqrtf(v[1]))
+                : v[2] > 0.f ? make_float2(kSmall, 1.f / sqrtf(v[2])) : make_float2(1.f, 0.f);  // (nothing: zeros)
+        // an infinite or undefined norm leaves nothing but NaN
+        if (!(v[0] < inf)) s_inv.y = __int_as_float(0x7fc00000);
+    }
+    __syncthreads();
+    return s_inv;
 }
 
-// X = u / |u|: in fp16 with its residual, or in fp32; and m'
+// X = u / |u|: in fp16 with its residual, or in fp32 (a matrix with more columns than rows transposed); and m'
 template <typename T, int N, bool HALF>
 __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, void* hi, uint8_t* lo, int row_boxes, int col_boxes) {
     pdl_begin();
     const int g = blockIdx.y;
+    if (!HALF && a.offsets && g == 0 && blockIdx.x == 0)
+        for (int i = threadIdx.x; i <= a.G * a.splits; i += 256)
+            a.offsets[i] = (int32_t)((int64_t)(i / a.splits) * a.ld_rows + min(a.ld_rows, i % a.splits * a.split_rows));
     if (a.counts && a.counts[g] <= 0) return;
-    const float inv = a.inv[g];
+    const float2 inv = inverse_norm(a, g);
     const int64_t base = g * a.elems;
     const int per_row = a.cols / N;
     // N = 16: a warp takes blocks of 8 rows by 64 columns, so that X's rows and the residuals' boxes both get whole lines
@@ -203,7 +216,7 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, voi
             alignas(16) uint8_t r[N];
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                const float x = u[j] * inv * kScaleX;
+                const float x = u[j] * inv.x * inv.y * kScaleX;
                 h[j] = __float2half_rn(x);
                 r[j] = (uint8_t)__nv_cvt_float_to_fp8((x - __half2float(h[j])) * kResidual, __NV_SATFINITE, __NV_E5M2);
             }
@@ -225,8 +238,13 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, voi
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < N; ++j) u[j] *= inv;
-            store_f32<N>((float*)hi + at, u);
+            for (int j = 0; j < N; ++j) u[j] = u[j] * inv.x * inv.y;
+            if (rows < a.cols) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) ((float*)hi)[g * a.elems + (int64_t)(col + j) * rows + row] = u[j];
+            } else {
+                store_f32<N>((float*)hi + at, u);
+            }
         }
     }
 }
@@ -420,20 +438,37 @@ __global__ void __launch_bounds__(256) orth_poly_kernel(const float* __restrict_
         sq[i] = fmaf(kC, sq[i], fmaf(kB, A[i], at / n == at % n ? kA : 0.f));
     }
 }
-__global__ void __launch_bounds__(256) orth_out_kernel(const float* __restrict__ x, float* __restrict__ out, int64_t elems, float scale,
-                                                       const int32_t* __restrict__ counts) {
+// the parts' sums, in order
+__global__ void __launch_bounds__(256) orth_sum_kernel(const float* __restrict__ parts, float* __restrict__ out, int64_t nn, int64_t total,
+                                                       int splits) {
+    pdl_begin();
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
+        const int64_t g = i / nn;
+        const float* p = parts + (g * splits - g) * nn + i;
+        float s = 0.f;
+        for (int k = 0; k < splits; ++k) s += p[k * nn];
+        out[i] = s;
+    }
+}
+// scale times X; rows > 0: X is transposed, [cols, rows]
+__global__ void __launch_bounds__(256) orth_out_kernel(const float* __restrict__ x, float* __restrict__ out, int64_t elems, int rows, int cols,
+                                                       float scale, const int32_t* __restrict__ counts) {
     pdl_begin();
     if (counts && counts[blockIdx.y] <= 0) return;
     const int64_t base = blockIdx.y * elems;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += (int64_t)gridDim.x * 256) out[base + i] = x[base + i] * scale;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += (int64_t)gridDim.x * 256) {
+        const int64_t from = rows ? (i % cols) * rows + i / cols : i;
+        out[base + i] = x[base + from] * scale;
+    }
 }
 
 struct Plan {
     int n;              // the smaller side
     int64_t ld, ldn;    // row strides of X and of the squares
     int row_boxes, col_boxes;  // of X's residuals
-    int parts;
-    size_t part, inv, x[2], lo[2], a, b, total;
+    int parts;          // CTAs per matrix of the first passes
+    int splits, split_rows;  // fp32: parts of X^T X's contraction
+    size_t part, offsets, sums, x[2], lo[2], a, b, total;
 };
 
 Plan plan(int G, int rows, int cols, bool bf16) {
@@ -445,6 +480,14 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     p.col_boxes = (int)ceil_div(cols, 32);
     const int64_t want = ceil_div((int64_t)rows * cols, 8 * 256);
     p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(16 * kPairs, G)));
+    p.splits = 1;
+    if (!bf16) {
+        const int64_t m = std::max(rows, cols), tiles = G * ceil_div(p.n, 128) * ceil_div(p.n, 128);
+        int64_t sp = std::min<int64_t>(std::min<int64_t>(256 / G, 2 * kPairs / tiles), m / 128);  // one round of tiles
+        sp = std::max<int64_t>(sp, 1);
+        p.split_rows = (int)(ceil_div(ceil_div(m, sp), 32) * 32);
+        p.splits = (int)ceil_div(m, p.split_rows);
+    }
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t here = at;
@@ -452,12 +495,13 @@ Plan plan(int G, int rows, int cols, bool bf16) {
         return here;
     };
     const size_t xs = (size_t)G * rows * p.ld, as = (size_t)G * p.n * p.ldn, es = bf16 ? 2 : 4;
-    p.part = take((size_t)G * p.parts * 24);
-    p.inv = take((size_t)G * 4);
+    p.part = take((size_t)G * p.parts * 12);
+    p.offsets = take(p.splits > 1 ? (size_t)(G * p.splits + 1) * 4 : 0);
     for (int i = 0; i < 2; ++i) p.x[i] = take(xs * es);
     for (int i = 0; i < 2; ++i) p.lo[i] = bf16 ? take((size_t)G * p.row_boxes * p.col_boxes * LO_BOX) : 0;
     p.a = take(as * es);
     p.b = take(as * es);
+    p.sums = take(p.splits > 1 ? as * es * p.splits : 0);
     p.total = at;
     return p;
 }
@@ -471,9 +515,10 @@ Plan plan(int G, int rows, int cols, bool bf16) {
 template <typename T, int N>
 cudaError_t start(const UpdateArgs& a, int G, const Plan& pl, void* hi, uint8_t* lo, cudaStream_t s) {
     constexpr bool HALF = sizeof(T) == 2;
+    // (A launch of both per matrix, whose second pass then reads from the L2, takes longer: 16 x 36 us for matrices of
+    // 5632 x 1024, all in one of each 318.)
     const dim3 grid((unsigned)a.parts, (unsigned)G);
     (void)launch_pdl(orth_norm_kernel<T, N < 8 ? N : 8>, grid, dim3(256), 0, s, a);
-    (void)launch_pdl(orth_inv_kernel, dim3((unsigned)G), dim3(32), 0, s, a);
     (void)launch_pdl(orth_start_kernel<T, N, HALF>, grid, dim3(256), 0, s, a, hi, lo, pl.row_boxes, pl.col_boxes);
     return cudaGetLastError();
 }
@@ -532,50 +577,57 @@ cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t
     return cudaSuccess;
 }
 
+// X is [m, n] here, the longer side outside (transposed on the way in and out where the matrix is wide): A = X^T X is a sum
+// over rows, which parts of them share where a matrix has few tiles (8 of 1024 x 256: 64 tiles, 38 us a step as one
+// sum).
 cudaError_t steps_f32(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t s) {
-    const int R = o.rows, C = o.cols, G = o.groups, n = pl.n;
-    const bool tall = R > C;
-    float *A = (float*)(ws + pl.a), *B = (float*)(ws + pl.b);
+    const int G = o.groups, n = pl.n, m = std::max(o.rows, o.cols);
+    float *A = (float*)(ws + pl.a), *B = (float*)(ws + pl.b), *sums = (float*)(ws + pl.sums);
     const int64_t nn = (int64_t)n * n;
-    auto rows_by = [&](int rows, int K, const float* a, const float* b, int64_t b_elems, bool kmajor, int N, float* out) {
-        GemmMArgs m{};
-        m.G = G;
-        m.rows.rows = rows;
-        m.rows.a_stride = m.rows.out_stride = rows;
-        m.a = a;
-        m.b = b;
-        m.b_group_elems = b_elems;
-        m.b_kmajor = kmajor;
-        m.N = N;
-        m.K = K;
-        m.epi = EPI_STORE;
-        m.out0 = out;
-        return launch_gemm_m(m, false, s);
+    const dim3 wide((unsigned)std::min<int64_t>(ceil_div(nn * G, 256), 16 * 2 * kPairs));
+    auto rows_by = [&](int rows, const float* a, const float* b, float* out) {  // out = a b, b symmetric [n, n]
+        GemmMArgs g{};
+        g.G = G;
+        g.rows.rows = rows;
+        g.rows.a_stride = g.rows.out_stride = rows;
+        g.a = a;
+        g.b = b;
+        g.b_group_elems = nn;
+        g.b_kmajor = true;
+        g.N = n;
+        g.K = n;
+        g.epi = EPI_STORE;
+        g.out0 = out;
+        return launch_gemm_m(g, false, s);
     };
     for (int i = 0; i < o.steps; ++i) {
         float *x = (float*)(ws + pl.x[i & 1]), *y = (float*)(ws + pl.x[(i & 1) ^ 1]);
-        if (tall) {
-            GemmKArgs k{};
-            k.G = G;
-            k.rows.rows = R;
-            k.rows.a_stride = k.rows.b_stride = R;
-            k.a = k.b = x;
-            k.M = k.N = C;
-            k.out = A;
-            MOE_TRY(launch_gemm_k(k, false, s));
+        GemmKArgs k{};
+        k.G = G * pl.splits;
+        k.a = k.b = x;
+        k.M = k.N = n;
+        if (pl.splits > 1) {
+            k.rows.offsets = (const int32_t*)(ws + pl.offsets);
+            k.rows.rows = G * m;
+            k.out = sums;
         } else {
-            MOE_TRY(rows_by(R, C, x, x, (int64_t)R * C, true, R, A));
+            k.rows.rows = m;
+            k.rows.a_stride = k.rows.b_stride = m;
+            k.out = A;
         }
-        MOE_TRY(rows_by(n, n, A, A, nn, true, n, B));
-        (void)launch_pdl(orth_poly_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(nn * G, 256), 16 * 2 * kPairs)), dim3(256), 0, s,
-                         (const float*)A, B, (int64_t)n, nn * G);
+        MOE_TRY(launch_gemm_k(k, false, s));
+        if (pl.splits > 1) {
+            (void)launch_pdl(orth_sum_kernel, wide, dim3(256), 0, s, (const float*)sums, A, nn, nn * G, pl.splits);
+            MOE_TRY(cudaGetLastError());
+        }
+        MOE_TRY(rows_by(n, A, A, B));
+        (void)launch_pdl(orth_poly_kernel, wide, dim3(256), 0, s, (const float*)A, B, (int64_t)n, nn * G);
         MOE_TRY(cudaGetLastError());
-        if (tall) MOE_TRY(rows_by(R, C, x, B, nn, true, C, y));
-        else MOE_TRY(rows_by(R, R, B, x, (int64_t)R * C, false, C, y));
+        MOE_TRY(rows_by(m, x, B, y));
     }
-    const int64_t elems = (int64_t)R * C;
+    const int64_t elems = (int64_t)o.rows * o.cols;
     (void)launch_pdl(orth_out_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(elems, 1024), 8 * kPairs), (unsigned)G), dim3(256), 0, s,
-                     (const float*)(ws + pl.x[o.steps & 1]), (float*)o.out, elems, o.scale, o.counts);
+                     (const float*)(ws + pl.x[o.steps & 1]), (float*)o.out, elems, o.rows < o.cols ? o.rows : 0, o.cols, o.scale, o.counts);
     return cudaGetLastError();
 }
 
@@ -598,9 +650,13 @@ cudaError_t launch_orthogonalise(const OrthArgs& o, void* workspace, cudaStream_
     a.group = o.rows * pl.ld;
     a.beta = o.beta;
     a.nesterov = o.nesterov;
-    a.part = (double*)(ws + pl.part);
+    a.part = (float*)(ws + pl.part);
     a.parts = pl.parts;
-    a.inv = (float*)(ws + pl.inv);
+    a.G = o.groups;
+    a.ld_rows = std::max(o.rows, o.cols);
+    a.splits = pl.splits;
+    a.split_rows = pl.split_rows;
+    if (pl.splits > 1) a.offsets = (int32_t*)(ws + pl.offsets);
     if (o.bf16) {
         MOE_TRY(start_n<__nv_bfloat16>(a, o.groups, pl, ws + pl.x[0], (uint8_t*)(ws + pl.lo[0]), s));
         return steps_half(pl, o, ws, s);

@@ -394,15 +394,26 @@ __global__ void __launch_bounds__(256) vocab_col_kernel(const float* __restrict_
 __global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z, int V, int n, const float* __restrict__ lse,
                                                            const int32_t* __restrict__ target, const float* __restrict__ weight,
                                                            const float* __restrict__ scal, const float* __restrict__ h,
-                                                           float* __restrict__ h_live, int d) {
+                                                           float* __restrict__ h_live, int d, int tokens) {
     pdl_begin();
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)n * d; i += (int64_t)gridDim.x * 256)
         h_live[i] = has_target(target[i / d], V) ? h[i] : 0.f;
-    const int64_t total = (int64_t)V * n;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int v = (int)(i / n), t = (int)(i - (int64_t)v * n), y = target[t];
-        const float u = !has_target(y, V) ? 0.f : weight ? weight[t] : scal[0];
-        z[i] = has_target(y, V) ? u * (expf(z[i] - lse[t]) - (v == y ? 1.f : 0.f)) : 0.f;
+    // a block of 32 tokens by 8 rows of threads, its vocabulary rows eight at a time
+    const int t = (int)(blockIdx.x % tokens) * 32 + (threadIdx.x & 31);
+    if (t >= n) return;
+    const int y = target[t];
+    const bool live = has_target(y, V);
+    const float u = !live ? 0.f : weight ? weight[t] : scal[0], l = lse[t];
+    const int step = (int)(gridDim.x / tokens) * 64;
+    for (int v0 = (int)(blockIdx.x / tokens) * 64 + (threadIdx.x >> 5); v0 < V; v0 += step) {
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = v0 + 8 * k < V ? z[(int64_t)(v0 + 8 * k) * n + t] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int v = v0 + 8 * k;
+            if (v < V) z[(int64_t)v * n + t] = live ? u * (expf(x[k] - l) - (v == y ? 1.f : 0.f)) : 0.f;
+        }
     }
 }
 __global__ void __launch_bounds__(256) vocab_add_kernel(float* __restrict__ to, const float* __restrict__ from, int64_t n) {
@@ -639,9 +650,11 @@ cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, c
     MOE_TRY(cudaGetLastError());
     MOE_TRY(join(pl, a, ws, piece, t0, n, zt, s));
     if (!a.dh) return cudaSuccess;
-    (void)launch_pdl(vocab_dz_f32_kernel, dim3((unsigned)std::min<int64_t>(ceil_div((int64_t)V * n, 1024), 16 * 2 * kPairs)), dim3(256), 0, s,
+    const int tokens = (int)ceil_div(n, 32);  // (columns of blocks)
+    const int64_t dz_ctas = tokens * std::min<int64_t>(ceil_div(V, 64), std::max<int64_t>(1, 16 * 2 * kPairs / tokens));
+    (void)launch_pdl(vocab_dz_f32_kernel, dim3((unsigned)dz_ctas), dim3(256), 0, s,
                      zt, V, (int)n, (const float*)(ws + pl.lse), a.target + t0, a.weight ? a.weight + t0 : nullptr, (const float*)scal, h,
-                     (float*)(ws + pl.live), d);
+                     (float*)(ws + pl.live), d, tokens);
     MOE_TRY(cudaGetLastError());
     // dh: sums over parts of the vocabulary, each a group of rows of both operands
     float *dh = (float*)a.dh + t0 * d, *sums = (float*)(ws + pl.sums);

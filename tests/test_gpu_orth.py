@@ -153,7 +153,7 @@ def test_in_place(kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("size", [1e-36, 1e-25, 1e-12, 1e12, 1e25, 1e36])
+@pytest.mark.parametrize("size", [1e-40, 1e-36, 1e-25, 1e-12, 1e12, 1e25, 1e36, 1.5e37])
 def test_range_of_the_gradient(kind, size):
     dw, _ = make(2, 64, 100, kind, 7, size=size)
     out, _ = run(dw, None)

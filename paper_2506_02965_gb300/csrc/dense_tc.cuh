@@ -48,6 +48,7 @@ struct Problem {
     int per_split;
     int tri;        // tiles on and below the diagonal only (M == N)
     int band;       // tile order: bands of this many rows of tiles
+    int tn;         // AR = 32: a tile's columns, a multiple of 16 up to 128
     const int32_t* counts;  // [G]: matrices with counts <= 0 are left out; null: none
     uint64_t wait_ns;
 };
@@ -158,7 +159,8 @@ __global__ void __launch_bounds__(threads(EW), 1)
         }
     }
     __syncthreads();
-    const int mt = (p.M + TM - 1) / TM, nt = (p.N + TN - 1) / TN;
+    const int tn = AR == 32 ? p.tn : TN;  // a tile's columns
+    const int mt = (p.M + TM - 1) / TM, nt = (p.N + tn - 1) / tn;
     const int64_t per = p.tri ? (int64_t)mt * (mt + 1) / 2 : (int64_t)mt * nt;
     const int64_t total = (int64_t)s_active * p.splits * per;
     if (tile0 >= total) return;  // (alike in both CTAs of a pair)
@@ -185,7 +187,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
         }
         ti.diag = m == n;
         ti.m0 = m * TM + (int)rank * 128;
-        ti.n0 = n * TN;
+        ti.n0 = n * tn;
         ti.kb0 = ti.split * p.per_split;
         ti.kb1 = min(stages, ti.kb0 + p.per_split);
         return ti;
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
                     const uint32_t fb = full0 + 8u * stage;
                     // only the leader arrives, for the bytes of both CTAs; the peer's copies complete on its
                     // barrier, after the leader's MMAs released the stage to both
-                    if (rank == 0) mbar_expect_tx(full_bar(stage), NPAIR * STAGE_BYTES);
+                    if (rank == 0) mbar_expect_tx(full_bar(stage), AR == 32 ? 2u * BOX_A + 256u * (uint32_t)tn : NPAIR * STAGE_BYTES);
                     const int k0 = kb * KST;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -308,6 +310,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
         int stage = 0, acc = 0;
         uint32_t phase = 0, acc_phase = 0;
         bool issued = false;
+        const uint32_t idesc = AR == 32 ? (IDESC & ~(63u << 17)) | (uint32_t)(tn >> 3) << 17 : IDESC;
         for (int64_t t = tile0; t < total && rank == 0; t += tile_step) {
             const Tile ti = tile_at(t);
             bool ok = warp_wait(tempty_bar(acc), acc_phase ^ 1u);
@@ -326,8 +329,8 @@ __global__ void __launch_bounds__(threads(EW), 1)
                         const uint64_t bd = B_MN ? smem_desc(sb + kk * 2048, BOX_BYTES, 1024)
                                                  : smem_desc(sb + (kk / 4) * BOX_BYTES + (kk % 4) * 32, 16, 1024);
                         const uint32_t more = kb > ti.kb0 || kk > 0 ? 1u : 0u;
-                        if constexpr (PAIR) mma_bf16_pair(d, ad, bd, IDESC, more);
-                        else mma_bf16(d, ad, bd, IDESC, more);
+                        if constexpr (PAIR) mma_bf16_pair(d, ad, bd, idesc, more);
+                        else mma_bf16(d, ad, bd, idesc, more);
                     }
                     if constexpr (PAIR) mma_commit_pair(empty_bar(stage), 3);
                     else mma_commit(empty_bar(stage));
@@ -427,7 +430,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
 
 // ------------------------------------------------------------------------ host side
 // A stack of G matrices [outer, inner], rows `ld` and matrices `group` elements apart (16 bytes or a multiple). As an
-// operand: boxes of 64 x 128 (box_rows: an A of 32 rows), zeros outside; as an output: boxes of 32 x 32, nothing written outside.
+// operand: boxes of 64 x 128 (box_rows: an A of 32 rows, a K-major B of tn), zeros outside; as an output: boxes of 32 x 32, nothing written outside.
 bool make_map3(CUtensorMap* m, const void* base, int64_t inner, int64_t outer, int64_t ld, int G, int64_t group, bool store,
                int box_rows = 128);
 
@@ -437,7 +440,8 @@ static cudaError_t launch_as(const CUtensorMap& a, const CUtensorMap& b, const C
     auto kern = dense_kernel<A_MN, B_MN, PAIR, F16, EW, AR, Epi>;
     cudaError_t e = allow_dynamic_smem<dense_kernel<A_MN, B_MN, PAIR, F16, EW, AR, Epi>>(SMEM);
     if (e != cudaSuccess) return e;
-    const int64_t mt = (p.M + TM - 1) / TM, nt = (p.N + TN - 1) / TN;
+    if (AR != 32) p.tn = TN;
+    const int64_t mt = (p.M + TM - 1) / TM, nt = (p.N + p.tn - 1) / p.tn;
     const int64_t tiles = (int64_t)p.G * p.splits * (p.tri ? mt * (mt + 1) / 2 : mt * nt);
     if (tiles <= 0) return cudaSuccess;
     int most = sm_count();
@@ -498,6 +502,7 @@ static inline Problem problem(int M, int N, int K, int G = 1) {
     p.G = G;
     p.splits = 1;
     p.per_split = (K + KST - 1) / KST;
+    p.tn = 128;
     return p;
 }
 static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }

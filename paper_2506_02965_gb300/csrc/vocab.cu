@@ -43,15 +43,15 @@ template <bool STORE> struct VocabEpi : Plain {
 
     template <int NBUF, typename H> __device__ __forceinline__ void run(const H&, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
         const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane, cols = w.c1 - w.c0;
-        const int base = ti.n0 + w.c0;
-        if (base >= p.N) return;
+        const int base = ti.n0 + w.c0, end = min(p.N, ti.n0 + p.tn);
+        if (base >= end) return;
         const int y = m < p.M ? target[m] : -1;
         float mx = kNegInf;
 #pragma unroll 1
-        for (int c = 0; c < cols && base + c < p.N; c += 32) {
+        for (int c = 0; c < cols && base + c < end; c += 32) {
             float v[32];
             tmem_ld32(w.tmem + w.c0 + c, v);
-            const int left = p.N - (base + c);
+            const int left = end - (base + c);
             if (left >= 32) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) mx = fmaxf(mx, v[i]);
@@ -60,7 +60,7 @@ template <bool STORE> struct VocabEpi : Plain {
                 for (int i = 0; i < 32; ++i)
                     if (i < left) mx = fmaxf(mx, v[i]);
             }
-            const bool mine = y >= base + c && y < base + c + 32 && y < p.N;
+            const bool mine = y >= base + c && y < base + c + 32 && y < end;
             if (__any_sync(0xffffffffu, mine)) {
                 float z = 0.f;
 #pragma unroll
@@ -72,10 +72,10 @@ template <bool STORE> struct VocabEpi : Plain {
         const float ref = mx == kNegInf ? 0.f : mx;
         float sum = 0.f;
 #pragma unroll 1
-        for (int c = 0; c < cols && base + c < p.N; c += 32) {
+        for (int c = 0; c < cols && base + c < end; c += 32) {
             float v[32];
             tmem_ld32(w.tmem + w.c0 + c, v);
-            const int left = p.N - (base + c);
+            const int left = end - (base + c);
 #pragma unroll
             for (int i = 0; i < 32; ++i) {
                 v[i] = fast_exp(v[i] - ref);
@@ -89,7 +89,7 @@ template <bool STORE> struct VocabEpi : Plain {
                 store_box<NBUF>(w, out, u, base + c, row0, 0);
             }
         }
-        if (m < p.M) part[(int64_t)m * shares + base / cols] = make_float2(mx, sum);
+        if (m < p.M) part[(int64_t)m * shares + (ti.n0 / p.tn) * (p.tn > cols ? p.tn / cols : 1) + w.c0 / cols] = make_float2(mx, sum);
     }
 };
 
@@ -214,7 +214,6 @@ struct JoinArgs {
     int64_t T;
     float* scal;             // null: not in this launch
     float* loss;             // one CTA that holds the whole batch: the loss too
-    const float* all_token;
     int32_t* offsets;        // fp32: the vocabulary's parts as row offsets, or null
     int splits, split_rows;
 };
@@ -238,11 +237,11 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* h, const __nv_bfl
 template <bool BF16> __global__ void __launch_bounds__(1024) vocab_join_kernel(const JoinArgs a) {
     pdl_begin();
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    if (a.scal && blockIdx.x == gridDim.x - 1) {
+    if (a.scal && !a.loss && blockIdx.x == gridDim.x - 1) {
         weights_scale(a.all_target, a.all_weight, a.T, a.V, a.scal);
         if (a.offsets)
             for (int i = threadIdx.x; i <= a.splits; i += blockDim.x) a.offsets[i] = (int)min64(a.V, (int64_t)i * a.split_rows);
-        if (!a.loss) return;
+        return;
     }
     const int64_t t = a.loss ? threadIdx.x >> 5 : (int64_t)blockIdx.x * warps + (threadIdx.x >> 5);
     if (t < a.rows) {
@@ -280,9 +279,28 @@ template <bool BF16> __global__ void __launch_bounds__(1024) vocab_join_kernel(c
             a.token[t] = l;
         }
     }
-    if (a.loss) {
-        __syncthreads();
-        total_loss(a.all_token, a.all_target, a.all_weight, a.scal, a.T, a.V, a.loss);
+    if (!a.loss) return;
+    // the whole batch, a lane a token: what weights_scale and total_loss find
+    if (a.offsets)
+        for (int i = threadIdx.x; i <= a.splits; i += blockDim.x) a.offsets[i] = (int)min64(a.V, (int64_t)i * a.split_rows);
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int y = lane < a.rows ? a.target[lane] : -1;
+        const bool live = has_target(y, a.V);
+        if (y >= a.V) record_status(MOE_ERR_DEVICE_CHECK);
+        float u = a.all_weight && live ? a.all_weight[lane] : 0.f;
+        const int n = __popc(__ballot_sync(0xffffffffu, live));
+        const float most = warp_max(u == u ? fabsf(u) : INFINITY);
+        const float scale = a.all_weight ? (most < 3.4e38f ? most : 1.f) : 1.f / (float)max(n, 1);
+        if (!a.all_weight) u = scale;
+        double sum = live ? (double)a.token[lane] * u : 0.0;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) {
+            a.scal[0] = scale;
+            a.scal[1] = scale > 0.f ? 1.f / scale : 0.f;
+            *a.loss = (float)sum;
+        }
     }
 }
 
@@ -429,10 +447,14 @@ struct Plan {
     int shares, share;
     Shape logits, dh, dw;
     int ew, dw_ew; // epilogue warps of the logits, of dw
+    int tn;        // columns of a logits tile
     int f32_splits, f32_rows;
     // workspace: offsets
     size_t scal, token, lse, zy, part, e, live, sums, dwsum, offsets, total;
 };
+
+// products with 32 rows of A (dense_tc.cuh: AR)
+bool short_a(bool pair, int64_t rows) { return !pair && rows <= 32; }
 
 Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
     Plan p{};
@@ -449,9 +471,23 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
         p.dh = pick_shape(p.rows, d, V, p.rows <= 128 ? 4 * kMaxSplits : kMaxSplits);
         p.dw = pick_shape(V, d, p.rows, 1);
         p.ew = d < 1024 ? 8 : 4;  // a short contraction: the epilogue, not the product, sets a tile's time
+        p.tn = p.logits.pair ? 256 : 128;
+        if (short_a(p.logits.pair, p.rows)) {
+            // few tokens stream W: the width by which the rounds of tiles come out fullest (65536: 112 columns, four rounds of
+            // 147 tiles; of 128 columns four of 128). Whole staging boxes where the exponentials are stored.
+            p.ew = 4;
+            int64_t least = 0;
+            for (int t = 128; t >= 64; t -= grads ? 32 : 16) {
+                const int64_t cost = ceil_div(ceil_div(V, t), 2 * kPairs) * (t + 8);
+                if (least == 0 || cost < least) {
+                    least = cost;
+                    p.tn = t;
+                }
+            }
+        }
         // a contraction of a few stages: the stores set the time
         p.dw_ew = p.rows <= kShortRows ? 8 : 4;
-        p.share = (p.logits.pair ? 256 : 128) / (p.ew / 4);
+        p.share = p.tn / (p.ew / 4);
         p.shares = (int)ceil_div(V, p.share);
     } else {
         const int64_t most = std::max<int64_t>(128, ((int64_t)1 << 28) / V / 128 * 128);
@@ -494,8 +530,6 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
     return p;
 }
 
-bool short_a(bool pair, int64_t rows) { return !pair && rows <= 32; }
-
 template <bool STORE>
 cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const VocabEpi<STORE>& e,
                    cudaStream_t s) {
@@ -504,8 +538,9 @@ cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, c
         return launch_as<false, false, true, false, 4>(a, b, o, p, e, s);
     }
     if (short_a(pl.logits.pair, p.M)) {
-        if (pl.ew == 8) return launch_as<false, false, false, false, 8, 32>(a, b, o, p, e, s);
-        return launch_as<false, false, false, false, 4, 32>(a, b, o, p, e, s);
+        Problem q = p;
+        q.tn = pl.tn;
+        return launch_as<false, false, false, false, 4, 32>(a, b, o, q, e, s);
     }
     if (pl.ew == 8) return launch_as<false, false, false, false, 8>(a, b, o, p, e, s);
     return launch_as<false, false, false, false, 4>(a, b, o, p, e, s);
@@ -555,7 +590,6 @@ cudaError_t join(const Plan& pl, const VocabArgs& a, char* ws, int piece, int64_
     j.zy = (const float*)(ws + pl.zy);
     j.zt = zt;
     j.lse = (float*)(ws + pl.lse);
-    j.all_token = token_loss(pl, a, ws);
     j.token = token_loss(pl, a, ws) + t0;
     j.all_target = a.target;
     j.all_weight = a.weight;
@@ -582,15 +616,16 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     const int d = a.d, V = a.V;
     const __nv_bfloat16* h = (const __nv_bfloat16*)a.h + t0 * d;
     float* scal = (float*)(ws + pl.scal);
-    CUtensorMap mh, mw, me;
-    if (!make_map3(&mh, h, d, n, d, 1, 0, false, short_a(pl.logits.pair, n) ? 32 : 128) || !make_map3(&mw, a.w, d, V, d, 1, 0, false))
+    CUtensorMap mh, mw, ml, me;  // (ml: W for the logits)
+    if (!make_map3(&mh, h, d, n, d, 1, 0, false, short_a(pl.logits.pair, n) ? 32 : 128) || !make_map3(&mw, a.w, d, V, d, 1, 0, false) ||
+        !make_map3(&ml, a.w, d, V, d, 1, 0, false, short_a(pl.logits.pair, n) ? pl.tn : 128))
         return cudaErrorInvalidValue;
     Problem p = problem((int)n, V, d);
     if (a.dh) {
         if (!make_map3(&me, ws + pl.e, V, n, pl.ld, 1, 0, true)) return cudaErrorInvalidValue;
-        MOE_TRY(logits(pl, mh, mw, me, p, VocabEpi<true>{{}, a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
+        MOE_TRY(logits(pl, mh, ml, me, p, VocabEpi<true>{{}, a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
     } else {
-        MOE_TRY(logits(pl, mh, mw, mh, p, VocabEpi<false>{{}, a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
+        MOE_TRY(logits(pl, mh, ml, mh, p, VocabEpi<false>{{}, a.target + t0, (float2*)(ws + pl.part), (float*)(ws + pl.zy), pl.shares}, s));
     }
     MOE_TRY(join(pl, a, ws, piece, t0, n, nullptr, s));
     if (!a.dh) return cudaSuccess;

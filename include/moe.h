@@ -502,7 +502,7 @@ moe_status moe_vocab_loss_workspace_size(int64_t T, int32_t d, int32_t V, moe_dt
  *   dh [T,d], dw [V,d] dtype out: both, or both NULL (the loss alone).
  * A token with target < 0 has none: token_loss 0 and no gradient, whatever its h holds (one with target >= V too, and it
  * is recorded as MOE_ERR_DEVICE_CHECK). With gradients the probabilities of a piece of the tokens are held at once: in
- * bf16 max(4096, 2d) tokens at most (2 V bytes each), in fp32 about 2^28 / V (4 V bytes each).
+ * bf16 max(4096, 2d, 2^28 / V) tokens at most (2 V bytes each), in fp32 about 2^28 / V (4 V bytes each).
  * bf16: d a multiple of 128; dz is rounded to bf16 (relative to the largest |u_t|), sums are fp32. fp32: d % 4 == 0.
  * h, w, dh, dw, workspace 16-byte aligned. Deterministic.
  */

@@ -96,6 +96,36 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// A product's fp32 sums, [splits][G][M][N] (N a multiple of 4), stored or (ADD) added to what is there.
+template <bool ADD> struct SumEpi {
+    template <int CHUNKS> struct Held {};
+    template <int NBUF, typename H> __device__ __forceinline__ void fetch(H&, const Problem&, const Tile&, Warp&) const {}
+    float* sums;
+
+    template <int NBUF, typename H> __device__ __forceinline__ void run(const H&, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap*) const {
+        const int m = ti.m0 + w.q * 32 + w.lane;
+        float* at = sums + (((int64_t)ti.split * p.G + ti.g) * p.M + m) * p.N;
+#pragma unroll 1
+        for (int c = w.c0; c < w.c1 && ti.n0 + c < p.N; c += 32) {
+            float v[32];
+            tmem_ld32(w.tmem + c, v);
+            if (m < p.M) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    if (ti.n0 + c + i >= p.N) break;
+                    float4* to = reinterpret_cast<float4*>(at + ti.n0 + c + i);
+                    float4 s = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                    if (ADD) {
+                        const float4 b = *to;
+                        s = make_float4(s.x + b.x, s.y + b.y, s.z + b.z, s.w + b.w);
+                    }
+                    *to = s;
+                }
+            }
+        }
+    }
+};
+
 // 32 columns of this lane's row, as 16 words of two 16-bit values, through a staging box to the output map (which
 // cuts what lies outside the matrix). NBUF boxes per warp, each store in flight until its box is needed again.
 template <int NBUF>
@@ -526,7 +556,7 @@ static inline Shape pick_shape(int64_t M, int64_t N, int64_t K, int max_splits, 
             const int64_t each = ceil_div(stages, s), real = ceil_div(stages, each);
             const int64_t rounds = ceil_div(tiles * real, pair ? kPairs : 2 * kPairs);
             const double cost = (double)rounds * ((double)each + 2) * (pair ? 1.0 : 0.92) +
-                                (real > 1 ? 4 + (double)real * M * N * 8 / (6.5e6 * 0.7) : 0);
+                                (real > 1 ? 5 + (double)real * G * M * N * 8 / (6.5e6 * 0.7) : 0);
             if (least == 0 || cost < least) {
                 least = cost;
                 best = {pair != 0, (int)real};

@@ -131,12 +131,20 @@ template <typename T, int N> __global__ void __launch_bounds__(256) orth_norm_ke
     const int g = blockIdx.y;
     if (a.counts && a.counts[g] <= 0) return;
     Squares q;
-    const int64_t spans = a.elems / N, base = g * a.elems;
+    // whole spans of the matrix, and the few values before and behind them
+    const int64_t first = g * a.elems, base = (first + N - 1) / N * N, end = first + a.elems;
+    const int64_t spans = end > base ? (end - base) / N : 0, head = min(base, end) - first, tail = end - (min(base, end) + spans * N);
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < spans; i += (int64_t)gridDim.x * 256) {
         float u[N], m[N];
         update_of<T, N>(a, base + i * N, u, m);
 #pragma unroll
         for (int j = 0; j < N; ++j) q.add(u[j]);
+    }
+    if (blockIdx.x == 0 && (int64_t)threadIdx.x < head + tail) {
+        const int64_t i = threadIdx.x;
+        float u[1], m[1];
+        update_of<T, 1>(a, i < head ? first + i : end - tail + (i - head), u, m);
+        q.add(u[0]);
     }
     float v[3] = {q.big, q.mid, q.small};
     __shared__ float s_part[8][3];
@@ -191,21 +199,17 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, voi
     if (a.counts && a.counts[g] <= 0) return;
     const float2 inv = inverse_norm(a, g);
     const int64_t base = g * a.elems;
-    const int per_row = a.cols / N;
-    // N = 16: a warp takes blocks of 8 rows by 64 columns, so that X's rows and the residuals' boxes both get whole lines
-    const int blocks = (per_row + 3) / 4, rows = (int)(a.elems / a.cols);
-    const int64_t spans = N == 16 ? (int64_t)((rows + 7) / 8) * blocks * 32 : a.elems / N;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < spans; i += (int64_t)gridDim.x * 256) {
-        int row, col;
-        if constexpr (N == 16) {
-            const uint32_t b = (uint32_t)(i >> 5), rb = b / (uint32_t)blocks;
-            row = (int)rb * 8 + (threadIdx.x & 31) / 4;
-            col = ((int)(b - rb * blocks) * 4 + (threadIdx.x & 3)) * 16;
-            if (row >= rows || col >= a.cols) continue;
-        } else {
-            row = (int)(i / per_row);
-            col = (int)(i - (int64_t)row * per_row) * N;
-        }
+    const int rows = (int)(a.elems / a.cols);
+    // N = 16: a warp takes blocks of 8 rows by 64 columns, so that X's rows and the residuals' boxes both get whole lines;
+    // else of 8 rows by 4 spans of N columns (1, of any alignment: of a row by 32)
+    constexpr int ACROSS = N == 1 ? 32 : 4, DOWN = 32 / ACROSS;
+    const int blocks = (a.cols + ACROSS * N - 1) / (ACROSS * N);
+    const int64_t items = (int64_t)((rows + DOWN - 1) / DOWN) * blocks;
+    for (int64_t it = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); it < items; it += (int64_t)gridDim.x * 8) {
+        const int rb = (int)((uint32_t)it / (uint32_t)blocks);
+        const int row = rb * DOWN + (threadIdx.x & 31) / ACROSS;
+        const int col = (((int)it - rb * blocks) * ACROSS + (threadIdx.x & (ACROSS - 1))) * N;
+        if (row >= rows || col >= a.cols) continue;
         const int64_t from = base + (int64_t)row * a.cols + col;
         float u[N], m[N];
         update_of<T, N>(a, from, u, m);
@@ -379,7 +383,7 @@ template <bool LAST> struct StepEpi {
     }
     template <int NBUF, int CHUNKS>
     __device__ __forceinline__ void run(const Held<CHUNKS>& held, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
-        const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
+        const int row0 = ti.m0 + w.q * 32;
 #pragma unroll
         for (int k = 0; k < CHUNKS; ++k) {
             const int col = ti.n0 + w.c0 + 32 * k;
@@ -402,11 +406,25 @@ template <bool LAST> struct StepEpi {
                 for (int i = 0; i < 16; ++i) u[i] = pack_bf16(v[2 * i] * scale, v[2 * i + 1] * scale);
                 if (by_map) {
                     store_box<NBUF>(w, map, u, col, row0, ti.g);
-                } else if (m < p.M) {
-                    __nv_bfloat16* to = out + ((int64_t)ti.g * p.M + m) * p.N + col;
+                } else {
+                    // rows that no map serves (their length is no multiple of 16 bytes): through the box, a row of 32
+                    // values a time, a lane each
+                    if (w.lane == 0) bulk_wait_read<NBUF - 1>();
+                    __syncwarp();
+                    uint8_t* box = w.box + w.seq % NBUF * OUT_BOX_BYTES;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (col + i < p.N) to[i] = __ushort_as_bfloat16((uint16_t)(u[i / 2] >> (i & 1 ? 16 : 0)));
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<uint4*>(box + w.lane * 64 + ((i ^ ((w.lane >> 1) & 3)) << 4)) =
+                            make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+                    __syncwarp();
+                    __nv_bfloat16* to = out + ((int64_t)ti.g * p.M + row0) * p.N + col + w.lane;
+                    const int rows = min(32, p.M - row0);
+                    for (int r = 0; r < rows; ++r) {
+                        const int j = w.lane / 8;
+                        const __nv_bfloat16 x = *reinterpret_cast<const __nv_bfloat16*>(box + r * 64 + ((j ^ ((r >> 1) & 3)) << 4) + (w.lane % 8) * 2);
+                        if (col + w.lane < p.N) to[(int64_t)r * p.N] = x;
+                    }
+                    __syncwarp();
                 }
             } else {
                 uint32_t r[8];
@@ -428,6 +446,28 @@ template <bool LAST> struct StepEpi {
         }
     }
 };
+
+// A in fp16 from its parts' sums, in order: [splits][G][n][width] -> rows of ld. A block row of 64 columns by 4 rows.
+__global__ void __launch_bounds__(256) orth_square_kernel(const float* __restrict__ sums, int splits, int n, int ld, int width, float alpha,
+                                                          __half* __restrict__ out, const int32_t* __restrict__ counts) {
+    pdl_begin();
+    const int g = blockIdx.y;
+    if (counts && counts[g] <= 0) return;
+    const int64_t part = (int64_t)gridDim.y * n * width;
+    for (int row = (int)blockIdx.x * 4 + (threadIdx.x >> 6); row < n; row += (int)gridDim.x * 4) {
+        for (int col = (threadIdx.x & 63) * 2; col < n; col += 128) {
+            const float* p = sums + ((int64_t)g * n + row) * width + col;
+            float x = 0.f, y = 0.f;
+#pragma unroll 8
+            for (int k = 0; k < splits; ++k) {
+                const float2 v = *reinterpret_cast<const float2*>(p + k * part);
+                x += v.x;
+                y += v.y;
+            }
+            *reinterpret_cast<uint32_t*>(out + ((int64_t)g * n + row) * ld + col) = pack_half(x * alpha, y * alpha);
+        }
+    }
+}
 
 // ---------------------------------------------------------------- fp32
 // B = a I + b A + c A A, over A's square
@@ -467,9 +507,23 @@ struct Plan {
     int64_t ld, ldn;    // row strides of X and of the squares
     int row_boxes, col_boxes;  // of X's residuals
     int parts;          // CTAs per matrix of the first passes
+    Shape gram;              // bf16: tiles and parts of A's product
     int splits, split_rows;  // fp32: parts of X^T X's contraction
     size_t part, offsets, sums, x[2], lo[2], a, b, total;
 };
+
+// A's product: the lower tiles in one, or (few tiles, a long side) all tiles in parts, whose sums a pass adds up.
+Shape pick_gram(int64_t G, int64_t n, int64_t m) {
+    const Shape whole = pick_shape(n, n, m, 1, G, true);
+    const Shape parts = pick_shape(n, ceil_div(n, 4) * 4, m, 64, G, false);
+    const double stages = (double)ceil_div(m, KST);
+    auto time = [&](const Shape& s, bool tri) {
+        const int64_t t = s.pair ? 256 : 128, mt = ceil_div(n, t), tiles = G * (tri ? mt * (mt + 1) / 2 : mt * mt) * s.splits;
+        return (double)ceil_div(tiles, s.pair ? kPairs : 2 * kPairs) * (stages / s.splits + 2) * (s.pair ? 1.0 : 0.92) +
+               (s.splits > 1 ? 8 + (double)s.splits * G * n * n * 8 / (6.5e6 * 0.7) : 0);
+    };
+    return parts.splits > 1 && time(parts, false) < time(whole, true) ? parts : Shape{whole.pair, 1};
+}
 
 Plan plan(int G, int rows, int cols, bool bf16) {
     Plan p{};
@@ -481,9 +535,13 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     const int64_t want = ceil_div((int64_t)rows * cols, 8 * 256);
     p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(16 * kPairs, G)));
     p.splits = 1;
-    if (!bf16) {
-        const int64_t m = std::max(rows, cols), tiles = G * ceil_div(p.n, 128) * ceil_div(p.n, 128);
+    const int m = std::max(rows, cols);
+    if (bf16) {
+        p.gram = pick_gram(G, p.n, m);
+    } else {
+        const int64_t tiles = G * ceil_div(p.n, 128) * ceil_div(p.n, 128);
         int64_t sp = std::min<int64_t>(std::min<int64_t>(256 / G, 2 * kPairs / tiles), m / 128);  // one round of tiles
+
         sp = std::max<int64_t>(sp, 1);
         p.split_rows = (int)(ceil_div(ceil_div(m, sp), 32) * 32);
         p.splits = (int)ceil_div(m, p.split_rows);
@@ -501,7 +559,7 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     for (int i = 0; i < 2; ++i) p.lo[i] = bf16 ? take((size_t)G * p.row_boxes * p.col_boxes * LO_BOX) : 0;
     p.a = take(as * es);
     p.b = take(as * es);
-    p.sums = take(p.splits > 1 ? as * es * p.splits : 0);
+    p.sums = take(p.splits > 1 ? as * 4 * p.splits : p.gram.splits > 1 ? (size_t)p.gram.splits * G * p.n * p.ldn * 4 : 0);
     p.total = at;
     return p;
 }
@@ -518,7 +576,7 @@ cudaError_t start(const UpdateArgs& a, int G, const Plan& pl, void* hi, uint8_t*
     // (A launch of both per matrix, whose second pass then reads from the L2, takes longer: 16 x 36 us for matrices of
     // 5632 x 1024, all in one of each 318.)
     const dim3 grid((unsigned)a.parts, (unsigned)G);
-    (void)launch_pdl(orth_norm_kernel<T, N < 8 ? N : 8>, grid, dim3(256), 0, s, a);
+    (void)launch_pdl(orth_norm_kernel<T, 8>, grid, dim3(256), 0, s, a);
     (void)launch_pdl(orth_start_kernel<T, N, HALF>, grid, dim3(256), 0, s, a, hi, lo, pl.row_boxes, pl.col_boxes);
     return cudaGetLastError();
 }
@@ -535,6 +593,12 @@ template <bool A_MN, bool B_MN, typename Epi>
 cudaError_t product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, Problem p, const Epi& e, cudaStream_t s) {
     if (pick_shape(p.M, p.N, p.K, 1, p.G, p.tri).pair) return launch_as<A_MN, B_MN, true, true, 8>(a, b, o, p, e, s);
     return launch_as<A_MN, B_MN, false, true, 8>(a, b, o, p, e, s);
+}
+
+template <bool TALL>
+cudaError_t launch_gram(bool pair, const CUtensorMap& x, const Problem& p, const SumEpi<false>& e, cudaStream_t s) {
+    if (pair) return launch_as<TALL, TALL, true, true, 8>(x, x, x, p, e, s);
+    return launch_as<TALL, TALL, false, true, 8>(x, x, x, p, e, s);
 }
 
 cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t s) {
@@ -554,12 +618,25 @@ cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t
     Problem sq = problem(n, n, tall ? R : C, G), cube = problem(n, n, n, G), step = problem(R, C, n, G);
     sq.tri = cube.tri = 1;
     sq.counts = cube.counts = step.counts = o.counts;
+    Problem parts = sq;
+    parts.tri = 0;
+    parts.N = (n + 3) / 4 * 4;  // (columns past n: products with zeros)
+    split_k(parts, pl.gram.splits);
     for (int i = 0; i < o.steps; ++i) {
         const int x = i & 1, y = x ^ 1;
         const Term none{nullptr, 0, 0, 0.f};
         const SymEpi ea{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag};
-        if (tall) MOE_TRY((product<true, true>(mx[x], mx[x], sa, sq, ea, s)));
-        else MOE_TRY((product<false, false>(mx[x], mx[x], sa, sq, ea, s)));
+        if (pl.gram.splits > 1) {
+            const SumEpi<false> es{(float*)(ws + pl.sums)};
+            if (tall) MOE_TRY((launch_gram<true>(pl.gram.pair, mx[x], parts, es, s)));
+            else MOE_TRY((launch_gram<false>(pl.gram.pair, mx[x], parts, es, s)));
+            (void)launch_pdl(orth_square_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 4), 16 * kPairs), (unsigned)G), dim3(256), 0, s,
+                             (const float*)(ws + pl.sums), parts.splits, n, (int)pl.ldn, parts.N, kScaleA / (kScaleX * kScaleX), A, o.counts);
+            MOE_TRY(cudaGetLastError());
+        } else {
+            if (tall) MOE_TRY((product<true, true>(mx[x], mx[x], sa, sq, ea, s)));
+            else MOE_TRY((product<false, false>(mx[x], mx[x], sa, sq, ea, s)));
+        }
         const SymEpi eb{{A, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag};
         MOE_TRY((product<false, false>(ma, ma, sb, cube, eb, s)));
         const Term cx{(const __half*)(ws + pl.x[x]), pl.ld, xg, kA};

@@ -25,7 +25,7 @@ namespace {
 
 using namespace dense;
 
-constexpr int kMaxSplits = 16;      // of dh's contraction over the vocabulary (four times as many for up to 128 tokens)
+constexpr int kMaxSplits = 16;      // of the gradients' contractions (dh's of up to 128 tokens four times as many)
 constexpr int kShortRows = 256;     // dw of up to so many tokens: eight epilogue warps
 constexpr int kF32Splits = 64;
 constexpr int kColChunk = 512;      // fp32: vocabulary rows whose statistics one CTA takes
@@ -93,42 +93,32 @@ template <bool STORE> struct VocabEpi : Plain {
     }
 };
 
-// A product that is stored in bf16, times *alpha (OUT_BF16), as fp32 sums of one split or piece (OUT_F32), added to
-// such sums (OUT_ADD), or with such sums added to it, in bf16 (OUT_LAST).
-enum { OUT_BF16, OUT_F32, OUT_ADD, OUT_LAST };
-template <int MODE> struct OutEpi : Plain {
+// A product in bf16, times *alpha; (LAST) with fp32 sums of the pieces before added to it.
+template <bool LAST> struct OutEpi : Plain {
     const float* alpha;
-    float* sums;  // [splits][M][N]
+    const float* sums;  // [M][N]
 
     template <int NBUF, typename H> __device__ __forceinline__ void run(const H&, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* out) const {
         const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
-        const float a = MODE == OUT_BF16 || MODE == OUT_LAST ? *alpha : 1.f;
-        float* at = MODE == OUT_BF16 ? nullptr : sums + ((int64_t)ti.split * p.M + m) * p.N;
+        const float a = *alpha;
 #pragma unroll 1
         for (int c = w.c0; c < w.c1 && ti.n0 + c < p.N; c += 32) {
             float v[32];
             tmem_ld32(w.tmem + c, v);
-            if constexpr (MODE == OUT_ADD || MODE == OUT_LAST) {
+            if constexpr (LAST) {
                 if (m < p.M) {
+                    const float* at = sums + (int64_t)m * p.N + ti.n0 + c;
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        const float4 s = *reinterpret_cast<const float4*>(at + ti.n0 + c + i);
+                        const float4 s = *reinterpret_cast<const float4*>(at + i);
                         v[i] += s.x; v[i + 1] += s.y; v[i + 2] += s.z; v[i + 3] += s.w;
                     }
                 }
             }
-            if constexpr (MODE == OUT_F32 || MODE == OUT_ADD) {
-                if (m < p.M) {
+            uint32_t u[16];
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        *reinterpret_cast<float4*>(at + ti.n0 + c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-                }
-            } else {
-                uint32_t u[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) u[i] = pack_bf16(a * v[2 * i], a * v[2 * i + 1]);
-                store_box<NBUF>(w, out, u, ti.n0 + c, row0, 0);
-            }
+            for (int i = 0; i < 16; ++i) u[i] = pack_bf16(a * v[2 * i], a * v[2 * i + 1]);
+            store_box<NBUF>(w, out, u, ti.n0 + c, row0, 0);
         }
     }
 };
@@ -462,14 +452,15 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
     if (bf16) {
         // Pieces: with more than one, dW's sums over them are kept in fp32, 4 V d bytes; as many tokens as the stored
         // exponentials' 2 V bytes make of that, and no fewer than 4096 (below, dW's contraction is short).
-        const int64_t most = grads ? std::max<int64_t>(4096, 2 * (int64_t)d) : (int64_t)1 << 24;
+        // A small vocabulary's exponentials are taken up to half a GB.
+        const int64_t most = grads ? std::max<int64_t>(std::max<int64_t>(4096, 2 * (int64_t)d), ((int64_t)1 << 28) / V) : (int64_t)1 << 24;
         p.pieces = (int)ceil_div(t1, most);
         p.rows = p.pieces == 1 ? t1 : ceil_div(ceil_div(t1, p.pieces), 256) * 256;
         p.pieces = (int)ceil_div(t1, p.rows);
         p.ld = ceil_div(V, 64) * 64;
         p.logits = pick_shape(p.rows, V, d, 1);
         p.dh = pick_shape(p.rows, d, V, p.rows <= 128 ? 4 * kMaxSplits : kMaxSplits);
-        p.dw = pick_shape(V, d, p.rows, 1);
+        p.dw = pick_shape(V, d, p.rows, p.pieces == 1 ? kMaxSplits : 1);
         p.ew = d < 1024 ? 8 : 4;  // a short contraction: the epilogue, not the product, sets a tile's time
         p.tn = p.logits.pair ? 256 : 128;
         if (short_a(p.logits.pair, p.rows)) {
@@ -514,7 +505,7 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
         if (grads) {
             p.e = take((size_t)p.rows * p.ld * 2);
             p.live = take((size_t)p.rows * d * 2);
-            p.sums = take(p.dh.splits > 1 ? (size_t)p.dh.splits * p.rows * d * 4 : 0);
+            p.sums = take(std::max(p.dh.splits > 1 ? (size_t)p.dh.splits * p.rows * d * 4 : 0, p.dw.splits > 1 ? (size_t)p.dw.splits * V * d * 4 : 0));
             p.dwsum = take(p.pieces > 1 ? (size_t)V * d * 4 : 0);
         }
     } else {
@@ -545,19 +536,18 @@ cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, c
     if (pl.ew == 8) return launch_as<false, false, false, false, 8>(a, b, o, p, e, s);
     return launch_as<false, false, false, false, 4>(a, b, o, p, e, s);
 }
-template <bool A_MN, int MODE>
-cudaError_t product(bool pair, int ew, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const OutEpi<MODE>& e,
+template <bool A_MN, typename Epi>
+cudaError_t product(bool pair, int ew, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const Epi& e,
                     cudaStream_t s) {
-    if constexpr (A_MN && MODE == OUT_BF16) {
+    if constexpr (A_MN) {
         if (ew == 8) {
             if (pair) return launch_as<A_MN, true, true, false, 8>(a, b, o, p, e, s);
             return launch_as<A_MN, true, false, false, 8>(a, b, o, p, e, s);
         }
-    }
-    if (pair) return launch_as<A_MN, true, true, false, 4>(a, b, o, p, e, s);
-    if constexpr (!A_MN) {
+    } else {
         if (short_a(pair, p.M)) return launch_as<A_MN, true, false, false, 4, 32>(a, b, o, p, e, s);
     }
+    if (pair) return launch_as<A_MN, true, true, false, 4>(a, b, o, p, e, s);
     return launch_as<A_MN, true, false, false, 4>(a, b, o, p, e, s);
 }
 
@@ -647,20 +637,25 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     split_k(p, pl.dh.splits);
     float* sums = (float*)(ws + pl.sums);
     if (p.splits > 1) {
-        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_F32>{{}, nullptr, sums}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, SumEpi<false>{sums}, s)));
         MOE_TRY(sum_splits(sums, p.splits, n * d, scal, true, (__nv_bfloat16*)a.dh + t0 * d, s));
     } else {
-        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<OUT_BF16>{{}, scal, nullptr}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<false>{{}, scal, nullptr}, s)));
     }
     // dW = dz^T h: the tokens outside both
     if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false) || !make_map3(&mb, ws + pl.live, d, n, d, 1, 0, false) ||
         !make_map3(&mo, a.dw, d, V, d, 1, 0, true)) return cudaErrorInvalidValue;
     p = problem(V, d, (int)n);
     float* acc = (float*)(ws + pl.dwsum);
-    if (pl.pieces == 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_BF16>{{}, scal, nullptr}, s);
-    if (piece == 0) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_F32>{{}, nullptr, acc}, s);
-    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_ADD>{{}, nullptr, acc}, s);
-    return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<OUT_LAST>{{}, scal, acc}, s);
+    if (pl.pieces == 1 && pl.dw.splits > 1) {
+        split_k(p, pl.dw.splits);
+        MOE_TRY((product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, SumEpi<false>{sums}, s)));
+        return sum_splits(sums, p.splits, (int64_t)V * d, scal, true, a.dw, s);
+    }
+    if (pl.pieces == 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<false>{{}, scal, nullptr}, s);
+    if (piece == 0) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, SumEpi<false>{acc}, s);
+    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, SumEpi<true>{acc}, s);
+    return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<true>{{}, scal, acc}, s);
 }
 
 cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, cudaStream_t s) {

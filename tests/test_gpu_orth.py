@@ -98,7 +98,8 @@ def check(out, mom_out, dw, mom, kind, beta=0.95, nesterov=1, counts=None, steps
 
 
 SIZES = [(1, 1, 1), (1, 1, 5), (2, 5, 1), (1, 16, 16), (3, 100, 33), (3, 33, 100), (2, 64, 257), (2, 333, 1000), (2, 1000, 333), (1, 512, 512),
-         (5, 257, 255), (2, 300, 700), (1, 130, 2000), (17, 40, 24)]
+         (5, 257, 255), (2, 300, 700), (1, 130, 2000), (17, 40, 24),
+         (3, 44, 6748), (2, 4501, 83), (1, 3000, 130)]
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])

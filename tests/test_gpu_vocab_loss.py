@@ -115,7 +115,7 @@ def test_f32(T, d, V, weighted):
 
 
 @pytest.mark.parametrize("kind,T,d,V", [("bf16", 4097, 128, 300), ("bf16", 9000, 128, 301), ("bf16", 12289, 256, 77),
-                                        ("f32", 1100, 16, 262144)])
+                                        ("bf16", 4100, 128, 70001), ("bf16", 8300, 128, 70001), ("f32", 1100, 16, 262144)])
 def test_pieces_of_the_batch(kind, T, d, V):
     h, w, y, u = make(T, d, V, kind, 5)
     y[::3] = -1

@@ -150,7 +150,8 @@ template <bool A_MN, bool B_MN, bool PAIR, bool F16, int EW, int AR, typename Ep
 __global__ void __launch_bounds__(threads(EW), 1)
     dense_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
                  const __grid_constant__ Problem p, const __grid_constant__ Epi epi) {
-    pdl_begin();
+    // as pdl_begin(), but what needs no other kernel's writes comes before the wait: barriers, TMEM, the copies' descriptors
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int NPAIR = PAIR ? 2 : 1;
     constexpr int TM = 128 * NPAIR, TN = 128 * NPAIR;
     static_assert(AR == 128 || (AR == 32 && !PAIR && !A_MN), "rows of A");
@@ -173,55 +174,6 @@ __global__ void __launch_bounds__(threads(EW), 1)
     volatile int* abort_flag = &s_abort;
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
     const int64_t tile0 = (int64_t)blockIdx.x / NPAIR, tile_step = (int64_t)gridDim.x / NPAIR;
-
-    if (warp == 0) {  // the matrices that take part
-        int run = 0;
-        for (int g0 = 0; g0 < p.G; g0 += 32) {
-            const int g = g0 + lane;
-            const bool in = g < p.G && (!p.counts || p.counts[g] > 0);
-            const uint32_t m = __ballot_sync(0xffffffffu, in);
-            if (in) s_group[run + __popc(m & ((1u << lane) - 1))] = (unsigned char)g;
-            run += __popc(m);
-        }
-        if (lane == 0) {
-            s_active = run;
-            s_abort = 0;
-        }
-    }
-    __syncthreads();
-    const int tn = AR == 32 ? p.tn : TN;  // a tile's columns
-    const int mt = (p.M + TM - 1) / TM, nt = (p.N + tn - 1) / tn;
-    const int64_t per = p.tri ? (int64_t)mt * (mt + 1) / 2 : (int64_t)mt * nt;
-    const int64_t total = (int64_t)s_active * p.splits * per;
-    if (tile0 >= total) return;  // (alike in both CTAs of a pair)
-    const int stages = (p.K + KST - 1) / KST;
-
-    auto tile_at = [&](int64_t t) -> Tile {
-        Tile ti;
-        const int64_t gs = t / per;
-        const int64_t local = t - gs * per;
-        ti.g = s_group[gs / p.splits];
-        ti.split = (int)(gs % p.splits);
-        int m, n;
-        if (p.tri) {
-            m = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
-            while ((int64_t)m * (m + 1) / 2 > local) --m;
-            while ((int64_t)(m + 1) * (m + 2) / 2 <= local) ++m;
-            n = (int)(local - (int64_t)m * (m + 1) / 2);
-        } else {  // bands of p.band rows of tiles, swept along N, a band's rows innermost
-            const int64_t b = local / ((int64_t)p.band * nt);
-            const int first = (int)b * p.band, rows = min(p.band, mt - first);
-            const int rem = (int)(local - b * p.band * nt);
-            m = first + rem % rows;
-            n = rem / rows;
-        }
-        ti.diag = m == n;
-        ti.m0 = m * TM + (int)rank * 128;
-        ti.n0 = n * tn;
-        ti.kb0 = ti.split * p.per_split;
-        ti.kb1 = min(stages, ti.kb0 + p.per_split);
-        return ti;
-    };
 
     // 1024-byte aligned ring, the staging boxes behind it
     const uint32_t raw_u32 = smem_u32(smem_raw);
@@ -263,6 +215,8 @@ __global__ void __launch_bounds__(threads(EW), 1)
         }
         mbar_init(drain_bar, 1);
         s_fills = 0;
+        s_abort = 0;
+        for (const CUtensorMap* m : {&tmA, &tmB, &tmO}) asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)m) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -276,10 +230,55 @@ __global__ void __launch_bounds__(threads(EW), 1)
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         }
     }
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (warp == 0) {  // the matrices that take part
+        int run = 0;
+        for (int g0 = 0; g0 < p.G; g0 += 32) {
+            const int g = g0 + lane;
+            const bool in = g < p.G && (!p.counts || p.counts[g] > 0);
+            const uint32_t m = __ballot_sync(0xffffffffu, in);
+            if (in) s_group[run + __popc(m & ((1u << lane) - 1))] = (unsigned char)g;
+            run += __popc(m);
+        }
+        if (lane == 0) s_active = run;
+    }
     fence_before();
     __syncthreads();
     if constexpr (PAIR) cluster_sync_all();  // the peer's barriers are initialised
     fence_after();
+    const int tn = AR == 32 ? p.tn : TN;  // a tile's columns
+    const int mt = (p.M + TM - 1) / TM, nt = (p.N + tn - 1) / tn;
+    const int64_t per = p.tri ? (int64_t)mt * (mt + 1) / 2 : (int64_t)mt * nt;
+    const int64_t total = (int64_t)s_active * p.splits * per;
+    const int stages = (p.K + KST - 1) / KST;
+
+    auto tile_at = [&](int64_t t) -> Tile {
+        Tile ti;
+        const int64_t gs = t / per;
+        const int64_t local = t - gs * per;
+        ti.g = s_group[gs / p.splits];
+        ti.split = (int)(gs % p.splits);
+        int m, n;
+        if (p.tri) {
+            m = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
+            while ((int64_t)m * (m + 1) / 2 > local) --m;
+            while ((int64_t)(m + 1) * (m + 2) / 2 <= local) ++m;
+            n = (int)(local - (int64_t)m * (m + 1) / 2);
+        } else {  // bands of p.band rows of tiles, swept along N, a band's rows innermost
+            const int64_t b = local / ((int64_t)p.band * nt);
+            const int first = (int)b * p.band, rows = min(p.band, mt - first);
+            const int rem = (int)(local - b * p.band * nt);
+            m = first + rem % rows;
+            n = rem / rows;
+        }
+        ti.diag = m == n;
+        ti.m0 = m * TM + (int)rank * 128;
+        ti.n0 = n * tn;
+        ti.kb0 = ti.split * p.per_split;
+        ti.kb1 = min(stages, ti.kb0 + p.per_split);
+        return ti;
+    };
+
     const uint32_t tmem_base = s_tmem;
     // waits for work in flight (microseconds): not shortened with the caller's limit
     const uint64_t drain_limit = p.wait_ns > 200000000ull ? p.wait_ns : 200000000ull;

@@ -84,7 +84,7 @@ struct SortArgs {
     int64_t T;
     int32_t V;
     int passes, bits;
-    int32_t *key[2], *tok[2];  // between passes; [0]: the result
+    int2* pair[2];             // (id, token) between passes; [0]: the result
     int32_t* runs;             // the sums' list of runs to join: its length, 0 here
     uint8_t* zero;             // dW, or null
     size_t zero_bytes;
@@ -118,7 +118,7 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
         zero_fill(a.zero, a.zero_bytes, (int64_t)(blockIdx.x - ctas) * SORT_THREADS + threadIdx.x, (int64_t)(gridDim.x - ctas) * SORT_THREADS);
         return;
     }
-    extern __shared__ int32_t s_hist[];  // [SORT_WARPS][bins], and of ONE [2][2][T] keys and tokens
+    extern __shared__ int32_t s_hist[];  // [SORT_WARPS][bins], and of ONE [2][T] pairs
     __shared__ int32_t s_tot[SORT_BINS], s_base[SORT_BINS], s_sum[SORT_WARPS];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int cta = (int)blockIdx.x;
@@ -127,28 +127,28 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
     const int64_t per = ((T + warps - 1) / warps + 31) / 32 * 32;
     const int64_t beg = min64(T, (cta * SORT_WARPS + warp) * per), end = min64(T, beg + per);
     int32_t* hist = s_hist + warp * bins;
-    int32_t* held = s_hist + SORT_WARPS * bins;
+    int2* held = reinterpret_cast<int2*>(s_hist + SORT_WARPS * bins);
 
     for (int p = 0; p < a.passes; ++p) {
         const int shift = p * bits, left = a.passes - 1 - p;
-        const int32_t *kin = ONE ? held + (left & 1) * 2 * T : a.key[(left + 1) & 1], *tin = ONE ? kin + T : a.tok[(left + 1) & 1];
-        int32_t *kout = ONE ? held + ((left + 1) & 1) * 2 * T : a.key[left & 1], *tout = ONE ? kout + T : a.tok[left & 1];
-        auto key_at = [&](int64_t i) -> int32_t {
-            if (p > 0) return ONE ? kin[i] : __ldcg(kin + i);  // (through L2: another SM of the cluster wrote them)
+        const int2* from = ONE ? held + (left & 1) * T : a.pair[(left + 1) & 1];
+        int2* to = ONE ? held + ((left + 1) & 1) * T : a.pair[left & 1];
+        auto pair_at = [&](int64_t i) -> int2 {
+            if (p > 0) return ONE ? from[i] : __ldcg(from + i);  // (through L2: another SM of the cluster wrote them)
             const int32_t id = a.ids[i];
             if (id >= a.V) record_status(MOE_ERR_DEVICE_CHECK);
-            return id < 0 || id >= a.V ? a.V : id;  // no row: after all others
+            return make_int2(id < 0 || id >= a.V ? a.V : id, (int32_t)i);  // no row: after all others
         };
         for (int i = lane; i < bins; i += 32) hist[i] = 0;
         __syncwarp();
         // KEYS keys a lane at a time; a warp with no more than that keeps them for the second walk
         constexpr int KEYS = 8;
-        int32_t k[KEYS];
+        int2 k[KEYS];
         auto load_keys = [&](int64_t i0) {
 #pragma unroll
             for (int j = 0; j < KEYS; ++j) {
                 const int64_t i = i0 + 32 * j + lane;
-                k[j] = i < end ? key_at(i) : 0;
+                k[j] = i < end ? pair_at(i) : make_int2(0, 0);
             }
         };
         for (int64_t i0 = beg; i0 < end; i0 += 32 * KEYS) {
@@ -159,7 +159,7 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
                 if (i - lane >= end) break;
                 const uint32_t there = __ballot_sync(0xffffffffu, i < end);
                 if (i < end) {
-                    const uint32_t d = ((uint32_t)k[j] >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
+                    const uint32_t d = ((uint32_t)k[j].x >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
                     if ((same & ((1u << lane) - 1)) == 0) hist[d] += __popc(same);
                 }
                 __syncwarp();
@@ -209,25 +209,18 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
         __syncthreads();
         for (int64_t i0 = beg; i0 < end; i0 += 32 * KEYS) {
             if (per > 32 * KEYS) load_keys(i0);
-            int32_t t[KEYS];
-#pragma unroll
-            for (int j = 0; j < KEYS; ++j) {
-                const int64_t i = i0 + 32 * j + lane;
-                t[j] = p == 0 || i >= end ? (int32_t)i : ONE ? tin[i] : __ldcg(tin + i);
-            }
 #pragma unroll
             for (int j = 0; j < KEYS; ++j) {
                 const int64_t i = i0 + 32 * j + lane;
                 if (i - lane >= end) break;
                 const uint32_t there = __ballot_sync(0xffffffffu, i < end);
                 if (i < end) {
-                    const uint32_t d = ((uint32_t)k[j] >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
+                    const uint32_t d = ((uint32_t)k[j].x >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
                     const int rank = __popc(same & ((1u << lane) - 1));
                     const int64_t at = s_base[d] + hist[d] + rank;
                     __syncwarp(there);
                     if (rank == 0) hist[d] += __popc(same);
-                    kout[at] = k[j];
-                    tout[at] = t[j];
+                    to[at] = k[j];
                 }
                 __syncwarp();
             }
@@ -236,19 +229,15 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
         if constexpr (ONE) __syncthreads();
         else tc::cluster_sync_all();
     }
-    if constexpr (ONE) {  // out in whole lines (scattered 4-byte stores take a cycle each)
-        for (int i = threadIdx.x; i < (int)T; i += SORT_THREADS) {
-            a.key[0][i] = held[2 * T + i];
-            a.tok[0][i] = held[3 * T + i];
-        }
+    if constexpr (ONE) {  // out in whole lines (scattered stores take a cycle each)
+        for (int i = threadIdx.x; i < (int)T; i += SORT_THREADS) a.pair[0][i] = held[T + i];
     }
     if (cta == 0 && threadIdx.x == 0) *a.runs = 0;
 }
 
 // ---------------------------------------------------------------- sums
 template <typename T> struct EmbedBwd {
-    const int32_t* key;  // [T] sorted ids, V: no row
-    const int32_t* tok;  // [T]
+    const int2* pair;    // [T] ids in order with their tokens; id V: no row
     int32_t* runs;       // [1 + chunks]: how many runs leave the chunk that they begin in, and those chunks, in any order
     const T* dout;
     T* dw;
@@ -289,9 +278,9 @@ __global__ void __launch_bounds__(PARTY) embed_sum_kernel(const EmbedBwd<T> a) {
     const uint32_t col = (uint32_t)(item % a.slabs) * a.party + threadIdx.x % a.party;
     const int64_t beg = chunk * a.chunk, end = min64(a.n, beg + a.chunk);
     if (beg >= end || col >= a.spr) return;
-    int32_t run = a.key[beg];
+    int32_t run = a.pair[beg].x;
     if (run >= a.V) return;
-    bool came = beg > 0 && a.key[beg - 1] == run;
+    bool came = beg > 0 && a.pair[beg - 1].x == run;
     float acc[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) acc[j] = 0.f;
@@ -305,8 +294,9 @@ __global__ void __launch_bounds__(PARTY) embed_sum_kernel(const EmbedBwd<T> a) {
         int32_t k[U], t[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            k[u] = p0 + u < end ? a.key[p0 + u] : a.V;
-            t[u] = p0 + u < end ? a.tok[p0 + u] : 0;
+            const int2 e = p0 + u < end ? a.pair[p0 + u] : make_int2(a.V, 0);
+            k[u] = e.x;
+            t[u] = e.y;
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -330,7 +320,7 @@ __global__ void __launch_bounds__(PARTY) embed_sum_kernel(const EmbedBwd<T> a) {
             for (int j = 0; j < N; ++j) acc[j] += f[j];
         }
     }
-    const bool leaves = end < a.n && a.key[end] == run;
+    const bool leaves = end < a.n && a.pair[end].x == run;
     if (came) part(0);
     else if (leaves) {
         part(1);
@@ -364,11 +354,11 @@ __global__ void __launch_bounds__(PARTY) embed_join_kernel(const EmbedBwd<T> a) 
     const int64_t chunks = (a.n + a.chunk - 1) / a.chunk, items = (int64_t)a.runs[0] * a.slabs;
     for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
         const int64_t chunk = a.runs[1 + item / a.slabs];
-        const int32_t run = a.key[(chunk + 1) * a.chunk];
+        const int32_t run = a.pair[(chunk + 1) * a.chunk].x;
         int64_t more = 0;  // chunks that the run comes into
         for (;;) {
             const int64_t c = chunk + 1 + more + threadIdx.x;
-            const int n = __syncthreads_count(c < chunks && a.key[c * a.chunk] == run);
+            const int n = __syncthreads_count(c < chunks && a.pair[c * a.chunk].x == run);
             more += n;
             if (n < PARTY) break;
         }
@@ -447,7 +437,7 @@ cudaError_t sums(EmbedBwd<T> a, int32_t d, cudaStream_t s) {
 }  // namespace
 
 size_t embed_workspace_bytes(int64_t T, int32_t d, int32_t V) {
-    return 4 * up((size_t)T * 4)+ up((size_t)(chunks_of(T, d) + 1) * 4) + up((size_t)chunks_of(T, d) * 2 * (size_t)d * 4);
+    return 2 * up((size_t)T * 8)+ up((size_t)(chunks_of(T, d) + 1) * 4) + up((size_t)chunks_of(T, d) * 2 * (size_t)d * 4);
 }
 
 cudaError_t launch_embed_fwd(const int32_t* ids, int64_t T, int32_t d, int32_t V, bool bf16, const void* w, float scale, void* out,
@@ -472,10 +462,8 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
     SortArgs b{};
     char* at = (char*)ws;
     for (int i = 0; i < 2; ++i) {
-        b.key[i] = (int32_t*)at;
-        at += up((size_t)T * 4);
-        b.tok[i] = (int32_t*)at;
-        at += up((size_t)T * 4);
+        b.pair[i] = (int2*)at;
+        at += up((size_t)T * 8);
     }
     b.runs = (int32_t*)at;
     at += up((size_t)(chunks_of(T, d) + 1) * 4);
@@ -514,9 +502,9 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
     // not: 131072 x 4096 237 us in two rounds)
     int clusters = 1;
     if (!accumulate) {
-        static std::atomic<int> resident[kMaxDevices][2] = {};
+        static std::atomic<int> resident[kMaxDevices][SORT_MAX_CTAS + 1] = {};
         const int dev = current_device();
-        std::atomic<int>* kept = dev >= 0 && dev < kMaxDevices && (one || ctas == SORT_MAX_CTAS) ? &resident[dev][one] : nullptr;
+        std::atomic<int>* kept = dev >= 0 && dev < kMaxDevices ? &resident[dev][ctas] : nullptr;
         clusters = kept ? kept->load() : 0;
         if (!clusters) {
             cfg.gridDim = dim3((unsigned)(sm_count() / ctas * ctas));
@@ -539,8 +527,7 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
     auto args = [&](auto* t) {
         using E = std::remove_pointer_t<decltype(t)>;
         EmbedBwd<E> a{};
-        a.key = b.key[0];
-        a.tok = b.tok[0];
+        a.pair = b.pair[0];
         a.runs = b.runs;
         a.dout = (const E*)dout;
         a.dw = (E*)dw;

@@ -196,8 +196,10 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, voi
     if (!HALF && a.offsets && g == 0 && blockIdx.x == 0)
         for (int i = threadIdx.x; i <= a.G * a.splits; i += 256)
             a.offsets[i] = (int32_t)((int64_t)(i / a.splits) * a.ld_rows + min(a.ld_rows, i % a.splits * a.split_rows));
-    if (a.counts && a.counts[g] <= 0) return;
-    const float2 inv = inverse_norm(a, g);
+    const bool called = !a.counts || a.counts[g] > 0;
+    if (HALF && !called) return;
+    // (the fp32 products take all matrices: one that is left out is zeros there)
+    const float2 inv = called ? inverse_norm(a, g) : make_float2(0.f, 0.f);
     const int64_t base = g * a.elems;
     const int rows = (int)(a.elems / a.cols);
     // N = 16: a warp takes blocks of 8 rows by 64 columns, so that X's rows and the residuals' boxes both get whole lines;
@@ -212,8 +214,13 @@ __global__ void __launch_bounds__(256) orth_start_kernel(const UpdateArgs a, voi
         if (row >= rows || col >= a.cols) continue;
         const int64_t from = base + (int64_t)row * a.cols + col;
         float u[N], m[N];
-        update_of<T, N>(a, from, u, m);
-        if (a.mom) store_f32<N>(a.mom_out + from, m);
+        if (called) {
+            update_of<T, N>(a, from, u, m);
+            if (a.mom) store_f32<N>(a.mom_out + from, m);
+        } else {
+#pragma unroll
+            for (int j = 0; j < N; ++j) u[j] = 0.f;
+        }
         const int64_t at = g * a.group + row * a.ld + col;
         if constexpr (HALF) {
             alignas(16) __half h[N];

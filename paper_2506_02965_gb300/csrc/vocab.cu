@@ -453,7 +453,7 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
         // Pieces: with more than one, dW's sums over them are kept in fp32, 4 V d bytes; as many tokens as the stored
         // exponentials' 2 V bytes make of that, and no fewer than 4096 (below, dW's contraction is short).
         // A small vocabulary's exponentials are taken up to half a GB.
-        const int64_t most = grads ? std::max<int64_t>(std::max<int64_t>(4096, 2 * (int64_t)d), ((int64_t)1 << 28) / V) : (int64_t)1 << 24;
+        const int64_t most = grads ? std::max<int64_t>(std::max<int64_t>(4096, 2 * (int64_t)d), ((int64_t)1 << 28) / V) : (int64_t)1 << 16;
         p.pieces = (int)ceil_div(t1, most);
         p.rows = p.pieces == 1 ? t1 : ceil_div(ceil_div(t1, p.pieces), 256) * 256;
         p.pieces = (int)ceil_div(t1, p.rows);

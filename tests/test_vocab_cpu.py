@@ -67,6 +67,7 @@ def test_vocab_loss_workspace():
     T, d, V = 8192, 1024, 131072
     logits = T * V * 2
     assert size(T, d, V, L.MOE_BF16, False) < logits / 50
+    assert size(100 * T, d, V, L.MOE_BF16, False) < logits / 4
     assert 4096 * V * 2 <= size(T, d, V, L.MOE_BF16, True) < logits + 4 * V * d
     assert size(16 * T, d, V, L.MOE_BF16, True) < size(T, d, V, L.MOE_BF16, True) * 1.05
     assert size(T, d, V, L.MOE_F32, True) < 3 * 2 ** 30

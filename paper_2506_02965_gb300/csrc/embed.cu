@@ -7,7 +7,7 @@
 // The gradient is a sum of rows in any order of ids, so the tokens are sorted by id first (stable: equal
 // ids stay in the order of the batch) and runs of equal ids are added in fp32, in that order, by fixed chunks of
 // the sorted tokens: no atomics, the same bits on every call. Three launches:
-//   sort    one cluster of 1 to 8 CTAs, a stable radix sort of (id, token) by digits of up to 9 bits; every
+//   sort    one cluster of 1 to 16 CTAs, a stable radix sort of (id, token) by digits of up to 9 bits; every
 //           warp owns a run of keys and counts their digits in shared memory, the CTAs read one another's
 //           totals through distributed shared memory; the other SMs zero dW meanwhile;
 //   sums    a party of threads per chunk of sorted tokens, a span of columns a thread: runs inside the chunk go
@@ -26,8 +26,9 @@ namespace {
 
 constexpr int SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32;
 constexpr int SORT_BITS = 9, SORT_BINS = 1 << SORT_BITS;
-constexpr int SORT_MAX_CTAS = 8;
-constexpr int SORT_ONE = 4096;  // tokens that one CTA sorts
+// Tokens that one CTA sorts; above, up to 16 of them (a cluster of that size has to be allowed, and found room for) with a
+// thousand tokens each or more: a CTA takes 8 us and 2.7 more per thousand tokens, a cluster's barriers 4.
+constexpr int SORT_MAX_CTAS = 16, SORT_ONE = 2048, SORT_PER_CTA = 1024;
 constexpr int PARTY = 256;  // threads of a CTA of the lookup, the sums and the joins
 
 // Sorted tokens per chunk: as many as leave one to two thousand threads an SM, 8 to 64 (a thread has eight rows on their
@@ -102,10 +103,12 @@ __device__ __forceinline__ void zero_fill(uint8_t* p, size_t bytes, int64_t part
 // The lanes of `there` whose digit is this lane's (a ballot per bit)
 __device__ __forceinline__ uint32_t alike(uint32_t there, uint32_t digit, int bits) {
     uint32_t m = there;
-    for (int b = 0; b < bits; ++b) {
-        const bool one = (digit >> b) & 1u;
-        const uint32_t v = __ballot_sync(there, one);
-        m &= one ? v : ~v;
+#pragma unroll
+    for (int b = 0; b < SORT_BITS; ++b) {
+        if (b < bits) {
+            const uint32_t one = (digit >> b) & 1u, v = __ballot_sync(there, one);
+            m &= v ^ (one - 1u);
+        }
     }
     return m;
 }
@@ -141,9 +144,10 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
         };
         for (int i = lane; i < bins; i += 32) hist[i] = 0;
         __syncwarp();
-        // KEYS keys a lane at a time; a warp with no more than that keeps them for the second walk
+        // KEYS keys a lane at a time; a warp with no more than that keeps them, and who is alike, for the second walk
         constexpr int KEYS = 8;
         int2 k[KEYS];
+        uint32_t same[KEYS];
         auto load_keys = [&](int64_t i0) {
 #pragma unroll
             for (int j = 0; j < KEYS; ++j) {
@@ -159,8 +163,9 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
                 if (i - lane >= end) break;
                 const uint32_t there = __ballot_sync(0xffffffffu, i < end);
                 if (i < end) {
-                    const uint32_t d = ((uint32_t)k[j].x >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
-                    if ((same & ((1u << lane) - 1)) == 0) hist[d] += __popc(same);
+                    const uint32_t d = ((uint32_t)k[j].x >> shift) & (uint32_t)(bins - 1);
+                    same[j] = alike(there, d, bits);
+                    if ((same[j] & ((1u << lane) - 1)) == 0) hist[d] += __popc(same[j]);
                 }
                 __syncwarp();
             }
@@ -208,18 +213,20 @@ template <bool ONE> __global__ void __launch_bounds__(SORT_THREADS) embed_sort_k
         }
         __syncthreads();
         for (int64_t i0 = beg; i0 < end; i0 += 32 * KEYS) {
-            if (per > 32 * KEYS) load_keys(i0);
+            const bool again = per > 32 * KEYS;
+            if (again) load_keys(i0);
 #pragma unroll
             for (int j = 0; j < KEYS; ++j) {
                 const int64_t i = i0 + 32 * j + lane;
                 if (i - lane >= end) break;
                 const uint32_t there = __ballot_sync(0xffffffffu, i < end);
                 if (i < end) {
-                    const uint32_t d = ((uint32_t)k[j].x >> shift) & (uint32_t)(bins - 1), same = alike(there, d, bits);
-                    const int rank = __popc(same & ((1u << lane) - 1));
+                    const uint32_t d = ((uint32_t)k[j].x >> shift) & (uint32_t)(bins - 1);
+                    if (again) same[j] = alike(there, d, bits);
+                    const int rank = __popc(same[j] & ((1u << lane) - 1));
                     const int64_t at = s_base[d] + hist[d] + rank;
                     __syncwarp(there);
-                    if (rank == 0) hist[d] += __popc(same);
+                    if (rank == 0) hist[d] += __popc(same[j]);
                     to[at] = k[j];
                 }
                 __syncwarp();
@@ -481,10 +488,18 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
     b.bits = (all + b.passes - 1) / b.passes;
     const bool one = T <= SORT_ONE;
     int ctas = one ? 1 : 2;
-    while (!one && ctas < SORT_MAX_CTAS && (int64_t)ctas * 4096 < T) ctas *= 2;
+    // (large clusters leave SMs without one, and so without a part in the zeros: four where those take longer than the sort;
+    // 16384 tokens, 131072 x 4096: 255 us with four, 290 with 16)
+    const int most = b.zero_bytes > (size_t)256 << 20 ? 4 : SORT_MAX_CTAS;
+    while (!one && ctas < most && (int64_t)ctas * SORT_PER_CTA < T) ctas *= 2;
     const size_t smem = (size_t)SORT_WARPS * (size_t)(1 << b.bits) * 4 + (one ? (size_t)T * 16 : 0);
     cudaError_t e = allow_dynamic_smem<embed_sort_kernel<true>>((size_t)SORT_WARPS * SORT_BINS * 4 + (size_t)SORT_ONE * 16);
-    if (e == cudaSuccess) e = allow_dynamic_smem<embed_sort_kernel<false>>((size_t)SORT_WARPS * SORT_BINS * 4);
+    if (e == cudaSuccess)
+        e = once_per_device<embed_sort_kernel<false>>([] {
+            const cudaError_t r = cudaFuncSetAttribute((const void*)embed_sort_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                       SORT_WARPS * SORT_BINS * 4);
+            return r != cudaSuccess ? r : cudaFuncSetAttribute((const void*)embed_sort_kernel<false>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        });
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(SORT_THREADS);
@@ -499,25 +514,28 @@ cudaError_t launch_embed_bwd(const int32_t* ids, int64_t T, int32_t d, int32_t V
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     // dW is zeroed by the SMs that do not sort, in one round: as many clusters as fit at once (19 of eight CTAs do
-    // not: 131072 x 4096 237 us in two rounds)
-    int clusters = 1;
-    if (!accumulate) {
-        static std::atomic<int> resident[kMaxDevices][SORT_MAX_CTAS + 1] = {};
-        const int dev = current_device();
+    // not: 131072 x 4096 237 us in two rounds, 170 in one)
+    static std::atomic<int> resident[kMaxDevices][SORT_MAX_CTAS + 1] = {};  // 1 more than that
+    const int dev = current_device();
+    int clusters = 0;
+    for (;; ctas /= 2) {
         std::atomic<int>* kept = dev >= 0 && dev < kMaxDevices ? &resident[dev][ctas] : nullptr;
-        clusters = kept ? kept->load() : 0;
-        if (!clusters) {
+        clusters = kept ? kept->load() - 1 : -1;
+        if (clusters < 0) {
             cfg.gridDim = dim3((unsigned)(sm_count() / ctas * ctas));
+            attr[0].val.clusterDim.x = (unsigned)ctas;
             if ((one ? cudaOccupancyMaxActiveClusters(&clusters, embed_sort_kernel<true>, &cfg)
-                     : cudaOccupancyMaxActiveClusters(&clusters, embed_sort_kernel<false>, &cfg)) != cudaSuccess ||
-                clusters < 2) {
+                     : cudaOccupancyMaxActiveClusters(&clusters, embed_sort_kernel<false>, &cfg)) != cudaSuccess) {
                 (void)cudaGetLastError();
-                clusters = 2;
+                clusters = 0;
             }
             clusters = std::min(clusters, sm_count() / ctas);
-            if (kept) *kept = clusters;
+            if (kept) *kept = clusters + 1;
         }
+        if (clusters >= 2 || ctas <= 2) break;
     }
+    attr[0].val.clusterDim.x = (unsigned)ctas;
+    clusters = accumulate ? 1 : std::max(clusters, 2);
     cfg.gridDim = dim3((unsigned)(clusters * ctas));
     cfg.numAttrs = 2;
     if ((e = one ? cudaLaunchKernelEx(&cfg, embed_sort_kernel<true>, b, ctas) : cudaLaunchKernelEx(&cfg, embed_sort_kernel<false>, b, ctas)) !=

@@ -9,10 +9,13 @@
 // bf16 matrices run in fp16. Every value is bounded (X's singular values never pass 1.21, so |X| < 1.21, |A| < 1.47,
 // |b A + c A A| < 2.81), so powers of two that put them below fp16's largest number keep 11 bits where bf16 would keep
 // 8: after five steps, which amplify what small singular directions carry by up to a^5 = 485, bf16 products are 1.2e-2
-// off (of the norm, 333 x 1000 to 2048 x 2048 matrices), fp16 ones 1.5e-3. Most of that is X's own rounding
-// between the steps, and it is where a few directions outweigh the rest (30 times: 8.5e-3) that it counts, so
-// the a X term takes X to 14 bits, its residual as an 8-bit float (e5m2, the upper half of an fp16). The other products
-// keep fp16. All sums are fp32.
+// off (of the norm, 333 x 1000 to 2048 x 2048 matrices of a gradient's few strong directions over noise). Two more
+// things bring that from 1.5e-3 (2.2e-3 for sides of some tens; 8.5e-3 where 16 directions outweigh the rest 30 times) to
+// 0.6e-3 (1.4e-3; 1e-3), below the 1.7e-3 of the result's own rounding to bf16:
+//   the a X term takes X to 14 bits, its residual as an 8-bit float (e5m2, the upper half of an fp16);
+//   from the third step on B = b A + c A A is held as B + t I, and a X + B X taken as (a - t) X + (B + t I) X: most singular
+//   values are near 1 by then, B near -2.5 I, and what is left of B + t I is rounded less, as is its product with X.
+// The other roundings stay fp16's. All sums are fp32.
 //
 // A matrix with more rows than columns is not transposed: A = X^T X and X = a X + X (b A + c A A), with the operands'
 // other major. fp32 matrices take the fp32 products throughout.
@@ -30,6 +33,8 @@ using namespace dense;
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kScaleX = 256.f, kScaleA = 4096.f;  // of the fp16 X, and of A and b A + c A A
 constexpr float kResidual = 4096.f;                 // of X's residual, which is 2^-12 of X at most
+// t of a step, a number of few bits: about the mean of -B's eigenvalues where a few directions do not outweigh the rest
+float shift_of(int step) { return step < 2 ? 0.f : step == 2 ? 1.25f : step == 3 ? 2.25f : 2.5f; }
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -313,6 +318,7 @@ struct SymEpi {
     float alpha;
     __half* out;
     int64_t ld, group;
+    float shift;  // added to the diagonal
 
     template <int CHUNKS> using Held = Ahead<CHUNKS>;
     template <int NBUF, int CHUNKS>
@@ -339,6 +345,10 @@ struct SymEpi {
                     v[2 * i] = fmaf(c.beta, y.x, v[2 * i]);
                     v[2 * i + 1] = fmaf(c.beta, y.y, v[2 * i + 1]);
                 }
+            }
+            if (row0 == ti.n0 + k && shift != 0.f) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] += i == w.lane ? shift : 0.f;
             }
             uint32_t u[16];
 #pragma unroll
@@ -632,7 +642,7 @@ cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t
     for (int i = 0; i < o.steps; ++i) {
         const int x = i & 1, y = x ^ 1;
         const Term none{nullptr, 0, 0, 0.f};
-        const SymEpi ea{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag};
+        const SymEpi ea{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag, 0.f};
         if (pl.gram.splits > 1) {
             const SumEpi<false> es{(float*)(ws + pl.sums)};
             if (tall) MOE_TRY((launch_gram<true>(pl.gram.pair, mx[x], parts, es, s)));
@@ -644,9 +654,10 @@ cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t
             if (tall) MOE_TRY((product<true, true>(mx[x], mx[x], sa, sq, ea, s)));
             else MOE_TRY((product<false, false>(mx[x], mx[x], sa, sq, ea, s)));
         }
-        const SymEpi eb{{A, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag};
+        const float t = shift_of(i);
+        const SymEpi eb{{A, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag, t * kScaleA};
         MOE_TRY((product<false, false>(ma, ma, sb, cube, eb, s)));
-        const Term cx{(const __half*)(ws + pl.x[x]), pl.ld, xg, kA};
+        const Term cx{(const __half*)(ws + pl.x[x]), pl.ld, xg, kA - t};
         const uint8_t* lo = (const uint8_t*)(ws + pl.lo[x]);
         if (i + 1 < o.steps) {
             const StepEpi<false> e{cx, lo, 1.f / kScaleA, (uint8_t*)(ws + pl.lo[y]), pl.row_boxes, pl.col_boxes, 1.f, nullptr, 1};

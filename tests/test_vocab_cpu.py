@@ -94,6 +94,10 @@ def test_orthogonalise_limits():
             status=L.MOE_ERR_UNSUPPORTED)
     with pytest.raises(L.MoEError):
         L.moe_orthogonalise_workspace_size(2, 0, 8, L.MOE_F32)
+    for rows, cols in ((1 << 24, 1), (1, 1 << 24)):  # either side's total is an int32 offset
+        assert L.moe_orthogonalise_workspace_size(127, rows, cols, L.MOE_F32) > 0
+        with pytest.raises(L.MoEError, match="2\\^31"):
+            L.moe_orthogonalise_workspace_size(128, rows, cols, L.MOE_F32)
     n = L.moe_orthogonalise_workspace_size(4, 5632, 1024, L.MOE_BF16)
     assert 6 * 4 * 5632 * 1024 <= n <= 7 * 4 * 5632 * 1024
     L.moe_orthogonalise(0, 8, 8, L.MOE_BF16, None, None, 0.9, 1, None, 5, 1.0, None, None, None, 0, stream=0)

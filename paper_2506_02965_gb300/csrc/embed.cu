@@ -355,7 +355,8 @@ __device__ __forceinline__ void load_part(const EmbedBwd<T>& a, int64_t slot, ui
 
 // A run that begins in a chunk and leaves it: the chunk's part and those of the chunks that it comes into. A CTA per run and
 // slab of columns; its parties take equal shares of the run's chunks, each with JOIN parts on their way at once, and
-// their sums are added in order: 16384 x 4096, whose most frequent id has 960 tokens, 18 us, 4096 x 1024 8. (The list's order is that of the sums' CTAs: it decides who does what, and no sum.)
+// their sums are added in order: 16384 x 4096, whose most frequent id has 960 tokens, 18 us, 4096 x 1024 8. (The list's
+// order is that of the sums' CTAs: it decides who does what, and no sum.)
 constexpr int JOIN = 8;
 template <typename T, int N>
 __global__ void __launch_bounds__(PARTY) embed_join_kernel(const EmbedBwd<T> a) {
@@ -447,7 +448,7 @@ cudaError_t sums(EmbedBwd<T> a, int32_t d, cudaStream_t s) {
 }  // namespace
 
 size_t embed_workspace_bytes(int64_t T, int32_t d, int32_t V) {
-    return 2 * up((size_t)T * 8)+ up((size_t)(chunks_of(T, d) + 1) * 4) + up((size_t)chunks_of(T, d) * 2 * (size_t)d * 4);
+    return 2 * up((size_t)T * 8) + up((size_t)(chunks_of(T, d) + 1) * 4) + up((size_t)chunks_of(T, d) * 2 * (size_t)d * 4);
 }
 
 cudaError_t launch_embed_fwd(const int32_t* ids, int64_t T, int32_t d, int32_t V, bool bf16, const void* w, float scale, void* out,

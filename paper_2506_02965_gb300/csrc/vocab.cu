@@ -128,7 +128,11 @@ template <bool LAST> struct OutEpi : Plain {
 // ---------------------------------------------------------------- passes
 __device__ __forceinline__ bool has_target(int y, int V) { return y >= 0 && y < V; }
 
-// scal[0] = the largest |weight| of a token with a target, or 1 / (tokens with a target); scal[1] = 1 / scal[0] or 0.
+// scal[0] = the largest |weight| of a token with a target, or 1 / (tokens with a target); scal[1] = 1 / scal[0]. Weights that
+// are all 0, too small for that or not finite are taken as they are.
+__device__ __forceinline__ float scale_of(bool weighted, float most, int n) {
+    return !weighted ? 1.f / (float)max(n, 1) : most > 1e-30f && most < 1e30f ? most : 1.f;
+}
 // One CTA of whole warps, up to 32.
 __device__ __forceinline__ void weights_scale(const int32_t* target, const float* weight, int64_t T, int V, float* scal) {
     __shared__ float s_max[32];
@@ -156,10 +160,9 @@ __device__ __forceinline__ void weights_scale(const int32_t* target, const float
         most = warp_max(lane < warps ? s_max[lane] : 0.f);
         n = __reduce_add_sync(0xffffffffu, lane < warps ? s_n[lane] : 0);
         if (lane == 0) {
-            // (weights with an infinity or a NaN are taken as they are)
-            const float a = weight ? (most < 3.4e38f ? most : 1.f) : 1.f / (float)max(n, 1);
+            const float a = scale_of(weight, most, n);
             scal[0] = a;
-            scal[1] = a > 0.f ? 1.f / a : 0.f;
+            scal[1] = 1.f / a;
         }
     }
     __syncthreads();
@@ -283,14 +286,14 @@ template <bool BF16> __global__ void __launch_bounds__(1024) vocab_join_kernel(c
         float u = a.all_weight && live ? a.all_weight[lane] : 0.f;
         const int n = __popc(__ballot_sync(0xffffffffu, live));
         const float most = warp_max(u == u ? fabsf(u) : INFINITY);
-        const float scale = a.all_weight ? (most < 3.4e38f ? most : 1.f) : 1.f / (float)max(n, 1);
+        const float scale = scale_of(a.all_weight, most, n);
         if (!a.all_weight) u = scale;
         double sum = live ? (double)a.token[lane] * u : 0.0;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (lane == 0) {
             a.scal[0] = scale;
-            a.scal[1] = scale > 0.f ? 1.f / scale : 0.f;
+            a.scal[1] = 1.f / scale;
             *a.loss = (float)sum;
         }
     }
@@ -384,8 +387,9 @@ __global__ void __launch_bounds__(256) vocab_sum_kernel(const float* __restrict_
 __global__ void __launch_bounds__(256) vocab_col_kernel(const float* __restrict__ z, int V, int n, float2* __restrict__ part, int shares) {
     pdl_begin();
     __shared__ float2 s_part[8][33];
-    const int c = (int)blockIdx.x * 32 + (threadIdx.x & 31), lane = threadIdx.x & 31, r = threadIdx.x >> 5;
-    const int v0 = (int)blockIdx.y * kColChunk, v1 = min(V, v0 + kColChunk);
+    const int share = (int)(blockIdx.x % (unsigned)shares);
+    const int c = (int)(blockIdx.x / (unsigned)shares) * 32 + (threadIdx.x & 31), lane = threadIdx.x & 31, r = threadIdx.x >> 5;
+    const int v0 = share * kColChunk, v1 = min(V, v0 + kColChunk);
     float m = kNegInf, s = 0.f;
     if (c < n) {
         for (int v = v0 + r; v < v1; v += 8) m = fmaxf(m, z[(int64_t)v * n + c]);
@@ -399,7 +403,7 @@ __global__ void __launch_bounds__(256) vocab_col_kernel(const float* __restrict_
         const float ref = m == kNegInf ? 0.f : m;
         s = 0.f;
         for (int k = 0; k < 8; ++k) s += s_part[k][lane].y * expf(s_part[k][lane].x == kNegInf ? kNegInf : s_part[k][lane].x - ref);
-        part[(int64_t)c * shares + blockIdx.y] = make_float2(m, s);
+        part[(int64_t)c * shares + share] = make_float2(m, s);
     }
 }
 __global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z, int V, int n, const float* __restrict__ lse,
@@ -446,8 +450,8 @@ struct Plan {
     size_t scal, token, lse, zy, part, e, live, sums, dwsum, offsets, total;
 };
 
-// products with 32 rows of A (dense_tc.cuh: AR)
-bool short_a(bool pair, int64_t rows) { return !pair && rows <= 32; }
+// Products with 32 rows of A (dense_tc.cuh: AR): by the plan's tokens at once, so that a short last piece is laid out as the others.
+bool short_a(const Shape& s, int64_t rows) { return !s.pair && rows <= 32; }
 
 Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
     Plan p{};
@@ -466,7 +470,7 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
         p.dw = pick_shape(V, d, p.rows, p.pieces == 1 ? kMaxSplits : 1);
         p.ew = d < 1024 ? 8 : 4;  // a short contraction: the epilogue, not the product, sets a tile's time
         p.tn = p.logits.pair ? 256 : 128;
-        if (short_a(p.logits.pair, p.rows)) {
+        if (short_a(p.logits, p.rows)) {
             // few tokens stream W: the width by which the rounds of tiles come out fullest (65536: 112 columns, four rounds of
             // 147 tiles; of 128 columns four of 128). Whole staging boxes where the exponentials are stored.
             p.ew = 4;
@@ -531,7 +535,7 @@ cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, c
         if (pl.ew == 8) return launch_as<false, false, true, false, 8>(a, b, o, p, e, s);
         return launch_as<false, false, true, false, 4>(a, b, o, p, e, s);
     }
-    if (short_a(pl.logits.pair, p.M)) {
+    if (short_a(pl.logits, pl.rows)) {
         Problem q = p;
         q.tn = pl.tn;
         return launch_as<false, false, false, false, 4, 32>(a, b, o, q, e, s);
@@ -540,7 +544,7 @@ cudaError_t logits(const Plan& pl, const CUtensorMap& a, const CUtensorMap& b, c
     return launch_as<false, false, false, false, 4>(a, b, o, p, e, s);
 }
 template <bool A_MN, typename Epi>
-cudaError_t product(bool pair, int ew, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const Epi& e,
+cudaError_t product(bool pair, bool few_rows, int ew, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const Problem& p, const Epi& e,
                     cudaStream_t s) {
     if constexpr (A_MN) {
         if (ew == 8) {
@@ -548,7 +552,7 @@ cudaError_t product(bool pair, int ew, const CUtensorMap& a, const CUtensorMap& 
             return launch_as<A_MN, true, false, false, 8>(a, b, o, p, e, s);
         }
     } else {
-        if (short_a(pair, p.M)) return launch_as<A_MN, true, false, false, 4, 32>(a, b, o, p, e, s);
+        if (few_rows) return launch_as<A_MN, true, false, false, 4, 32>(a, b, o, p, e, s);
     }
     if (pair) return launch_as<A_MN, true, true, false, 4>(a, b, o, p, e, s);
     return launch_as<A_MN, true, false, false, 4>(a, b, o, p, e, s);
@@ -610,8 +614,8 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     const __nv_bfloat16* h = (const __nv_bfloat16*)a.h + t0 * d;
     float* scal = (float*)(ws + pl.scal);
     CUtensorMap mh, mw, ml, me;  // (ml: W for the logits)
-    if (!make_map3(&mh, h, d, n, d, 1, 0, false, short_a(pl.logits.pair, n) ? 32 : 128) || !make_map3(&mw, a.w, d, V, d, 1, 0, false) ||
-        !make_map3(&ml, a.w, d, V, d, 1, 0, false, short_a(pl.logits.pair, n) ? pl.tn : 128))
+    if (!make_map3(&mh, h, d, n, d, 1, 0, false, short_a(pl.logits, pl.rows) ? 32 : 128) || !make_map3(&mw, a.w, d, V, d, 1, 0, false) ||
+        !make_map3(&ml, a.w, d, V, d, 1, 0, false, short_a(pl.logits, pl.rows) ? pl.tn : 128))
         return cudaErrorInvalidValue;
     Problem p = problem((int)n, V, d);
     if (a.dh) {
@@ -634,16 +638,16 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     }
     CUtensorMap ma, mb, mo;
     // dh = dz W: the vocabulary inside dz's rows, outside W's
-    if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false, short_a(pl.dh.pair, n) ? 32 : 128)) return cudaErrorInvalidValue;
+    if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false, short_a(pl.dh, pl.rows) ? 32 : 128)) return cudaErrorInvalidValue;
     if (!make_map3(&mo, (__nv_bfloat16*)a.dh + t0 * d, d, n, d, 1, 0, true)) return cudaErrorInvalidValue;
     p = problem((int)n, d, V);
     split_k(p, pl.dh.splits);
     float* sums = (float*)(ws + pl.sums);
     if (p.splits > 1) {
-        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, SumEpi<false>{sums}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, short_a(pl.dh, pl.rows), 4, ma, mw, mo, p, SumEpi<false>{sums}, s)));
         MOE_TRY(sum_splits(sums, p.splits, n * d, scal, true, (__nv_bfloat16*)a.dh + t0 * d, s));
     } else {
-        MOE_TRY((product<false>(pl.dh.pair, 4, ma, mw, mo, p, OutEpi<false>{{}, scal, nullptr}, s)));
+        MOE_TRY((product<false>(pl.dh.pair, short_a(pl.dh, pl.rows), 4, ma, mw, mo, p, OutEpi<false>{{}, scal, nullptr}, s)));
     }
     // dW = dz^T h: the tokens outside both
     if (!make_map3(&ma, ws + pl.e, V, n, pl.ld, 1, 0, false) || !make_map3(&mb, ws + pl.live, d, n, d, 1, 0, false) ||
@@ -652,13 +656,13 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
     float* acc = (float*)(ws + pl.dwsum);
     if (pl.pieces == 1 && pl.dw.splits > 1) {
         split_k(p, pl.dw.splits);
-        MOE_TRY((product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, SumEpi<false>{sums}, s)));
+        MOE_TRY((product<true>(pl.dw.pair, false, pl.dw_ew, ma, mb, mo, p, SumEpi<false>{sums}, s)));
         return sum_splits(sums, p.splits, (int64_t)V * d, scal, true, a.dw, s);
     }
-    if (pl.pieces == 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<false>{{}, scal, nullptr}, s);
-    if (piece == 0) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, SumEpi<false>{acc}, s);
-    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, SumEpi<true>{acc}, s);
-    return product<true>(pl.dw.pair, pl.dw_ew, ma, mb, mo, p, OutEpi<true>{{}, scal, acc}, s);
+    if (pl.pieces == 1) return product<true>(pl.dw.pair, false, pl.dw_ew, ma, mb, mo, p, OutEpi<false>{{}, scal, nullptr}, s);
+    if (piece == 0) return product<true>(pl.dw.pair, false, pl.dw_ew, ma, mb, mo, p, SumEpi<false>{acc}, s);
+    if (piece < pl.pieces - 1) return product<true>(pl.dw.pair, false, pl.dw_ew, ma, mb, mo, p, SumEpi<true>{acc}, s);
+    return product<true>(pl.dw.pair, false, pl.dw_ew, ma, mb, mo, p, OutEpi<true>{{}, scal, acc}, s);
 }
 
 cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, cudaStream_t s) {
@@ -678,7 +682,7 @@ cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, c
     m.epi = EPI_STORE;
     m.out0 = zt;
     MOE_TRY(launch_gemm_m(m, false, s));
-    (void)launch_pdl(vocab_col_kernel, dim3((unsigned)ceil_div(n, 32), (unsigned)pl.shares), dim3(256), 0, s, (const float*)zt, V, (int)n,
+    (void)launch_pdl(vocab_col_kernel, dim3((unsigned)(ceil_div(n, 32) * pl.shares)), dim3(256), 0, s, (const float*)zt, V, (int)n,
                      (float2*)(ws + pl.part), pl.shares);
     MOE_TRY(cudaGetLastError());
     MOE_TRY(join(pl, a, ws, piece, t0, n, zt, s));

@@ -168,6 +168,40 @@ def test_peaked_and_flat_rows(kind):
     check(run(h, w, y, None, kind), h, w, y, None, kind)
 
 
+@pytest.mark.parametrize("size", [1e-42, 1e-36, 1e34])
+@pytest.mark.parametrize("T", [20, 300])
+def test_weights_of_any_size(size, T):
+    h, w, y, u = make(T, 128, 300, "bf16", 13)
+    y[::5] = -1
+    u = u * size
+    r = run(h, w, y, u, "bf16")
+    if size > 1:
+        check(r, h, w, y, u, "bf16")
+    else:  # below bf16's normal numbers a step is 2^-133 (and 2^-149 in fp32): next to that, the sums of as many terms
+        live = (y >= 0).double()
+        p = torch.softmax(h.double() @ w.double().T, 1)
+        dz = (u.double() * live)[:, None] * (p - torch.zeros_like(p).scatter_(1, y.long().clamp(min=0)[:, None], 1.0))
+        for got, ref, n in ((r.dh, dz @ w.double(), 300), (r.dw, dz.T @ h.double(), T)):
+            mag = 2.0 ** -133 * n * 40 + ref.abs().max() * 2.0 ** -6
+            assert torch.isfinite(got).all() and ((got.double() - ref).abs() <= mag).all()
+
+
+@pytest.mark.slow
+def test_a_last_piece_of_one_token():
+    """Pieces of 4096 tokens and one of a single token, with gradients."""
+    T, d, V = 17 * 4096 + 1, 128, 65600
+    h, w, y, _ = make(T, d, V, "bf16", 15)
+    r = run(h, w, y, None, "bf16")
+    z = h[-1].double() @ w.double().T
+    lse = torch.logsumexp(z, 0)
+    assert abs(r.token[-1].item() - (lse - z[y[-1].long()]).item()) <= 1e-4
+    dz = torch.exp(z - lse)
+    dz[y[-1].long()] -= 1
+    ref = dz @ w.double() / T
+    assert (r.dh[-1].double() - ref).norm() <= 1e-2 * ref.norm()
+    assert torch.isfinite(r.dw).all() and torch.isfinite(r.dh).all()
+
+
 def test_targets_out_of_range_are_recorded():
     h, w, y, _ = make(50, 128, 300, "bf16", 6)
     y[7], y[9] = 300, 2 ** 31 - 1

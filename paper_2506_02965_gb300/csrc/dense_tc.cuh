@@ -47,6 +47,7 @@ struct Problem {
     int splits;     // of the contraction, each of `per_split` stages (the last may have fewer)
     int per_split;
     int tri;        // tiles on and below the diagonal only (M == N)
+    int tail;       // tiles in flight at once, if a last round of few is cut into parts (see Tail; splits == 1); else 0
     int band;       // tile order: bands of this many rows of tiles
     int tn;         // AR = 32: a tile's columns, a multiple of 16 up to 128
     const int32_t* counts;  // [G]: matrices with counts <= 0 are left out; null: none
@@ -58,7 +59,44 @@ struct Tile {
     int m0, n0;    // of this CTA's accumulator rows, and of the tile's columns
     int kb0, kb1;  // stages
     bool diag;     // (tri) a tile that the diagonal crosses
+    int part;      // of a cut tile, counted over all of them; -1: a whole one
 };
+
+// The last round of tiles: `rest` of them behind `whole`, each in `parts` parts of `each` stages (1: not cut), so that
+// as many parts as there are places fill it. Sums of the parts are left to another launch.
+struct Tail {
+    int whole, rest, parts, each;
+};
+__host__ __device__ __forceinline__ Tail tail_of(int tiles, int places, int stages) {
+    Tail t{tiles, 0, 1, stages};
+    const int rest = places ? tiles % places : 0;
+    if (rest == 0 || places / rest < 2 || stages < 2) return t;
+    t.each = (stages + places / rest - 1) / (places / rest);
+    t.parts = (stages + t.each - 1) / t.each;
+    t.rest = rest;
+    t.whole = tiles - rest;
+    return t;
+}
+// The matrices that take part, in order; by a warp. Returns how many.
+__device__ __forceinline__ int called_groups(const int32_t* counts, int G, unsigned char* list) {
+    const int lane = threadIdx.x & 31;
+    int run = 0;
+    for (int g0 = 0; g0 < G; g0 += 32) {
+        const int g = g0 + lane;
+        const bool in = g < G && (!counts || counts[g] > 0);
+        const uint32_t m = __ballot_sync(0xffffffffu, in);
+        if (in) list[run + __popc(m & ((1u << lane) - 1))] = (unsigned char)g;
+        run += __popc(m);
+    }
+    return run;
+}
+// Row and column of tiles of the i-th tile on and below the diagonal
+__device__ __forceinline__ int2 lower_tile(int i) {
+    int m = (int)((sqrtf(8.f * (float)i + 1.f) - 1.f) * 0.5f);
+    while (m * (m + 1) / 2 > i) --m;
+    while ((m + 1) * (m + 2) / 2 <= i) ++m;
+    return make_int2(m, i - m * (m + 1) / 2);
+}
 
 // What an epilogue gets besides its tile: this warp's TMEM address, its lane quarter, the share of the columns
 // [c0, c1) that it drains, and its staging boxes.
@@ -84,6 +122,7 @@ __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t sr
 }
 // An epilogue that reads nothing beside the product.
 struct Plain {
+    static constexpr bool CUT = false;  // takes parts of cut tiles (see Tail)
     template <int CHUNKS> struct Held {};
     template <int NBUF, typename H> __device__ __forceinline__ void fetch(H&, const Problem&, const Tile&, Warp&) const {}
 };
@@ -98,6 +137,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 
 // A product's fp32 sums, [splits][G][M][N] (N a multiple of 4), stored or (ADD) added to what is there.
 template <bool ADD> struct SumEpi {
+    static constexpr bool CUT = false;
     template <int CHUNKS> struct Held {};
     template <int NBUF, typename H> __device__ __forceinline__ void fetch(H&, const Problem&, const Tile&, Warp&) const {}
     float* sums;
@@ -173,7 +213,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort_flag = &s_abort;
     const uint32_t rank = PAIR ? cluster_rank() : 0u;
-    const int64_t tile0 = (int64_t)blockIdx.x / NPAIR, tile_step = (int64_t)gridDim.x / NPAIR;
+    const int tile0 = (int)blockIdx.x / NPAIR, tile_step = (int)gridDim.x / NPAIR;
 
     // 1024-byte aligned ring, the staging boxes behind it
     const uint32_t raw_u32 = smem_u32(smem_raw);
@@ -232,14 +272,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 0) {  // the matrices that take part
-        int run = 0;
-        for (int g0 = 0; g0 < p.G; g0 += 32) {
-            const int g = g0 + lane;
-            const bool in = g < p.G && (!p.counts || p.counts[g] > 0);
-            const uint32_t m = __ballot_sync(0xffffffffu, in);
-            if (in) s_group[run + __popc(m & ((1u << lane) - 1))] = (unsigned char)g;
-            run += __popc(m);
-        }
+        const int run = called_groups(p.counts, p.G, s_group);
         if (lane == 0) s_active = run;
     }
     fence_before();
@@ -248,26 +281,34 @@ __global__ void __launch_bounds__(threads(EW), 1)
     fence_after();
     const int tn = AR == 32 ? p.tn : TN;  // a tile's columns
     const int mt = (p.M + TM - 1) / TM, nt = (p.N + tn - 1) / tn;
-    const int64_t per = p.tri ? (int64_t)mt * (mt + 1) / 2 : (int64_t)mt * nt;
-    const int64_t total = (int64_t)s_active * p.splits * per;
+    const int per = p.tri ? mt * (mt + 1) / 2 : mt * nt;
     const int stages = (p.K + KST - 1) / KST;
+    Tail tail{s_active * p.splits * per, 0, 1, stages};
+    if constexpr (Epi::CUT) tail = tail_of(tail.whole, p.tail, stages);
+    const int total = tail.whole + tail.rest * tail.parts;
 
-    auto tile_at = [&](int64_t t) -> Tile {
+    auto tile_at = [&](int t) -> Tile {
         Tile ti;
-        const int64_t gs = t / per;
-        const int64_t local = t - gs * per;
+        ti.part = -1;
+        int k = 0;
+        if (Epi::CUT && t >= tail.whole) {
+            ti.part = t - tail.whole;
+            k = ti.part % tail.parts;
+            t = tail.whole + ti.part / tail.parts;
+        }
+        const int gs = t / per;
+        const int local = t - gs * per;
         ti.g = s_group[gs / p.splits];
-        ti.split = (int)(gs % p.splits);
+        ti.split = gs % p.splits;
         int m, n;
         if (p.tri) {
-            m = (int)((sqrtf(8.f * (float)local + 1.f) - 1.f) * 0.5f);
-            while ((int64_t)m * (m + 1) / 2 > local) --m;
-            while ((int64_t)(m + 1) * (m + 2) / 2 <= local) ++m;
-            n = (int)(local - (int64_t)m * (m + 1) / 2);
+            const int2 mn = lower_tile(local);
+            m = mn.x;
+            n = mn.y;
         } else {  // bands of p.band rows of tiles, swept along N, a band's rows innermost
-            const int64_t b = local / ((int64_t)p.band * nt);
-            const int first = (int)b * p.band, rows = min(p.band, mt - first);
-            const int rem = (int)(local - b * p.band * nt);
+            const int b = local / (p.band * nt);
+            const int first = b * p.band, rows = min(p.band, mt - first);
+            const int rem = local - first * nt;
             m = first + rem % rows;
             n = rem / rows;
         }
@@ -276,6 +317,10 @@ __global__ void __launch_bounds__(threads(EW), 1)
         ti.n0 = n * tn;
         ti.kb0 = ti.split * p.per_split;
         ti.kb1 = min(stages, ti.kb0 + p.per_split);
+        if (Epi::CUT && ti.part >= 0) {
+            ti.kb0 = k * tail.each;
+            ti.kb1 = min(stages, ti.kb0 + tail.each);
+        }
         return ti;
     };
 
@@ -299,7 +344,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
                 if constexpr (PAIR) tma_load_3d_pair(dst, map, fb, c0, c1, c2);
                 else tma_load_3d(dst, map, fb, c0, c1, c2);
             };
-            for (int64_t t = tile0; t < total && ok; t += tile_step) {
+            for (int t = tile0; t < total && ok; t += tile_step) {
                 const Tile ti = tile_at(t);
                 const int n0 = ti.n0 + (int)rank * 128;
                 for (int kb = ti.kb0; kb < ti.kb1; ++kb) {
@@ -340,7 +385,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
         uint32_t phase = 0, acc_phase = 0;
         bool issued = false;
         const uint32_t idesc = AR == 32 ? (IDESC & ~(63u << 17)) | (uint32_t)(tn >> 3) << 17 : IDESC;
-        for (int64_t t = tile0; t < total && rank == 0; t += tile_step) {
+        for (int t = tile0; t < total && rank == 0; t += tile_step) {
             const Tile ti = tile_at(t);
             bool ok = warp_wait(tempty_bar(acc), acc_phase ^ 1u);
             if (!ok) break;
@@ -404,7 +449,7 @@ __global__ void __launch_bounds__(threads(EW), 1)
         w.seq = 0;
         int acc = 0;
         uint32_t acc_phase = 0;
-        for (int64_t t = tile0; t < total; t += tile_step) {
+        for (int t = tile0; t < total; t += tile_step) {
             const Tile ti = tile_at(t);
             typename Epi::template Held<TN / SPLIT / 32> held;  // what the epilogue reads, on its way during the product
             epi.template fetch<NBUF>(held, p, ti, w);
@@ -473,6 +518,7 @@ static cudaError_t launch_as(const CUtensorMap& a, const CUtensorMap& b, const C
     const int64_t mt = (p.M + TM - 1) / TM, nt = (p.N + p.tn - 1) / p.tn;
     const int64_t tiles = (int64_t)p.G * p.splits * (p.tri ? mt * (mt + 1) / 2 : mt * nt);
     if (tiles <= 0) return cudaSuccess;
+    if (tiles > 0x7fffff00) return cudaErrorInvalidValue;  // (terabytes)
     int most = sm_count();
     if constexpr (PAIR) {  // clusters that fit at once
         static std::atomic<int> resident[kMaxDevices] = {};
@@ -496,7 +542,7 @@ static cudaError_t launch_as(const CUtensorMap& a, const CUtensorMap& b, const C
             if (dev >= 0 && dev < kMaxDevices) resident[dev] = most;
         }
     }
-    const int at_once = (int)std::min<int64_t>(tiles, most);
+    const int at_once = (int)std::min<int64_t>(p.tail ? std::max<int64_t>(tiles, p.tail) : tiles, most);
     // Tile order: where one operand of a matrix fits the L2 beside what streams past it, the other is read once;
     // else bands of about the square root of the tiles in flight, which read the fewest blocks per round.
     constexpr int64_t kResident = 48ll << 20;

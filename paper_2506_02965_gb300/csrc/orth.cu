@@ -314,14 +314,29 @@ template <int CHUNKS> struct Ahead {
 };
 __device__ __forceinline__ float2 two_halves(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 
+// The mirror image of 32 columns, from n on, of this lane's row m (two columns a word): of columns j, j + 1 the even lanes
+// write rows (m, m + 1) of column j, the odd ones those of column j + 1.
+__device__ __forceinline__ void store_mirror(const uint32_t (&u)[16], int lane, int m, int n, int M, __half* out, int64_t ld) {
+    __half* to = out + (n + (lane & 1)) * ld + (m & ~1);
+    const int rows = (m & ~1) < M ? M - n - (lane & 1) : 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i, to += 2 * ld) {
+        const uint32_t mine = u[i], other = __shfl_xor_sync(0xffffffffu, mine, 1);
+        const uint32_t pair = (lane & 1) ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
+        if (2 * i < rows) *reinterpret_cast<uint32_t*>(to) = pair;
+    }
+}
+
 // A symmetric product in fp16, its lower tiles and their mirror images. 16 of 1024 x 1024: A over 5632 terms 96 us (160 tiles in
 // three rounds of 76 pairs), its square 29; two of 4096 x 4096 over 8192 terms 175, 1.67 PFLOP/s of what is computed.
-struct SymEpi {
+template <bool CUT_> struct SymEpi {
+    static constexpr bool CUT = CUT_;
     Term c;
     float alpha;
     __half* out;
     int64_t ld, group;
     float shift;  // added to the diagonal
+    float* parts; // sums of a cut tile's parts, by 32 x 32 chunks as they come from TMEM: [part][chunk][4 columns][row]
 
     template <int CHUNKS> using Held = Ahead<CHUNKS>;
     template <int NBUF, int CHUNKS>
@@ -331,6 +346,19 @@ struct SymEpi {
     template <int NBUF, int CHUNKS>
     __device__ __forceinline__ void run(const Ahead<CHUNKS>& held, const Problem& p, const Tile& ti, Warp& w, const CUtensorMap* map) const {
         const int row0 = ti.m0 + w.q * 32, m = row0 + w.lane;
+        if (CUT && ti.part >= 0) {
+            const int across = p.tn / 32;  // (a tile is a square)
+            const int64_t rows = (ti.m0 % p.tn) / 32 + w.q;
+#pragma unroll 1
+            for (int k = w.c0; k < w.c1; k += 32) {
+                float v[32];
+                tmem_ld32(w.tmem + k, v);
+                float4* to = reinterpret_cast<float4*>(parts + ((ti.part * across + rows) * across + k / 32) * 1024) + w.lane;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to[32 * i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+            return;
+        }
 #pragma unroll
         for (int chunk = 0; chunk < CHUNKS; ++chunk) {
             const int k = w.c0 + 32 * chunk;
@@ -358,16 +386,7 @@ struct SymEpi {
             for (int i = 0; i < 16; ++i) u[i] = pack_half(v[2 * i], v[2 * i + 1]);
             store_box<NBUF>(w, map, u, ti.n0 + k, row0, ti.g);
             if (!ti.diag) {
-                // rows of the mirror image: of two columns j, j + 1 the even lanes write rows (m, m + 1) of column j,
-                // the odd ones those of column j + 1
-                __half* to = out + ti.g * group + (int64_t)(ti.n0 + k) * ld + (m & ~1);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const uint32_t mine = u[i], other = __shfl_xor_sync(0xffffffffu, mine, 1);
-                    const uint32_t pair = (w.lane & 1) ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
-                    const int col = 2 * i + (w.lane & 1);
-                    if ((m & ~1) < p.M && ti.n0 + k + col < p.N) *reinterpret_cast<uint32_t*>(to + (int64_t)col * ld) = pair;
-                }
+                store_mirror(u, w.lane, m, ti.n0 + k, p.M, out + ti.g * group, ld);
             }
         }
     }
@@ -376,6 +395,7 @@ struct SymEpi {
 // X' = alpha acc + beta X in fp16 with its residual; (LAST) in the matrix's own type, times a scale. 16 x 5632 x 1024 140 us (1.35
 // PFLOP/s, 4.1 TB/s of DRAM), 2 x 4096 x 8192 312 (1.76 PFLOP/s).
 template <bool LAST> struct StepEpi {
+    static constexpr bool CUT = false;
     Term c;
     const uint8_t* lo_in;
     float alpha;
@@ -468,6 +488,53 @@ template <bool LAST> struct StepEpi {
     }
 };
 
+// A's cut tiles from their parts (dense_tc.cuh: Tail), in order, and their mirror images; a warp a chunk of 32 x 32.
+__global__ void __launch_bounds__(128) orth_tail_kernel(const float* __restrict__ sums, const Problem p, float alpha, __half* __restrict__ out,
+                                                        int64_t ld, int64_t group) {
+    pdl_begin();
+    __shared__ unsigned char s_group[MAX_GROUPS];
+    __shared__ int s_active;
+    if (threadIdx.x < 32) {
+        const int run = called_groups(p.counts, p.G, s_group);
+        if (threadIdx.x == 0) s_active = run;
+    }
+    __syncthreads();
+    const int mt = (p.M + p.tn - 1) / p.tn, across = p.tn / 32;
+    const int per = mt * (mt + 1) / 2;
+    const Tail tail = tail_of(s_active * per, p.tail, (p.K + KST - 1) / KST);
+    const int lane = threadIdx.x & 31, chunks = across * across;
+    const int tile = (int)blockIdx.x * 4 / chunks, chunk = (int)blockIdx.x * 4 % chunks + (threadIdx.x >> 5);
+    if (tile >= tail.rest) return;
+    const int t = tail.whole + tile, gs = t / per;
+    const int2 mn = lower_tile(t - gs * per);
+    const int row0 = mn.x * p.tn + chunk / across * 32, n = mn.y * p.tn + chunk % across * 32;
+    if (row0 >= p.M || n >= p.N) return;
+    const float4* from = reinterpret_cast<const float4*>(sums + ((int64_t)tile * tail.parts * chunks + chunk) * 1024) + lane;
+    float v[32] = {};
+#pragma unroll 2
+    for (int k = 0; k < tail.parts; ++k, from += (int64_t)chunks * 256) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 x = from[32 * i];
+            v[4 * i] += x.x;
+            v[4 * i + 1] += x.y;
+            v[4 * i + 2] += x.z;
+            v[4 * i + 3] += x.w;
+        }
+    }
+    uint32_t u[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) u[i] = pack_half(v[2 * i] * alpha, v[2 * i + 1] * alpha);
+    const int m = row0 + lane;
+    __half* to = out + s_group[gs] * group;
+    if (m < p.M) {  // (rows of A hold whole 64s of columns)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint4*>(to + m * ld + n + 8 * i) = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+    }
+    if (mn.x != mn.y) store_mirror(u, lane, m, n, p.M, to, ld);
+}
+
 // A in fp16 from its parts' sums, in order: [splits][G][n][width] -> rows of ld. A block row of 64 columns by 4 rows.
 __global__ void __launch_bounds__(256) orth_square_kernel(const float* __restrict__ sums, int splits, int n, int ld, int width, float alpha,
                                                           __half* __restrict__ out, const int32_t* __restrict__ counts) {
@@ -529,21 +596,39 @@ struct Plan {
     int row_boxes, col_boxes;  // of X's residuals
     int parts;          // CTAs per matrix of the first passes
     Shape gram;              // bf16: tiles and parts of A's product
+    int tail;                // its last round of tiles in parts (dense_tc.cuh: Tail), or 0
     int splits, split_rows;  // fp32: parts of X^T X's contraction
     size_t part, offsets, sums, x[2], lo[2], a, b, total;
 };
 
-// A's product: the lower tiles in one, or (few tiles, a long side) all tiles in parts, whose sums a pass adds up.
-Shape pick_gram(int64_t G, int64_t n, int64_t m) {
-    const Shape whole = pick_shape(n, n, m, 1, G, true);
+// A's product: the lower tiles, whole or those of the last round in parts, which a pass adds up, or (few tiles, a long side)
+// all tiles in parts. In units of a pair's stage as pick_shape; the pass is 12 of them.
+Shape pick_gram(int64_t G, int64_t n, int64_t m, int* tail) {
+    const int stages = (int)ceil_div(m, KST);
     const Shape parts = pick_shape(n, ceil_div(n, 4) * 4, m, 64, G, false);
-    const double stages = (double)ceil_div(m, KST);
-    auto time = [&](const Shape& s, bool tri) {
-        const int64_t t = s.pair ? 256 : 128, mt = ceil_div(n, t), tiles = G * (tri ? mt * (mt + 1) / 2 : mt * mt) * s.splits;
-        return (double)ceil_div(tiles, s.pair ? kPairs : 2 * kPairs) * (stages / s.splits + 2) * (s.pair ? 1.0 : 0.92) +
-               (s.splits > 1 ? 8 + (double)s.splits * G * n * n * 8 / (6.5e6 * 0.7) : 0);
+    Shape best{true, 1};
+    double least = 0;
+    auto take = [&](const Shape& s, int places, double cost) {
+        if (least != 0 && cost >= least) return;
+        least = cost;
+        best = s;
+        *tail = places;
     };
-    return parts.splits > 1 && time(parts, false) < time(whole, true) ? parts : Shape{whole.pair, 1};
+    for (int pair = 1; pair >= 0; --pair) {
+        const int places = pair ? kPairs : 2 * kPairs;
+        const int64_t mt = ceil_div(n, pair ? 256 : 128), tiles = std::min<int64_t>(G * mt * (mt + 1) / 2, 0x7fffffff);
+        const double each = pair ? 1.0 : 0.92;
+        take({pair != 0, 1}, 0, (double)ceil_div(tiles, places) * (stages + 2) * each);
+        const Tail t = tail_of((int)tiles, places, stages);
+        if (t.rest) take({pair != 0, 1}, places, ((double)(t.whole / places) * (stages + 2) + t.each + 2) * each + 12);
+    }
+    if (parts.splits > 1) {
+        const int64_t mt = ceil_div(n, parts.pair ? 256 : 128);
+        take(parts, 0, (double)ceil_div(G * mt * mt * parts.splits, parts.pair ? kPairs : 2 * kPairs) *
+                           ((double)stages / parts.splits + 2) * (parts.pair ? 1.0 : 0.92) +
+                           8 + (double)parts.splits * G * n * n * 8 / (6.5e6 * 0.7));
+    }
+    return best;
 }
 
 Plan plan(int G, int rows, int cols, bool bf16) {
@@ -558,7 +643,7 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     p.splits = 1;
     const int m = std::max(rows, cols);
     if (bf16) {
-        p.gram = pick_gram(G, p.n, m);
+        p.gram = pick_gram(G, p.n, m, &p.tail);
     } else {
         const int64_t tiles = G * ceil_div(p.n, 128) * ceil_div(p.n, 128);
         int64_t sp = std::min<int64_t>(std::min<int64_t>(256 / G, 2 * kPairs / tiles), m / 128);  // one round of tiles
@@ -580,7 +665,8 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     for (int i = 0; i < 2; ++i) p.lo[i] = bf16 ? take((size_t)G * p.row_boxes * p.col_boxes * LO_BOX) : 0;
     p.a = take(as * es);
     p.b = take(as * es);
-    p.sums = take(p.splits > 1 ? as * 4 * p.splits : p.gram.splits > 1 ? (size_t)p.gram.splits * G * p.n * p.ldn * 4 : 0);
+    const size_t cut = p.tail ? (size_t)p.tail * (p.gram.pair ? 256 * 256 : 128 * 128) * 4 : 0;  // (a part a place at most)
+    p.sums = take(p.splits > 1 ? as * 4 * p.splits : p.gram.splits > 1 ? (size_t)p.gram.splits * G * p.n * p.ldn * 4 : cut);
     p.total = at;
     return p;
 }
@@ -616,6 +702,11 @@ cudaError_t product(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMa
     return launch_as<A_MN, B_MN, false, true, 8>(a, b, o, p, e, s);
 }
 
+template <bool TALL, bool CUT>
+cudaError_t launch_lower(bool pair, const CUtensorMap& x, const CUtensorMap& o, const Problem& p, const SymEpi<CUT>& e, cudaStream_t s) {
+    if (pair) return launch_as<TALL, TALL, true, true, 8>(x, x, o, p, e, s);
+    return launch_as<TALL, TALL, false, true, 8>(x, x, o, p, e, s);
+}
 template <bool TALL>
 cudaError_t launch_gram(bool pair, const CUtensorMap& x, const Problem& p, const SumEpi<false>& e, cudaStream_t s) {
     if (pair) return launch_as<TALL, TALL, true, true, 8>(x, x, x, p, e, s);
@@ -639,14 +730,17 @@ cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t
     Problem sq = problem(n, n, tall ? R : C, G), cube = problem(n, n, n, G), step = problem(R, C, n, G);
     sq.tri = cube.tri = 1;
     sq.counts = cube.counts = step.counts = o.counts;
-    Problem parts = sq;
+    Problem lower = sq, parts = sq;
+    lower.tail = pl.tail;
+    lower.tn = pl.gram.pair ? 256 : 128;
     parts.tri = 0;
     parts.N = (n + 3) / 4 * 4;  // (columns past n: products with zeros)
     split_k(parts, pl.gram.splits);
     for (int i = 0; i < o.steps; ++i) {
         const int x = i & 1, y = x ^ 1;
         const Term none{nullptr, 0, 0, 0.f};
-        const SymEpi ea{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag, 0.f};
+        const SymEpi<false> ea{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag, 0.f, nullptr};
+        const SymEpi<true> cut{none, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag, 0.f, (float*)(ws + pl.sums)};
         if (pl.gram.splits > 1) {
             const SumEpi<false> es{(float*)(ws + pl.sums)};
             if (tall) MOE_TRY((launch_gram<true>(pl.gram.pair, mx[x], parts, es, s)));
@@ -655,11 +749,18 @@ cudaError_t steps_half(const Plan& pl, const OrthArgs& o, char* ws, cudaStream_t
                              (const float*)(ws + pl.sums), parts.splits, n, (int)pl.ldn, parts.N, kScaleA / (kScaleX * kScaleX), A, o.counts);
             MOE_TRY(cudaGetLastError());
         } else {
-            if (tall) MOE_TRY((product<true, true>(mx[x], mx[x], sa, sq, ea, s)));
-            else MOE_TRY((product<false, false>(mx[x], mx[x], sa, sq, ea, s)));
+            // (whole tiles: by the kernel of the square, which is at hand in the instruction caches)
+            if (pl.tail) MOE_TRY((tall ? launch_lower<true>(pl.gram.pair, mx[x], sa, lower, cut, s) : launch_lower<false>(pl.gram.pair, mx[x], sa, lower, cut, s)));
+            else MOE_TRY((tall ? launch_lower<true>(pl.gram.pair, mx[x], sa, lower, ea, s) : launch_lower<false>(pl.gram.pair, mx[x], sa, lower, ea, s)));
+            if (pl.tail) {
+                const unsigned chunks = lower.tn * lower.tn / 1024;  // of a tile, four a CTA; half of the places' tiles at most
+                (void)launch_pdl(orth_tail_kernel, dim3((unsigned)pl.tail / 2 * chunks / 4), dim3(128), 0, s, (const float*)(ws + pl.sums),
+                                 lower, kScaleA / (kScaleX * kScaleX), A, pl.ldn, ag);
+                MOE_TRY(cudaGetLastError());
+            }
         }
         const float t = shift_of(i);
-        const SymEpi eb{{A, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag, t * kScaleA};
+        const SymEpi<false> eb{{A, pl.ldn, ag, kB}, kC / kScaleA, B, pl.ldn, ag, t * kScaleA, nullptr};
         MOE_TRY((product<false, false>(ma, ma, sb, cube, eb, s)));
         const Term cx{(const __half*)(ws + pl.x[x]), pl.ld, xg, kA - t};
         const uint8_t* lo = (const uint8_t*)(ws + pl.lo[x]);

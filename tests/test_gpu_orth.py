@@ -122,6 +122,18 @@ def test_large(G, R, C):
     check(out, mo, dw, mom, "bf16")
 
 
+@pytest.mark.parametrize("G,R,C,left", [(26, 300, 4000, 0), (26, 300, 4000, 1), (26, 4001, 301, 20), (13, 520, 4100, 0), (13, 4099, 519, 1), (13, 4099, 520, 12)])
+def test_a_last_round_in_parts(G, R, C, left):
+    """One tile or a few more than run at once (and, with matrices left out, about as many or a few in all)."""
+    dw, mom = make(G, R, C, "bf16", R)
+    counts = torch.ones(G, dtype=torch.int32, device="cuda")
+    counts[:left] = 0
+    out, mo = run(dw, mom, counts=counts)
+    check(out, mo, dw, mom, "bf16", counts=counts)
+    again, _ = run(dw, mom, counts=counts)
+    assert torch.equal(out, again) and L.moe_device_status() == 0
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("nesterov,beta,momentum,steps", [(0, 0.9, True, 5), (1, 0.0, True, 5), (0, 0.5, False, 5), (1, 0.95, True, 1), (1, 0.95, True, 2),
                                                            (1, 0.95, True, 8)])

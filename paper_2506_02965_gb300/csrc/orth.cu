@@ -327,8 +327,9 @@ __device__ __forceinline__ void store_mirror(const uint32_t (&u)[16], int lane, 
     }
 }
 
-// A symmetric product in fp16, its lower tiles and their mirror images. 16 of 1024 x 1024: A over 5632 terms 96 us (160 tiles in
-// three rounds of 76 pairs), its square 29; two of 4096 x 4096 over 8192 terms 175, 1.67 PFLOP/s of what is computed.
+// A symmetric product in fp16, its lower tiles and their mirror images. 16 of 1024 x 1024: A over 5632 terms 74 us and 9 for
+// the sums of its cut tiles (160 tiles are 2.1 rounds of 76 pairs: 95 us as three), its square 27.5; two of 4096 x 4096 over
+// 8192 terms 175, 1.67 PFLOP/s of what is computed.
 template <bool CUT_> struct SymEpi {
     static constexpr bool CUT = CUT_;
     Term c;
@@ -639,7 +640,9 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     p.row_boxes = (int)ceil_div(rows, 32);
     p.col_boxes = (int)ceil_div(cols, 32);
     const int64_t want = ceil_div((int64_t)rows * cols, 8 * 256);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(16 * kPairs, G)));
+    // (some 48 CTAs a SM: rows of odd lengths are read by single values, whose latency many CTAs hide best; 17 x 5518 x 831 1764 us
+    // with 8, 1691 with 16, 1657 with 48, 1664 with 96, whole lines alike)
+    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>(want, ceil_div(96 * kPairs, G)));
     p.splits = 1;
     const int m = std::max(rows, cols);
     if (bf16) {

@@ -489,7 +489,7 @@ moe_status moe_embed_bwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const
                          const void* dout, float scale, int accumulate, void* dw, void* workspace,
                          size_t workspace_bytes, moe_stream_t stream);
 
-/* Bytes of workspace for moe_vocab_loss; with_grads: with dh and dw. Host only. */
+/* Bytes of workspace for moe_vocab_loss; with_grads: with dh and dw. Host only. V as there. */
 moe_status moe_vocab_loss_workspace_size(int64_t T, int32_t d, int32_t V, moe_dtype dtype,
                                          int with_grads, size_t* bytes /* HOST out */);
 
@@ -504,7 +504,7 @@ moe_status moe_vocab_loss_workspace_size(int64_t T, int32_t d, int32_t V, moe_dt
  * is recorded as MOE_ERR_DEVICE_CHECK). With gradients the probabilities of a piece of the tokens are held at once: in
  * bf16 max(4096, 2d, 2^28 / V) tokens at most (2 V bytes each), in fp32 about 2^28 / V (4 V bytes each).
  * bf16: d a multiple of 128; dz is rounded to bf16 (relative to the largest |u_t|), sums are fp32. fp32: d % 4 == 0.
- * h, w, dh, dw, workspace 16-byte aligned. Deterministic.
+ * V up to 2^31 - 1 - 2^18 (MOE_ERR_UNSUPPORTED above). h, w, dh, dw, workspace 16-byte aligned. Deterministic.
  */
 moe_status moe_vocab_loss(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const void* h,
                           const void* w, const int32_t* target, const float* weight, float* loss,

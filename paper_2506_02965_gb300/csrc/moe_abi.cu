@@ -1169,6 +1169,8 @@ moe_status moe_embed_bwd(int64_t T, int32_t d, int32_t V, moe_dtype dtype, const
 static moe_status check_loss(int64_t T, int32_t d, int32_t V, moe_dtype dtype) {
     moe_status st = check_vocab(T, d, V, dtype);
     if (st) return st;
+    if (V > kVocabLossMax)
+        return fail(MOE_ERR_UNSUPPORTED, "V=%d > %d, the largest vocabulary whose loss this build computes", V, kVocabLossMax);
     if (dtype == MOE_BF16 && d % 128) return fail(MOE_ERR_INVALID_ARG, "bf16 needs d a multiple of 128 (got %d)", d);
     if (dtype == MOE_F32 && d % 4) return fail(MOE_ERR_INVALID_ARG, "fp32 needs d %% 4 == 0 (got %d)", d);
     return MOE_OK;

@@ -113,6 +113,9 @@ struct VocabArgs {
     void* dh;              // [T,d] or null (both gradients or neither)
     void* dw;              // [V,d]
 };
+// The largest vocabulary: the passes and the products count its rows in 32 bits, and step past the last one by a grid's rows (the
+// fp32 pass of dz 155648 at most: 16 * 152 blocks of 64) or a tile's.
+constexpr int32_t kVocabLossMax = INT32_MAX - (1 << 18);
 size_t vocab_workspace_bytes(int64_t T, int32_t d, int32_t V, bool bf16, bool grads);
 cudaError_t launch_vocab_loss(const VocabArgs& a, void* workspace, cudaStream_t s);
 cudaError_t vocab_status(cudaStream_t s, int* code);

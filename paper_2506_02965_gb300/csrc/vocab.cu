@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z
     const int y = target[t];
     const bool live = has_target(y, V);
     const float u = !live ? 0.f : weight ? weight[t] : scal[0], l = lse[t];
-    const int step = (int)(gridDim.x / tokens) * 64;
+    const int step = (int)(gridDim.x / tokens) * 64;  // (at most 2^18: see kVocabLossMax)
     for (int v0 = (int)(blockIdx.x / tokens) * 64 + (threadIdx.x >> 5); v0 < V; v0 += step) {
         float x[8];
 #pragma unroll

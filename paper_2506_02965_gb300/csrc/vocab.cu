@@ -1,13 +1,16 @@
 // Softmax cross entropy over a vocabulary, without keeping the logits, and its gradients.
 //   z = h W^T;  lse_t = log sum_v exp z_tv;  l_t = lse_t - z_t,y;  loss = sum_t u_t l_t
+// lse is never one number: with r the row's largest logit and s = sum_v exp(z - r), l = (r - z_y) + log s, and
+// softmax(z) = exp(z - r) / s. As one fp32 number it would round l and every probability to a step of its own size, 8e-6 at
+// 100: all of the loss, and of the gradient at the target, of a token that is as sure as that.
 //   dz_t = u_t (softmax(z_t) - onehot(y_t));  dh = dz W;  dW = dz^T h
 // Three products of 2 T V d operations bound a training step (the tensor pipe), reading W a forward of few tokens.
 //
 // bf16. The logits stay in the tensor cores' accumulators: the product's epilogue takes a row's largest logit m and
 // sum of exp(z - m) over a share of the vocabulary (a tile's columns, or half of them), and a pass over
-// these joins them to lse. A forward keeps nothing else. For the gradients the epilogue also stores exp(z - m), in
+// these joins them to r and s. A forward keeps nothing else. For the gradients the epilogue also stores exp(z - m), in
 // fp16: at most 1, so that fp16's range is enough (what is lost below 2^-25 is lost against 1), and rounded to 11
-// bits where bf16 would keep 8. A pass then makes dz = u (exp(z - m) exp(m - lse) - onehot) in place, in bf16, the
+// bits where bf16 would keep 8. A pass then makes dz = u (exp(z - m) exp(m - r) / s - onehot) in place, in bf16, the
 // one rounding of dz that counts, and two products make dh and dW from it. The softmax is not computed again
 // for that (a fourth product), which costs a pass over 2 bytes a logit, and room for them: so tokens are taken in
 // pieces, as many at once as cost no more room than the fp32 sums of dW over the pieces would.
@@ -202,7 +205,8 @@ struct JoinArgs {
     const float* zy;         // bf16: the target's logit as the product has it
     const __nv_bfloat16 *h, *w;
     const float* zt;         // fp32: the transposed logits
-    float *lse, *token;
+    float2* stat;            // a token's largest logit r and 1 / s
+    float* token;
     // the whole batch
     const int32_t* all_target;
     const float* all_weight;
@@ -225,10 +229,11 @@ __device__ __forceinline__ float warp_dot(const __nv_bfloat16* h, const __nv_bfl
     }
     return warp_sum(s);
 }
-// lse and the token's loss from its shares' statistics: a warp per token, and one more CTA for what the batch needs as a
+// r, s and the token's loss from its shares' statistics: a warp per token, and one more CTA for what the batch needs as a
 // whole. In bf16 the target's logit is taken once more as an fp32 dot product: the tensor cores' accumulators truncate,
 // which leaves a large logit a few 1e-6 of it short (7 tokens, d = 2048: the losses 1.2e-6 off, and 1e-7 with
-// this); lse follows by its share p_y of the difference.
+// this); its term of s, exp(z_y - r), follows. The probabilities are all of the accumulators' logits, the target's too:
+// so they add up to 1, and dz at a sure target is the sum of the others'.
 template <bool BF16> __global__ void __launch_bounds__(1024) vocab_join_kernel(const JoinArgs a) {
     pdl_begin();
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
@@ -258,19 +263,19 @@ template <bool BF16> __global__ void __launch_bounds__(1024) vocab_join_kernel(c
         }
         const float top = warp_max(m), ref = top == kNegInf ? 0.f : top;
         s = warp_sum(s * expf(m - ref));
-        float lse = ref + logf(s), l = 0.f;
+        float l = 0.f;
         if (has_target(y, a.V)) {
             if constexpr (BF16) {
-                const float z = a.zy[t], off = warp_dot(a.h + t * a.d, a.w + (int64_t)y * a.d, a.d, lane) - z;
-                const float mine = expf(z - lse) * off;
-                l = (lse - z) - (off - mine);
-                lse += mine;
+                const float z = a.zy[t];
+                const float off = z - z == 0.f ? warp_dot(a.h + t * a.d, a.w + (int64_t)y * a.d, a.d, lane) - z : 0.f;
+                // (the largest logit: of s only what the others add to its 1, so that a small loss keeps its digits)
+                l = z == ref ? log1pf((s - 1.f) * expf(-off)) : ((ref - z) - off) + logf(fmaf(expf(z - ref), expm1f(off), s));
             } else {
-                l = lse - a.zt[(int64_t)y * a.rows + t];
+                l = (ref - a.zt[(int64_t)y * a.rows + t]) + logf(s);
             }
         }
         if (lane == 0) {
-            a.lse[t] = lse;
+            a.stat[t] = make_float2(ref, 1.f / s);
             a.token[t] = l;
         }
     }
@@ -315,7 +320,7 @@ struct TotalArgs {  // of the whole batch; loss null: not in this launch
 // exp(z - m) in fp16 -> dz / scal[0] in bf16, in place. Rows of ld elements, eight a thread, four times. HBM bounds it: 4096
 // tokens, 32768 words: 80 us, 6.5 TB/s.
 __global__ void __launch_bounds__(256) vocab_dz_kernel(uint4* __restrict__ e, int64_t ld, const float2* __restrict__ part, int shares,
-                                                       int share, const float* __restrict__ lse, const int32_t* __restrict__ target,
+                                                       int share, const float2* __restrict__ stat, const int32_t* __restrict__ target,
                                                        const float* __restrict__ weight, const float* __restrict__ scal, int V,
                                                        const uint4* __restrict__ h, uint4* __restrict__ h_live, int words,
                                                        const TotalArgs total) {
@@ -330,7 +335,7 @@ __global__ void __launch_bounds__(256) vocab_dz_kernel(uint4* __restrict__ e, in
     const bool live = has_target(y, V);
     if (blockIdx.x == 0) live_row(h, h_live, t, words, live);
     const float u = !live ? 0.f : weight ? weight[t] * scal[1] : 1.f;
-    const float l = lse[t];
+    const float2 st = stat[t];
     uint4* row = e + t * (ld / 8);
     const int first = (int)blockIdx.x * (256 * U) + (int)threadIdx.x;
     uint4 v[U];
@@ -346,7 +351,7 @@ __global__ void __launch_bounds__(256) vocab_dz_kernel(uint4* __restrict__ e, in
         if (i * 8 >= V) break;
         // (a token without a target has no gradient, whatever its logits are)
         const float m = live ? part[t * shares + i * 8 / share].x : 0.f;
-        const float f = live ? u * fast_exp(m - l) : 0.f;
+        const float f = live ? u * (fast_exp(m - st.x) * st.y) : 0.f;
         uint32_t* q = reinterpret_cast<uint32_t*>(&v[k]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -406,7 +411,7 @@ __global__ void __launch_bounds__(256) vocab_col_kernel(const float* __restrict_
         part[(int64_t)c * shares + share] = make_float2(m, s);
     }
 }
-__global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z, int V, int n, const float* __restrict__ lse,
+__global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z, int V, int n, const float2* __restrict__ stat,
                                                            const int32_t* __restrict__ target, const float* __restrict__ weight,
                                                            const float* __restrict__ scal, const float* __restrict__ h,
                                                            float* __restrict__ h_live, int d, int tokens) {
@@ -418,7 +423,8 @@ __global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z
     if (t >= n) return;
     const int y = target[t];
     const bool live = has_target(y, V);
-    const float u = !live ? 0.f : weight ? weight[t] : scal[0], l = lse[t];
+    const float u = !live ? 0.f : weight ? weight[t] : scal[0];
+    const float2 st = stat[t];
     const int step = (int)(gridDim.x / tokens) * 64;  // (at most 2^18: see kVocabLossMax)
     for (int v0 = (int)(blockIdx.x / tokens) * 64 + (threadIdx.x >> 5); v0 < V; v0 += step) {
         float x[8];
@@ -427,7 +433,7 @@ __global__ void __launch_bounds__(256) vocab_dz_f32_kernel(float* __restrict__ z
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int v = v0 + 8 * k;
-            if (v < V) z[(int64_t)v * n + t] = live ? u * (expf(x[k] - l) - (v == y ? 1.f : 0.f)) : 0.f;
+            if (v < V) z[(int64_t)v * n + t] = live ? u * (expf(x[k] - st.x) * st.y - (v == y ? 1.f : 0.f)) : 0.f;
         }
     }
 }
@@ -447,7 +453,7 @@ struct Plan {
     int tn;        // columns of a logits tile
     int f32_splits, f32_rows;
     // workspace: offsets
-    size_t scal, token, lse, zy, part, e, live, sums, dwsum, offsets, total;
+    size_t scal, token, stat, zy, part, e, live, sums, dwsum, offsets, total;
 };
 
 // Products with 32 rows of A (dense_tc.cuh: AR): by the plan's tokens at once, so that a short last piece is laid out as the others.
@@ -505,7 +511,7 @@ Plan plan(int64_t T, int32_t d, int32_t V, bool bf16, bool grads) {
     };
     p.scal = take(8);
     p.token = take((size_t)t1 * 4);
-    p.lse = take((size_t)p.rows * 4);
+    p.stat = take((size_t)p.rows * 8);
     p.zy = take((size_t)p.rows * 4);
     p.part = take((size_t)p.rows * p.shares * 8);
     if (bf16) {
@@ -586,7 +592,7 @@ cudaError_t join(const Plan& pl, const VocabArgs& a, char* ws, int piece, int64_
     j.target = a.target + t0;
     j.zy = (const float*)(ws + pl.zy);
     j.zt = zt;
-    j.lse = (float*)(ws + pl.lse);
+    j.stat = (float2*)(ws + pl.stat);
     j.token = token_loss(pl, a, ws) + t0;
     j.all_target = a.target;
     j.all_weight = a.weight;
@@ -632,7 +638,7 @@ cudaError_t piece_bf16(const Plan& pl, const VocabArgs& a, char* ws, int piece, 
         if (!few(a) && piece == pl.pieces - 1 && r == 0) total.loss = a.loss;
         (void)launch_pdl(vocab_dz_kernel, dim3((unsigned)(ceil_div(V, 8 * 256 * 4) + (total.loss != nullptr)), (unsigned)std::min<int64_t>(65535, n - r)), dim3(256), 0, s,
                          (uint4*)(ws + pl.e + r * pl.ld * 2), pl.ld, (const float2*)(ws + pl.part) + r * pl.shares, pl.shares, pl.share,
-                         (const float*)(ws + pl.lse) + r, a.target + t0 + r, weight ? weight + r : nullptr, (const float*)scal, V,
+                         (const float2*)(ws + pl.stat) + r, a.target + t0 + r, weight ? weight + r : nullptr, (const float*)scal, V,
                          (const uint4*)(h + r * d), (uint4*)(ws + pl.live + r * d * 2), d / 8, total);
         MOE_TRY(cudaGetLastError());
     }
@@ -690,7 +696,7 @@ cudaError_t piece_f32(const Plan& pl, const VocabArgs& a, char* ws, int piece, c
     const int tokens = (int)ceil_div(n, 32);  // (columns of blocks)
     const int64_t dz_ctas = tokens * std::min<int64_t>(ceil_div(V, 64), std::max<int64_t>(1, 16 * 2 * kPairs / tokens));
     (void)launch_pdl(vocab_dz_f32_kernel, dim3((unsigned)dz_ctas), dim3(256), 0, s,
-                     zt, V, (int)n, (const float*)(ws + pl.lse), a.target + t0, a.weight ? a.weight + t0 : nullptr, (const float*)scal, h,
+                     zt, V, (int)n, (const float2*)(ws + pl.stat), a.target + t0, a.weight ? a.weight + t0 : nullptr, (const float*)scal, h,
                      (float*)(ws + pl.live), d, tokens);
     MOE_TRY(cudaGetLastError());
     // dh: sums over parts of the vocabulary, each a group of rows of both operands

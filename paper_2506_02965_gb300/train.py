@@ -68,7 +68,8 @@ class RoundRobinTrainer:
         return self.layer.w2
 
     def load(self, init: dict):
-        """The common initialization: w_router [n,E,d], w1, w2 as numpy arrays."""
+        """The common initialization: w_router [n,E,d], w1, w2 as numpy arrays. A run starts from it: of the updates'
+        momentum nothing is left of a run before."""
         def put(dst, a):
             dst.copy_(torch.from_numpy(np.ascontiguousarray(a)).to(dst.dtype))
 
@@ -79,6 +80,8 @@ class RoundRobinTrainer:
             put(self.m_router, init["w_router"])
             put(self.m1, init["w1"])
             put(self.m2, init["w2"])
+        for m in self.muon or ():
+            m.momentum.zero_()
 
     # ------------------------------------------------------------------ one batch
     def step(self, party: int, x, y, stream=None, record=None):

@@ -142,4 +142,6 @@ class RoundRobinTrainer:
 
     def kernels_per_step(self) -> int:
         """CUDA kernels per batch by SGD: the layer's, 2 for the loss, 3 updates."""
+        if self.muon:
+            raise ValueError('kernels_per_step counts update="sgd": an orthogonalised update\'s launches depend on its sizes')
         return self.layer.kernels_per_step() + 2 + 3

@@ -37,3 +37,12 @@ def test_a_loaded_trainer_starts_anew(L, dtype, update):
         assert all(m.momentum.any() for m in tr.muon)
         tr.load(init)
         assert not any(m.momentum.any() for m in tr.muon)
+
+
+def test_kernels_are_counted_for_sgd_only(L):
+    from paper_2506_02965_gb300.train import RoundRobinTrainer
+    sh = mi.MoEShape("t", 8, 128, 4, 128, 2, "bf16")
+    tr = RoundRobinTrainer(sh, 1, lr=0.1)
+    assert tr.kernels_per_step() == tr.layer.kernels_per_step() + 5
+    with pytest.raises(ValueError, match="sgd"):
+        RoundRobinTrainer(sh, 1, lr=0.1, update="muon").kernels_per_step()

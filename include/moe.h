@@ -525,7 +525,7 @@ moe_status moe_orthogonalise_workspace_size(int32_t groups, int32_t rows, int32_
  *   group_counts [groups] i32 or NULL: a matrix whose count is <= 0 is left out, its momentum_out and out as they were.
  * A matrix of zeros gives zeros. bf16: the products run in fp16 with fp32 sums (the values are bounded; X also with a
  * residual of 8 bits); fp32: as the fp32 GEMMs. steps in 1..16, groups up to 256 (MOE_ERR_UNSUPPORTED above), sides up to 2^24,
- * groups times the longer below 2^31.
+ * rows times cols below 2^40, groups times the longer side below 2^31.
  * out may be dw's buffer. All buffers but group_counts 16-byte aligned. Deterministic.
  */
 moe_status moe_orthogonalise(int32_t groups, int32_t rows, int32_t cols, moe_dtype dtype,

@@ -1229,7 +1229,7 @@ static moe_status check_orth(int32_t groups, int32_t rows, int32_t cols, moe_dty
     if (rows < 1 || cols < 1) return fail(MOE_ERR_INVALID_ARG, "rows=%d and cols=%d must be > 0", rows, cols);
     if (rows > 1 << 24 || cols > 1 << 24 || (int64_t)rows * cols >= (int64_t)1 << 40 ||
         (int64_t)groups * std::max(rows, cols) >= (int64_t)1 << 31)
-        return fail(MOE_ERR_INVALID_ARG, "matrices of %d x %d, %d of them: sides up to 2^24, groups * the longer < 2^31", rows, cols, groups);
+        return fail(MOE_ERR_INVALID_ARG, "matrices of %d x %d, %d of them: sides up to 2^24, rows * cols < 2^40, groups * the longer < 2^31", rows, cols, groups);
     return MOE_OK;
 }
 

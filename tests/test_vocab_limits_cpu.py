@@ -32,3 +32,11 @@ def test_vocab_loss_largest(dtype, d):
     # what the counters may reach: a grid's step of dz, a share of the column statistics, a tile
     for step in (16 * 152 * 64, 512, 256):
         assert LOSS_MAX + step + 63 < 2 ** 31
+
+
+def test_orthogonalise_elements():
+    """A matrix has fewer than 2^40 elements, and the refusal says so."""
+    for rows, cols in ((1 << 24, 1 << 16), (1 << 16, 1 << 24), (1 << 20, 1 << 20)):
+        with pytest.raises(L.MoEError, match="rows \\* cols < 2\\^40"):
+            L.moe_orthogonalise_workspace_size(1, rows, cols, L.MOE_F32)
+    assert L.moe_orthogonalise_workspace_size(1, 1 << 20, (1 << 20) - 1, L.MOE_F32) > 1 << 42

@@ -267,9 +267,13 @@ template <bool BF16> __global__ void __launch_bounds__(1024) vocab_join_kernel(c
         if (has_target(y, a.V)) {
             if constexpr (BF16) {
                 const float z = a.zy[t];
-                const float off = z - z == 0.f ? warp_dot(a.h + t * a.d, a.w + (int64_t)y * a.d, a.d, lane) - z : 0.f;
-                // (the largest logit: of s only what the others add to its 1, so that a small loss keeps its digits)
-                l = z == ref ? log1pf((s - 1.f) * expf(-off)) : ((ref - z) - off) + logf(fmaf(expf(z - ref), expm1f(off), s));
+                float off = z - z == 0.f ? warp_dot(a.h + t * a.d, a.w + (int64_t)y * a.d, a.d, lane) - z : 0.f;
+                // (logits above 2^26 are that far off; no infinity from it. The largest logit: of s only what the others add to its
+                // 1, so that a small loss keeps its digits)
+                off = fminf(fmaxf(off, -64.f), 64.f);
+                const bool first = z == ref;
+                const float c = expf(first ? -off : off);
+                l = (first ? 0.f : (ref - z) - off) + log1pf(first ? (s - 1.f) * c : fmaf(expf(z - ref), c - 1.f, s - 1.f));
             } else {
                 l = (ref - a.zt[(int64_t)y * a.rows + t]) + logf(s);
             }

@@ -11,7 +11,8 @@ half step for dz. The products' own terms and the result's rounding as in test_g
 import pytest
 import torch
 
-from tests.test_gpu_vocab_loss import DT, run
+from tests.test_gpu_vocab_loss import DT, check, run
+from tests.test_gpu_vocab_loss import make as make_plain
 
 pytestmark = pytest.mark.gpu
 
@@ -78,3 +79,15 @@ def test_a_single_word_costs_nothing(kind):
     h, w = torch.randn(70, 128, generator=g, device="cuda").mul(30).to(dt), torch.randn(1, 128, generator=g, device="cuda").to(dt)
     r = run(h, w, torch.zeros(70, dtype=torch.int32, device="cuda"), None, kind)
     assert r.loss.item() == 0 and not r.token.any() and not r.dh.any() and not r.dw.any()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(20, 1), (20, 300), (300, 2), (300, 300)])
+@pytest.mark.parametrize("size", [1e5, 1e9, 1e13])
+def test_logits_without_digits(kind, T, V, size):
+    """Logits whose fp32 step is above 1: losses within the products' error, gradients of probabilities near 0 and 1, all finite."""
+    h, w, y, _ = make_plain(T, 256, V, kind, 17)
+    h = (h.float() * size).to(h.dtype)
+    r = run(h, w, y, None, kind)
+    check(r, h, w, y, None, kind)
+    assert torch.isfinite(r.token).all() and (V > 1 or not r.token.any())

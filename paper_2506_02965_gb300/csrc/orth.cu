@@ -15,6 +15,12 @@
 //   the a X term takes X to 14 bits, its residual as an 8-bit float (e5m2, the upper half of an fp16);
 //   from the third step on B = b A + c A A is held as B + t I, and a X + B X taken as (a - t) X + (B + t I) X: most singular
 //   values are near 1 by then, B near -2.5 I, and what is left of B + t I is rounded less, as is its product with X.
+// Where few directions outweigh the rest the other singular values are not near 1 by then, and the shift costs. Off by, without the
+// result's rounding, with and without t (512 x 768, eight directions; after five steps, and after eight, 1e-3 of the norm):
+//   directions of the noise    0            3            30           100         1000
+//   five steps              0.8 / 1.6    0.65 / 1.2   0.7 / 0.4    1.8 / 1.1    3.2 / 1.9
+//   eight                   1.6 / 3.2    1.4 / 2.7    1.3 / 1.8    3.1 / 2.2    11.5 / 7.0
+// Without the residual (fp16 X, no t) five steps are 8, 23 and 40 off for the last three.
 // The other roundings stay fp16's. All sums are fp32.
 //
 // A matrix with more rows than columns is not transposed: A = X^T X and X = a X + X (b A + c A A), with the operands'

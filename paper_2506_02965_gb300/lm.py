@@ -6,7 +6,8 @@ embedding's own matrix (tied) or another. One pass is
   forward : moe_embed_fwd -> the stack's forward -> moe_vocab_loss (the loss, the gradients of the states and of W_out)
   backward: the stack's backward -> moe_embed_bwd (added to W_out's gradient where the two are tied)
 
-The logits are never in memory. A padding token has id < 0 (its state is zero) and a token whose loss does not count
+The logits are never in memory. In bf16 a tied matrix's gradient is rounded twice, as the loss's part and again when the embedding's
+is added to it (in fp32, to the rounded one). A padding token has id < 0 (its state is zero) and a token whose loss does not count
 target < 0.
 
 ``Muon``: the update of a set of matrices of one size (the experts' W1 or W2, a router's): momentum, moe_orthogonalise,

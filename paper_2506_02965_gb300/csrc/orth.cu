@@ -652,7 +652,8 @@ Plan plan(int G, int rows, int cols, bool bf16) {
     // with 8, 1691 with 16, 1657 with 48, 1664 with 96, whole lines alike), but no more than 8 where a matrix's CTAs, each of
     // which adds up all of its matrix's parts, would read more of those than 12/16 of a byte for each value beside the 13 bytes that
     // the value moves: one step of 1 x 4096 x 4096 249 us, 280 with 48; 2 x 4096 x 4096 470, 487; 4 x 2048 x 2048 179, 196;
-    // 1 x 8192 x 8192 1526, 1545 (with a whole byte more or a quarter of them within 3%; the many matrices above keep their 48).
+    // 1 x 8192 x 8192 1526, 1545 (with 3 bytes a value 252, 472, 183, 1524, with 3/16 249, 465, 185, 1524; the many matrices above keep
+    // their 48).
     const int64_t few = (int64_t)std::sqrt((double)rows * cols / 16);
     p.parts = (int)std::max<int64_t>(1, std::min({want, ceil_div(96 * kPairs, G), std::max(ceil_div(16 * kPairs, G), few)}));
     p.splits = 1;

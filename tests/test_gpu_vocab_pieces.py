@@ -59,3 +59,28 @@ def test_small_weights(kind, T, size):
         assert ((got.double() - ref).abs() <= lim).all(), ((got.double() - ref).abs() / lim).max()
         if size >= 1e-33:  # zeros, or another size's values, are far outside
             assert ref.norm() >= 10 * lim.norm(), (ref.norm() / lim.norm())
+
+
+@pytest.mark.slow
+def test_the_largest_vocabulary():
+    """One token against 2^31 - 1 - 2^18 words (35 GB of W and of dW): logits of 0 but for the last three words'. A lane of the statistics
+    adds up 2^17 shares of 512 equal terms, each half a step off: 2^17 2^-25 of its sum, a 32nd of V exp(-24) = 0.081, in 32 lanes."""
+    T, d, V = 1, 4, 2 ** 31 - 1 - 2 ** 18
+    w = torch.zeros(V, d, device="cuda")
+    w[-3:, 0] = torch.tensor([1.0, 2.0, 3.0], device="cuda")
+    h = torch.tensor([[8.0, 0.0, 0.0, 0.0]], device="cuda")
+    y = torch.tensor([V - 1], dtype=torch.int32, device="cuda")
+    r = run(h, w, y, None, "f32")
+    e = torch.exp(torch.tensor([-24.0, -16.0, -8.0, 0.0], dtype=torch.float64))
+    total = ((V - 3) * e[0] + e[1] + e[2] + e[3]).item()
+    p = [x.item() / total for x in e]
+    off = 2.0 ** 17 * 2.0 ** -25 * V * e[0].item() / total + 2.0 ** -20  # relative, of s and so of every probability
+    assert abs(r.token.item() - torch.log(torch.tensor(total, dtype=torch.float64)).item()) <= off and torch.equal(r.loss, r.token)
+    rest = r.dw[:-3, 0]
+    for extreme in (rest.amin(), rest.amax()):  # the first rows, those past 2^30 and the last ones alike
+        assert abs(extreme.item() - 8 * p[0]) <= 8 * p[0] * (off + 2.0 ** -20)
+    for i, want in ((-3, p[1]), (-2, p[2]), (-1, p[3] - 1.0)):
+        assert abs(r.dw[i, 0].item() - 8 * want) <= 8 * (p[3] * off + 2.0 ** -20)
+    assert r.dw[:, 1:].amax().item() == 0 and r.dw[:, 1:].amin().item() == 0
+    assert abs(r.dh[0, 0].item() - (p[1] + 2 * p[2] + 3 * (p[3] - 1.0))) <= 3 * off + 2.0 ** -18 and not r.dh[0, 1:].any()
+    assert L.moe_device_status() == 0

@@ -11,7 +11,8 @@
 // these joins them to r and s. A forward keeps nothing else. For the gradients the epilogue also stores exp(z - m), in
 // fp16: at most 1, and rounded to 11 bits where bf16 would keep 8, down to 2^-14; below, steps of 2^-24 are left (8 bits at 2^-17, as
 // bf16; none from 2^-25 on): a word that far under a neighbour of its share loses its probability, which is lost
-// against the neighbour's 1 in dh, but in the word's own row of dW only against other tokens' parts. A pass then makes dz = u (exp(z - m) exp(m - r) / s - onehot) in place, in bf16, the
+// against the neighbour's 1 in dh, but in the word's own row of dW only against other tokens' parts.
+// A pass then makes dz = u (exp(z - m) exp(m - r) / s - onehot) in place, in bf16, the
 // one rounding of dz that counts, and two products make dh and dW from it. The softmax is not computed again
 // for that (a fourth product), which costs a pass over 2 bytes a logit, and room for them: so tokens are taken in
 // pieces, as many at once as cost no more room than the fp32 sums of dW over the pieces would.
